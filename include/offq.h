@@ -33,7 +33,16 @@
  *                              key cache / queries with the structured M (bf16)
  *
  * and the offline transform builder (top-1 tokens, top-1 PCA direction,
- * reflection, sorted grouping, fusion into the weights).
+ * reflection, sorted grouping, fusion into the weights),
+ *
+ * and what a decoder layer does between its linears:
+ *
+ *   offq_rope_heads        RMS norm, rotary positions and H3 of heads, one pass
+ *   offq_kv4_paged_write   the same for queries and keys; keys and values into
+ *                          the pages of a 4-bit cache
+ *   offq_kv4_paged_read    cached tokens back as values
+ *   offq_paged_attention   new tokens (one or many per sequence) over the pages
+ *   offq_prompt_attention  packed prompts on 16-bit keys and values
  *
  * Conventions shared by every call
  *   - Pointers named as device buffers are device pointers allocated and owned
@@ -46,8 +55,8 @@
  *     returns OFFQ_ERR_MISALIGNED; a failed launch returns OFFQ_ERR_CUDA.
  *     Nothing is written when a call returns an error.
  *   - Errors that only the device can see (a bounded wait that ran out inside
- *     a kernel) are recorded in a device status word; offq_get_device_status
- *     reads and clears it.
+ *     a kernel, an index in a device buffer outside its range) are recorded in
+ *     a device status word; offq_get_device_status reads and clears it.
  *   - NaN or Inf inputs: results are unspecified (no checks on the hot path).
  *   - Calls are thread-safe. The only state is set on first use per device
  *     (kernel attributes, the SM count, the status word's address) and the
@@ -107,7 +116,10 @@ enum { OFFQ_F32 = 0, OFFQ_BF16 = 1, OFFQ_F16 = 2 };
 /* Flags of the quantizers. */
 enum {
   OFFQ_ROTATE = 1, /* apply the online block Hadamard H/sqrt(g) (Eq. 4)       */
-  OFFQ_OFFSET = 2  /* subtract each block's mean as its offset (Eq. 5)        */
+  OFFQ_OFFSET = 2, /* subtract each block's mean as its offset (Eq. 5)        */
+  /* The calls between the projections and attention also take */
+  OFFQ_INTERLEAVED = 4, /* rotary pairs (2m, 2m + 1) instead of (m, m + rot_dim / 2) */
+  OFFQ_ROTATE_V = 8     /* the Hadamard for the values too                     */
 };
 
 /* Forms of offq_w4a4_linear (offq_w4a4_linear_form). */
@@ -571,6 +583,141 @@ int offq_mx_linear(const uint8_t* a_codes, const uint8_t* a_shifts, const float*
                    int64_t T, int64_t N, int64_t K, int32_t g, const uint8_t* w_codes, const uint8_t* w_shifts,
                    const float* w_scale, const float* w_offsum, void* out, int out_dtype, int64_t ldo, void* stream);
 
+/*
+ * Heads between the projections and attention. Keys take H3 after the rotary
+ * positions and before the cache (Sec. 3.3 Step 2 (3)); the queries take the
+ * same rotation, so that Q K^T is unchanged.
+ *
+ * offq_rope_heads -- for each token t and head h, x of head_dim channels:
+ *   x <- (x * (1 / sqrt(mean(x^2) + eps))) * norm[h]    if norm is given
+ *   (x_a, x_b) <- (x_a c_m - x_b s_m, x_b c_m + x_a s_m)  for m < rot_dim / 2,
+ *       (a, b) = (m, m + rot_dim / 2), or (2m, 2m + 1) with OFFQ_INTERLEAVED;
+ *       c_m = table[p][m], s_m = table[p][rot_dim / 2 + m], p = positions[t]
+ *   y = x H / sqrt(head_dim) with OFFQ_ROTATE, else x
+ * in fp32, rounded once to out_dtype. Other channels pass the rotary step
+ * unchanged. Long-context scaling is a matter of the table's contents.
+ *
+ *   x         device, element (t, h, d) at x[t*ld_token + h*head_dim + d] of dtype;
+ *             16-byte aligned, ld_token * sizeof(elem) a multiple of 16,
+ *             ld_token >= H * head_dim. out may be x itself (same type and ld).
+ *   T, H      tokens (>= 0) and heads (1..65535).
+ *   head_dim  64 or 128 (OFFQ_ERR_UNSUPPORTED otherwise).
+ *   positions device, [T] int32. A position outside [0, max_pos) leaves its
+ *             token's rows unwritten and records OFFQ_ERR_INVALID_ARG in the
+ *             device status word.
+ *   table     device, [max_pos][rot_dim] float32, 16-byte aligned.
+ *   rot_dim   0 (no rotary positions; positions and table unused) to head_dim,
+ *             a multiple of 16 (other even values: OFFQ_ERR_UNSUPPORTED).
+ *   norm      device, [H][head_dim] float32, 16-byte aligned, or NULL.
+ *   flags     OR of OFFQ_ROTATE, OFFQ_INTERLEAVED.
+ *   out       device, as x with ld_out and out_dtype.
+ *
+ * Arithmetic: each operation above is rounded on its own. mean(x^2) sums
+ * neighbours first (a balanced tree); the Hadamard is a radix-2 tree of
+ * additions, distance 1 first, then one product with fp32(1/sqrt(head_dim)).
+ */
+int offq_rope_heads(const void* x, int dtype, int64_t T, int32_t H, int32_t head_dim, int64_t ld_token,
+                    const int32_t* positions, const float* table, int64_t max_pos, int32_t rot_dim,
+                    const float* norm, float eps, int32_t flags, void* out, int out_dtype, int64_t ld_out,
+                    void* stream);
+
+/*
+ * A paged 4-bit cache of one layer is four buffers of the caller:
+ *   k_codes, v_codes    [pages][H][page_size][head_dim / 2] uint8: codes u = q + 8
+ *                       as nibbles, even channel low (the row-major form of
+ *                       offq_kv4_quantize), 16-byte aligned
+ *   k_params, v_params  [pages][H][page_size][2] float32: (scale, offset) of the
+ *                       head's vector, 16-byte aligned
+ * so a head's tokens of one page are contiguous. Slot s is token s % page_size of
+ * page s / page_size. page_size is 16, 32, 64, 128 or 256 (other values:
+ * OFFQ_ERR_UNSUPPORTED). Slots that hold no token may hold anything.
+ *
+ * offq_kv4_paged_write -- keys as in offq_rope_heads (k_norm, table, OFFQ_ROTATE),
+ * then quantized into the token's slot; values quantized as they are (or rotated
+ * with OFFQ_ROTATE_V); in the same launch the Hq query heads as in offq_rope_heads
+ * (q_norm) to q_out. The codes of a vector y (after the rotation, if any):
+ *   o = mean(y) with OFFQ_OFFSET (else 0; with the rotation fl(x_0 / sqrt(d))),
+ *   r = y - o, s = max|r| / 7, u = clamp(rne(r * (7 / max|r|)), -7, 7) + 8.
+ *
+ *   q, k, v   device, as x in offq_rope_heads with their own leading dimensions.
+ *             Hq may be 0 (q, q_out unused); H counts the key and value heads.
+ *   slots     device, [T] int64. A negative slot writes no key or value; one
+ *             past the cache records OFFQ_ERR_INVALID_ARG in the device status
+ *             word and writes none. Two tokens of a call may not share a slot.
+ *   flags     OR of OFFQ_ROTATE (queries and keys), OFFQ_OFFSET,
+ *             OFFQ_INTERLEAVED, OFFQ_ROTATE_V.
+ */
+int offq_kv4_paged_write(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq, int32_t H,
+                         int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v, const int32_t* positions,
+                         const float* table, int64_t max_pos, int32_t rot_dim, const float* q_norm,
+                         const float* k_norm, float eps, int32_t flags, const int64_t* slots, uint8_t* k_codes,
+                         float* k_params, uint8_t* v_codes, float* v_params, int64_t pages, int32_t page_size,
+                         void* q_out, int out_dtype, int64_t ld_q_out, void* stream);
+
+/*
+ * offq_kv4_paged_read -- s (u - 8) + o of the tokens in slots, the keys times
+ * H / sqrt(head_dim) with OFFQ_ROTATE (the rotation undone), the values with
+ * OFFQ_ROTATE_V, rounded once to out_dtype.
+ *   slots     device, [T] int64; a slot outside the cache gives zeros (one past
+ *             it is also recorded in the device status word).
+ *   k_out, v_out  device, [T][ld_k / ld_v], heads contiguous; either may be NULL.
+ */
+int offq_kv4_paged_read(const uint8_t* k_codes, const float* k_params, const uint8_t* v_codes, const float* v_params,
+                        int64_t pages, int32_t page_size, int32_t H, int32_t head_dim, const int64_t* slots,
+                        int64_t T, int32_t flags, void* k_out, void* v_out, int out_dtype, int64_t ld_k,
+                        int64_t ld_v, void* stream);
+
+/*
+ * offq_paged_attention -- attention of each sequence's newest tokens over its
+ * pages (which hold them already). Sequence b has len = lens[b] cached tokens, of
+ * which its n = cu_q[b + 1] - cu_q[b] queries are the last: query i sees tokens
+ * 0 .. len - n + i. Per query i and head h, with kv head h / (Hq / H):
+ *   z_j = scale * q_i . k_j,  out_i = sum_j e^(z_j - m) v_j / sum_j e^(z_j - m),
+ *   lse_i = log sum_j e^z_j,
+ * k_j and v_j the cached values s (u - 8) + o. A query that sees nothing
+ * (len - n + i < 0) gets out 0 and lse -inf. The codes enter the products
+ * exactly; softmax statistics and sums are fp32.
+ *
+ *   q         device, element (t, h, d) at q[t*ld_q + h*head_dim + d], dtype
+ *             OFFQ_BF16 or OFFQ_F16 (OFFQ_F32: OFFQ_ERR_UNSUPPORTED), 16-byte
+ *             aligned, ld_q a multiple of 8; in the keys' rotated basis.
+ *   Tq        query rows in all sequences; Hq a multiple of H, Hq / H <= 64.
+ *   block_table  device, [B][ld_table] int32: the pages of a sequence, in order.
+ *             Entries past its length are not read; one outside [0, pages) counts
+ *             as a page of nothing that is seen, and is recorded in the device
+ *             status word, as is a length past ld_table * page_size (cut there).
+ *   lens      device, [B] int32.   cu_q  device, [B + 1] int32, cu_q[0] = 0,
+ *             non-decreasing, cu_q[B] <= Tq.
+ *   max_q     most queries of one sequence. A sequence with more is recorded in
+ *             the device status word and left out.
+ *   out       device, as q with ld_out.   lse  device, [Tq][Hq] float32 or NULL.
+ *   workspace device, 16-byte aligned, offq_paged_attention_workspace(...) bytes
+ *             of the same sizes (NULL if that is 0); its contents mean nothing
+ *             between calls, and calls on different streams need one each.
+ */
+int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int64_t ld_q,
+                         const uint8_t* k_codes, const float* k_params, const uint8_t* v_codes, const float* v_params,
+                         int64_t pages, int32_t page_size, const int32_t* block_table, int64_t ld_table,
+                         const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q, float scale, void* out,
+                         int64_t ld_out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of offq_paged_attention's workspace on the current device (-1 on sizes
+ * it refuses). */
+int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B, int32_t max_q);
+
+/*
+ * offq_prompt_attention -- attention inside packed sequences: rows cu[b] ..
+ * cu[b + 1] - 1 of q, k and v are sequence b; query i sees keys 0 .. i (all of
+ * the sequence's with causal = 0). Formulas, q, out and lse as in
+ * offq_paged_attention; k and v [T][H][head_dim] with ld_k, ld_v (multiples of 8)
+ * of the same type. cu: device, [B + 1] int32, non-decreasing, cu[B] <= T; rows
+ * outside cu[0] .. cu[B] are left as they are. What one sequence holds (infinities
+ * or NaN too) does not reach another's outputs.
+ */
+int offq_prompt_attention(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq, int32_t H,
+                          int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v, const int32_t* cu, int32_t B,
+                          float scale, int32_t causal, void* out, int64_t ld_out, float* lse, void* stream);
+
 /* Bytes of a tiled MXFP4 shift buffer for R rows of K channels (-1 unless K is
  * a positive multiple of 128 and R >= 0): ceil(R/32) * 32 * K / 32. */
 int64_t offq_mx_shift_bytes(int64_t R, int64_t K);
@@ -584,8 +731,9 @@ int64_t offq_weight_codes_bytes(int64_t N, int64_t K);
 
 /*
  * offq_get_device_status -- synchronizes `stream`, returns the device status
- * word of the current device (OFFQ_OK, or OFFQ_ERR_TIMEOUT when a kernel's
- * bounded wait ran out since the last call) and clears it. Returns
+ * word of the current device (OFFQ_OK; OFFQ_ERR_TIMEOUT when a kernel's bounded
+ * wait ran out since the last call; OFFQ_ERR_INVALID_ARG when a kernel met a
+ * position, slot, page or length outside what its call allows) and clears it. Returns
  * OFFQ_ERR_CUDA if the synchronization itself fails.
  */
 int offq_get_device_status(void* stream);

@@ -1,0 +1,574 @@
+// Heads on their way into attention: RMS norm, rotary positions and the per-head Hadamard H3 in one
+// pass (offq_rope_heads); the same for queries and keys with keys and values quantized into a paged
+// 4-bit cache (offq_kv4_paged_write); cached tokens read back (offq_kv4_paged_read).
+//
+// For a head x of D channels (all fp32):
+//   norm    x <- (x * (1 / sqrt(mean(x^2) + eps))) * w[h]
+//   rotary  (x_a, x_b) <- (x_a c - x_b s, x_b c + x_a s) on the first rot_dim channels, pairs
+//           (m, m + rot_dim / 2) or (2m, 2m + 1), c and s from the table row of the position
+//   H3      y = x H_D / sqrt(D), a radix-2 tree of additions, distance 1 first
+//   codes   o = mean(y) (with H3: x_0 / sqrt(D)), r = y - o, s = max|r| / 7,
+//           u = clamp(rne(r * (7 / max|r|)), -7, 7) + 8
+// Every operation above is rounded on its own (no contraction), so the codes are a function of the
+// formula and not of the compiler.
+//
+// A lane owns 8 neighbouring channels (one 16-byte load of a 16-bit type), so a head of 128 takes
+// half a warp and a head of 64 a quarter; sums, maxima and the outer butterflies are xor shuffles.
+// A warp stays with one token and takes several groups of heads, with the token's cosines and sines
+// in registers: they would otherwise be read again for each head, four times the data's own bytes.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "offq.h"
+#include "offq_device.cuh"
+#include "offq_host.h"
+
+namespace {
+
+using namespace offq;
+
+constexpr int kE = 8;        // channels per lane
+constexpr int kWarps = 8;    // warps per CTA
+constexpr uint32_t kAll = 0xFFFFFFFFu;
+
+struct HeadArgs {
+  // Virtual heads of a token: H[0] queries, H[1] keys, H[2] values.
+  const void* x[3];
+  int64_t ld[3];
+  int H[3];
+  const float* norm[2];
+  int64_t T;
+  const int32_t* pos;
+  const float* table;
+  int64_t max_pos;
+  int rot;           // channels that take the rotary positions (0: none)
+  int interleaved;
+  float eps;
+  int rotate[3];     // H3
+  int offset;
+  void* out;         // queries
+  int64_t ld_out;
+  const int64_t* slots;
+  uint8_t* codes[2];
+  float* params[2];
+  int64_t slots_in_cache;
+  int page_shift;
+  int iters;         // groups of heads per warp
+  int* status;
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[kE]) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+      }
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[kE]) {
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+      } else {
+        const __half2 b = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// Sum of a head's channels, neighbours first, in every lane of the head.
+template <int D>
+__device__ __forceinline__ float head_sum(const float (&v)[kE]) {
+  float s = __fadd_rn(__fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3])),
+                      __fadd_rn(__fadd_rn(v[4], v[5]), __fadd_rn(v[6], v[7])));
+#pragma unroll
+  for (int m = 1; m < D / kE; m <<= 1) s = __fadd_rn(s, __shfl_xor_sync(kAll, s, m));
+  return s;
+}
+
+template <int D>
+__device__ __forceinline__ float head_absmax(const float (&v)[kE]) {
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) s = fmaxf(s, fabsf(v[e]));
+#pragma unroll
+  for (int m = 1; m < D / kE; m <<= 1) s = fmaxf(s, __shfl_xor_sync(kAll, s, m));
+  return s;
+}
+
+// x H_D, not normalised.
+template <int D>
+__device__ __forceinline__ void head_hadamard(float (&v)[kE], int lane) {
+#pragma unroll
+  for (int h = 1; h < kE; h <<= 1) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      if (e & h) continue;
+      const float a = v[e], b = v[e + h];
+      v[e] = __fadd_rn(a, b);
+      v[e + h] = __fsub_rn(a, b);
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < D / kE; m <<= 1) {
+    const float sign = (lane & m) ? -1.f : 1.f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      const float o = __shfl_xor_sync(kAll, v[e], m);
+      v[e] = __fmaf_rn(sign, v[e], o);  // o + v or o - v: the product with +-1 is exact
+    }
+  }
+}
+
+// Cosines and sines of this lane's channels: with neighbouring pairs the first four of each.
+struct Angles {
+  float c[kE], s[kE];
+};
+
+template <int D>
+__device__ __forceinline__ void load_angles(const HeadArgs& a, const float* row, int d0, Angles& t) {
+  const int half = a.rot / 2;
+  if (d0 >= a.rot) return;
+  if (a.interleaved) {
+    const float4 c = __ldg(reinterpret_cast<const float4*>(row + d0 / 2));
+    const float4 s = __ldg(reinterpret_cast<const float4*>(row + half + d0 / 2));
+    t.c[0] = c.x; t.c[1] = c.y; t.c[2] = c.z; t.c[3] = c.w;
+    t.s[0] = s.x; t.s[1] = s.y; t.s[2] = s.z; t.s[3] = s.w;
+  } else {
+    const int f = d0 < half ? d0 : d0 - half;
+    load8(row + f, t.c);
+    load8(row + half + f, t.s);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void rotary(const HeadArgs& a, const Angles& t, int d0, int lane, float (&v)[kE]) {
+  if (a.rot == 0) return;
+  if (a.interleaved) {
+    if (d0 >= a.rot) return;
+#pragma unroll
+    for (int m = 0; m < kE / 2; ++m) {
+      const float x = v[2 * m], y = v[2 * m + 1];
+      v[2 * m] = __fsub_rn(__fmul_rn(x, t.c[m]), __fmul_rn(y, t.s[m]));
+      v[2 * m + 1] = __fadd_rn(__fmul_rn(y, t.c[m]), __fmul_rn(x, t.s[m]));
+    }
+    return;
+  }
+  const int half = a.rot / 2, step = half / kE;  // rot_dim is a multiple of 16: a pair is two lanes, same element
+  const bool first = d0 < half, in = d0 < a.rot;
+  const int src = in ? (first ? lane + step : lane - step) : lane;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const float o = __shfl_sync(kAll, v[e], src);
+    if (in) {
+      const float p = __fmul_rn(v[e], t.c[e]), q = __fmul_rn(o, t.s[e]);
+      v[e] = first ? __fsub_rn(p, q) : __fadd_rn(p, q);
+    }
+  }
+}
+
+// Codes of a head y (before H3 where `rotate`) into its slot.
+template <int D>
+__device__ __forceinline__ void quantize_head(float (&v)[kE], bool rotate, bool offset, bool live, int lane,
+                                              uint8_t* codes, float* params) {
+  constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;  // 1 / sqrt(D) in fp32
+  const int l = lane % (D / kE);
+  float o = 0.f;
+  if (rotate) {
+    if (offset) {
+      o = __fmul_rn(__shfl_sync(kAll, v[0], lane - l), kRoot);
+      if (l == 0) v[0] = 0.f;  // the first row of H_D is all ones: without x_0 the mean is 0
+    }
+    head_hadamard<D>(v, lane);
+  } else if (offset) {
+    o = __fmul_rn(head_sum<D>(v), 1.0f / D);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) v[e] = __fsub_rn(v[e], o);
+  }
+  const float top = head_absmax<D>(v);
+  const float inv = top > 0.f ? __fdiv_rn(7.0f, top) : 0.f;
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const float q = fminf(fmaxf(rintf(__fmul_rn(v[e], inv)), -7.f), 7.f);
+    w |= static_cast<uint32_t>(static_cast<int>(q) + 8) << (4 * e);
+  }
+  if (!live) return;
+  reinterpret_cast<uint32_t*>(codes)[l] = w;
+  if (l == 0) {
+    const float s = rotate ? __fmul_rn(__fmul_rn(top, kRoot), 1.0f / 7.0f) : __fmul_rn(top, 1.0f / 7.0f);
+    *reinterpret_cast<float2*>(params) = make_float2(s, o);
+  }
+}
+
+template <int D, typename Tin, typename Tout>
+__global__ void __launch_bounds__(kWarps * 32) heads_kernel(const HeadArgs a) {
+  constexpr int kLanes = D / kE, kUnits = 32 / kLanes;  // lanes per head, heads per warp
+  constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
+  const int lane = threadIdx.x & 31, l = lane % kLanes, unit = lane / kLanes;
+  griddep_wait();
+  griddep_launch_dependents();
+  // Groups of kUnits heads of one kind, so that a warp does not mix kinds.
+  const int g0 = (a.H[0] + kUnits - 1) / kUnits, g1 = g0 + (a.H[1] + kUnits - 1) / kUnits;
+  const int groups = g1 + (a.H[2] + kUnits - 1) / kUnits;
+  const int parts = (groups + a.iters - 1) / a.iters;
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t t = w / parts;
+  if (t >= a.T) return;
+  const int first = static_cast<int>(w % parts) * a.iters, last = min(groups, first + a.iters);
+
+  Angles ang = {};
+  bool pos_ok = true;
+  if (a.rot != 0 && first < g1) {
+    const int64_t p = __ldg(a.pos + t);
+    pos_ok = p >= 0 && p < a.max_pos;
+    if (pos_ok) load_angles<D>(a, a.table + p * a.rot, l * kE, ang);
+  }
+  int64_t slot = -1;
+  if (last > g0) {
+    slot = __ldg(a.slots + t);
+    if (slot >= a.slots_in_cache) {
+      slot = -1;
+      if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+    }
+  }
+  if (!pos_ok && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+
+  for (int g = first; g < last; ++g) {
+    const int kind = g < g0 ? 0 : g < g1 ? 1 : 2;
+    const int h = (g - (kind == 0 ? 0 : kind == 1 ? g0 : g1)) * kUnits + unit;
+    bool live = h < a.H[kind];
+    float v[kE];
+    load8(static_cast<const Tin*>(a.x[kind]) + t * a.ld[kind] + static_cast<int64_t>(live ? h : 0) * D + l * kE, v);
+    if (kind < 2) {
+      if (a.norm[kind] != nullptr) {
+        float sq[kE], wt[kE];
+        load8(a.norm[kind] + static_cast<int64_t>(live ? h : 0) * D + l * kE, wt);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) sq[e] = __fmul_rn(v[e], v[e]);
+        const float mean = __fmul_rn(head_sum<D>(sq), 1.0f / D);
+        const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(mean, a.eps)));
+#pragma unroll
+        for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(__fmul_rn(v[e], inv), wt[e]);
+      }
+      rotary<D>(a, ang, l * kE, lane, v);
+      live = live && pos_ok;
+    }
+    if (kind == 0) {
+      if (a.rotate[0]) {
+        head_hadamard<D>(v, lane);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(v[e], kRoot);
+      }
+      if (live) store8(static_cast<Tout*>(a.out) + t * a.ld_out + static_cast<int64_t>(h) * D + l * kE, v);
+      continue;
+    }
+    live = live && slot >= 0;
+    const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
+    const int64_t row = (((page * a.H[kind]) + h) << a.page_shift) + at;
+    quantize_head<D>(v, a.rotate[kind] != 0, a.offset != 0, live, lane, a.codes[kind - 1] + (live ? row * (D / 2) : 0),
+                     a.params[kind - 1] + (live ? row * 2 : 0));
+  }
+}
+
+struct ReadArgs {
+  const uint8_t* codes[2];
+  const float* params[2];
+  void* out[2];
+  int64_t ld[2];
+  int rotate[2];
+  int64_t T, slots_in_cache;
+  int H, page_shift;
+  const int64_t* slots;
+  int iters;
+  int* status;
+};
+
+// Values s (u - 8) + o of cached heads, keys taken back by H3 (symmetric and orthonormal: its own inverse).
+template <int D, typename Tout>
+__global__ void __launch_bounds__(kWarps * 32) read_kernel(const ReadArgs a) {
+  constexpr int kLanes = D / kE, kUnits = 32 / kLanes;
+  constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
+  const int lane = threadIdx.x & 31, l = lane % kLanes, unit = lane / kLanes;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int groups = (a.H + kUnits - 1) / kUnits, parts = (2 * groups + a.iters - 1) / a.iters;
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t t = w / parts;
+  if (t >= a.T) return;
+  int64_t slot = __ldg(a.slots + t);
+  if (slot >= a.slots_in_cache) {
+    slot = -1;
+    if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+  }
+  const int first = static_cast<int>(w % parts) * a.iters, last = min(2 * groups, first + a.iters);
+  for (int g = first; g < last; ++g) {
+    const int kind = g >= groups;
+    const int h = (g - kind * groups) * kUnits + unit;
+    const bool live = h < a.H;
+    if (a.out[kind] == nullptr) continue;
+    float v[kE] = {};
+    if (live && slot >= 0) {
+      const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
+      const int64_t row = (((page * a.H) + h) << a.page_shift) + at;
+      const uint32_t c = __ldg(reinterpret_cast<const uint32_t*>(a.codes[kind] + row * (D / 2)) + l);
+      const float2 p = __ldg(reinterpret_cast<const float2*>(a.params[kind]) + row);
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+        v[e] = __fadd_rn(__fmul_rn(static_cast<float>(static_cast<int>((c >> (4 * e)) & 15u) - 8), p.x), p.y);
+    }
+    if (a.rotate[kind]) {
+      head_hadamard<D>(v, lane);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(v[e], kRoot);
+    }
+    if (live) store8(static_cast<Tout*>(a.out[kind]) + t * a.ld[kind] + static_cast<int64_t>(h) * D + l * kE, v);
+  }
+}
+
+// Groups of heads per warp: several where there are enough warps to fill the chip without it.
+int groups_per_warp(int64_t T, int groups, int sms) {
+  const int64_t per = T * groups / (static_cast<int64_t>(sms) * 64);
+  return static_cast<int>(std::clamp<int64_t>(per, 1, 8));
+}
+
+template <int D, typename Tin, typename Tout>
+int launch_heads(HeadArgs a, int sms, cudaStream_t s) {
+  constexpr int kUnits = 32 * kE / D;
+  const int groups = (a.H[0] + kUnits - 1) / kUnits + (a.H[1] + kUnits - 1) / kUnits + (a.H[2] + kUnits - 1) / kUnits;
+  a.iters = groups_per_warp(a.T, groups, sms);
+  const int64_t warps = a.T * ((groups + a.iters - 1) / a.iters), blocks = (warps + kWarps - 1) / kWarps;
+  if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
+  return launch_pdl(heads_kernel<D, Tin, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kWarps * 32), 0, s, a);
+}
+
+template <int D, typename Tin>
+int launch_heads_out(const HeadArgs& a, int out_dtype, int sms, cudaStream_t s) {
+  switch (out_dtype) {
+    case OFFQ_F32: return launch_heads<D, Tin, float>(a, sms, s);
+    case OFFQ_BF16: return launch_heads<D, Tin, __nv_bfloat16>(a, sms, s);
+    default: return launch_heads<D, Tin, __half>(a, sms, s);
+  }
+}
+
+template <int D>
+int launch_heads_in(const HeadArgs& a, int dtype, int out_dtype, int sms, cudaStream_t s) {
+  switch (dtype) {
+    case OFFQ_F32: return launch_heads_out<D, float>(a, out_dtype, sms, s);
+    case OFFQ_BF16: return launch_heads_out<D, __nv_bfloat16>(a, out_dtype, sms, s);
+    default: return launch_heads_out<D, __half>(a, out_dtype, sms, s);
+  }
+}
+
+int run_heads(HeadArgs& a, int dtype, int out_dtype, int head_dim, void* stream) {
+  a.status = device_status_ptr();
+  const int sms = device_sms();
+  if (a.status == nullptr || sms == 0) return OFFQ_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return head_dim == 128 ? launch_heads_in<128>(a, dtype, out_dtype, sms, s)
+                         : launch_heads_in<64>(a, dtype, out_dtype, sms, s);
+}
+
+template <int D, typename Tout>
+int launch_read(ReadArgs a, int sms, cudaStream_t s) {
+  constexpr int kUnits = 32 * kE / D;
+  const int groups = 2 * ((a.H + kUnits - 1) / kUnits);
+  a.iters = groups_per_warp(a.T, groups, sms);
+  const int64_t warps = a.T * ((groups + a.iters - 1) / a.iters), blocks = (warps + kWarps - 1) / kWarps;
+  if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
+  return launch_pdl(read_kernel<D, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kWarps * 32), 0, s, a);
+}
+
+bool dtype_ok(int d) { return elem_bytes(d) != 0; }
+
+// Shape rules that the calls of this file share.
+int check_heads(int64_t T, int64_t H, int32_t head_dim) {
+  if (T < 0 || H < 1 || head_dim < 1) return OFFQ_ERR_INVALID_ARG;
+  if ((head_dim != 64 && head_dim != 128) || H > 65535 || T > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
+  return OFFQ_OK;
+}
+
+int check_rotary(const int32_t* positions, const float* table, int64_t max_pos, int32_t rot_dim, int32_t head_dim) {
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 2 != 0) return OFFQ_ERR_INVALID_ARG;
+  if (rot_dim % 16 != 0) return OFFQ_ERR_UNSUPPORTED;
+  if (rot_dim > 0 && (positions == nullptr || table == nullptr || max_pos < 1)) return OFFQ_ERR_INVALID_ARG;
+  return OFFQ_OK;
+}
+
+bool row_ok(const void* p, int64_t ld, int bytes) { return aligned(p, 16) && (ld * bytes) % 16 == 0; }
+
+}  // namespace
+
+extern "C" int offq_rope_heads(const void* x, int dtype, int64_t T, int32_t H, int32_t head_dim, int64_t ld_token,
+                               const int32_t* positions, const float* table, int64_t max_pos, int32_t rot_dim,
+                               const float* norm, float eps, int32_t flags, void* out, int out_dtype, int64_t ld_out,
+                               void* stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(out_dtype) || (flags & ~(OFFQ_ROTATE | OFFQ_INTERLEAVED)) != 0 || !(eps >= 0.f))
+    return OFFQ_ERR_INVALID_ARG;
+  if (const int rc = check_heads(T, H, head_dim); rc != OFFQ_OK) return rc;
+  const int64_t width = static_cast<int64_t>(H) * head_dim;
+  if (ld_token < width || ld_out < width) return OFFQ_ERR_INVALID_ARG;
+  if (T == 0) return OFFQ_OK;
+  if (x == nullptr || out == nullptr) return OFFQ_ERR_INVALID_ARG;
+  if (const int rc = check_rotary(positions, table, max_pos, rot_dim, head_dim); rc != OFFQ_OK) return rc;
+  if (!row_ok(x, ld_token, elem_bytes(dtype)) || !row_ok(out, ld_out, elem_bytes(out_dtype)) || !aligned(table, 16) ||
+      !aligned(norm, 16) || !aligned(positions, 4))
+    return OFFQ_ERR_MISALIGNED;
+  HeadArgs a = {};
+  a.x[0] = x;
+  a.ld[0] = ld_token;
+  a.H[0] = H;
+  a.norm[0] = norm;
+  a.T = T;
+  a.pos = positions;
+  a.table = table;
+  a.max_pos = max_pos;
+  a.rot = rot_dim;
+  a.interleaved = (flags & OFFQ_INTERLEAVED) != 0;
+  a.eps = eps;
+  a.rotate[0] = (flags & OFFQ_ROTATE) != 0;
+  a.out = out;
+  a.ld_out = ld_out;
+  return run_heads(a, dtype, out_dtype, head_dim, stream);
+}
+
+extern "C" int offq_kv4_paged_write(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq,
+                                    int32_t H, int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                                    const int32_t* positions, const float* table, int64_t max_pos, int32_t rot_dim,
+                                    const float* q_norm, const float* k_norm, float eps, int32_t flags,
+                                    const int64_t* slots, uint8_t* k_codes, float* k_params, uint8_t* v_codes,
+                                    float* v_params, int64_t pages, int32_t page_size, void* q_out, int out_dtype,
+                                    int64_t ld_q_out, void* stream) {
+  if (!dtype_ok(dtype) || !(eps >= 0.f) ||
+      (flags & ~(OFFQ_ROTATE | OFFQ_OFFSET | OFFQ_INTERLEAVED | OFFQ_ROTATE_V)) != 0 || Hq < 0)
+    return OFFQ_ERR_INVALID_ARG;
+  if (const int rc = check_heads(T, H, head_dim); rc != OFFQ_OK) return rc;
+  if (Hq > 65535) return OFFQ_ERR_UNSUPPORTED;
+  const int64_t width = static_cast<int64_t>(H) * head_dim, q_width = static_cast<int64_t>(Hq) * head_dim;
+  if (ld_k < width || ld_v < width || pages < 1 || page_size < 1) return OFFQ_ERR_INVALID_ARG;
+  if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || pages > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
+  if (Hq > 0 && (ld_q < q_width || ld_q_out < q_width || !dtype_ok(out_dtype))) return OFFQ_ERR_INVALID_ARG;
+  if (T == 0) return OFFQ_OK;
+  if (k == nullptr || v == nullptr || slots == nullptr || k_codes == nullptr || k_params == nullptr ||
+      v_codes == nullptr || v_params == nullptr || (Hq > 0 && (q == nullptr || q_out == nullptr)))
+    return OFFQ_ERR_INVALID_ARG;
+  if (const int rc = check_rotary(positions, table, max_pos, rot_dim, head_dim); rc != OFFQ_OK) return rc;
+  const int b = elem_bytes(dtype);
+  if (!row_ok(k, ld_k, b) || !row_ok(v, ld_v, b) || !aligned(table, 16) || !aligned(q_norm, 16) ||
+      !aligned(k_norm, 16) || !aligned(positions, 4) || !aligned(slots, 8) || !aligned(k_codes, 16) ||
+      !aligned(v_codes, 16) || !aligned(k_params, 16) || !aligned(v_params, 16) ||
+      (Hq > 0 && (!row_ok(q, ld_q, b) || !row_ok(q_out, ld_q_out, elem_bytes(out_dtype)))))
+    return OFFQ_ERR_MISALIGNED;
+  HeadArgs a = {};
+  a.x[0] = q;
+  a.x[1] = k;
+  a.x[2] = v;
+  a.ld[0] = ld_q;
+  a.ld[1] = ld_k;
+  a.ld[2] = ld_v;
+  a.H[0] = Hq;
+  a.H[1] = a.H[2] = H;
+  a.norm[0] = q_norm;
+  a.norm[1] = k_norm;
+  a.T = T;
+  a.pos = positions;
+  a.table = table;
+  a.max_pos = max_pos;
+  a.rot = rot_dim;
+  a.interleaved = (flags & OFFQ_INTERLEAVED) != 0;
+  a.eps = eps;
+  a.rotate[0] = a.rotate[1] = (flags & OFFQ_ROTATE) != 0;
+  a.rotate[2] = (flags & OFFQ_ROTATE_V) != 0;
+  a.offset = (flags & OFFQ_OFFSET) != 0;
+  a.out = q_out;
+  a.ld_out = ld_q_out;
+  a.slots = slots;
+  a.codes[0] = k_codes;
+  a.codes[1] = v_codes;
+  a.params[0] = k_params;
+  a.params[1] = v_params;
+  a.slots_in_cache = pages * page_size;
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  return run_heads(a, dtype, Hq > 0 ? out_dtype : OFFQ_F32, head_dim, stream);
+}
+
+extern "C" int offq_kv4_paged_read(const uint8_t* k_codes, const float* k_params, const uint8_t* v_codes,
+                                   const float* v_params, int64_t pages, int32_t page_size, int32_t H,
+                                   int32_t head_dim, const int64_t* slots, int64_t T, int32_t flags, void* k_out,
+                                   void* v_out, int out_dtype, int64_t ld_k, int64_t ld_v, void* stream) {
+  if (!dtype_ok(out_dtype) || (flags & ~(OFFQ_ROTATE | OFFQ_ROTATE_V)) != 0) return OFFQ_ERR_INVALID_ARG;
+  if (const int rc = check_heads(T, H, head_dim); rc != OFFQ_OK) return rc;
+  const int64_t width = static_cast<int64_t>(H) * head_dim;
+  if (pages < 1 || page_size < 1 || (k_out != nullptr && ld_k < width) || (v_out != nullptr && ld_v < width))
+    return OFFQ_ERR_INVALID_ARG;
+  if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || pages > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
+  if (T == 0 || (k_out == nullptr && v_out == nullptr)) return OFFQ_OK;
+  if (slots == nullptr || (k_out != nullptr && (k_codes == nullptr || k_params == nullptr)) ||
+      (v_out != nullptr && (v_codes == nullptr || v_params == nullptr)))
+    return OFFQ_ERR_INVALID_ARG;
+  const int b = elem_bytes(out_dtype);
+  if (!aligned(slots, 8) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_params, 16) ||
+      !aligned(v_params, 16) || (k_out != nullptr && !row_ok(k_out, ld_k, b)) ||
+      (v_out != nullptr && !row_ok(v_out, ld_v, b)))
+    return OFFQ_ERR_MISALIGNED;
+  ReadArgs a = {};
+  a.codes[0] = k_codes;
+  a.codes[1] = v_codes;
+  a.params[0] = k_params;
+  a.params[1] = v_params;
+  a.out[0] = k_out;
+  a.out[1] = v_out;
+  a.ld[0] = ld_k;
+  a.ld[1] = ld_v;
+  a.rotate[0] = (flags & OFFQ_ROTATE) != 0;
+  a.rotate[1] = (flags & OFFQ_ROTATE_V) != 0;
+  a.T = T;
+  a.slots_in_cache = pages * page_size;
+  a.H = H;
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  a.slots = slots;
+  a.status = device_status_ptr();
+  const int sms = device_sms();
+  if (a.status == nullptr || sms == 0) return OFFQ_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (head_dim == 128) {
+    switch (out_dtype) {
+      case OFFQ_F32: return launch_read<128, float>(a, sms, s);
+      case OFFQ_BF16: return launch_read<128, __nv_bfloat16>(a, sms, s);
+      default: return launch_read<128, __half>(a, sms, s);
+    }
+  }
+  switch (out_dtype) {
+    case OFFQ_F32: return launch_read<64, float>(a, sms, s);
+    case OFFQ_BF16: return launch_read<64, __nv_bfloat16>(a, sms, s);
+    default: return launch_read<64, __half>(a, sms, s);
+  }
+}

@@ -13,9 +13,10 @@ tensors holding the tiled operand layout of include/offq.h.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import re
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -29,7 +30,7 @@ OFFQ_ERR_CUDA = -4
 OFFQ_ERR_TIMEOUT = -5
 
 OFFQ_F32, OFFQ_BF16, OFFQ_F16 = 0, 1, 2
-OFFQ_ROTATE, OFFQ_OFFSET = 1, 2
+OFFQ_ROTATE, OFFQ_OFFSET, OFFQ_INTERLEAVED, OFFQ_ROTATE_V = 1, 2, 4, 8
 OFFQ_FORM_FEW, OFFQ_FORM_MID, OFFQ_FORM_PAIR = 1, 2, 3
 
 _DTYPE_CODE = {torch.float32: OFFQ_F32, torch.bfloat16: OFFQ_BF16, torch.float16: OFFQ_F16}
@@ -39,6 +40,7 @@ _c_vp = ctypes.c_void_p
 _c_i64 = ctypes.c_int64
 _c_i32 = ctypes.c_int32
 _c_int = ctypes.c_int
+_c_f32 = ctypes.c_float
 
 _SIGNATURES = {
     "offq_quantize_act": (_c_int, [_c_vp, _c_int, _c_i64, _c_i64, _c_i64, _c_i32, _c_i32, _c_vp, _c_vp, _c_vp, _c_vp]),
@@ -85,6 +87,19 @@ _SIGNATURES = {
     "offq_column_absmax": (_c_int, [_c_vp, _c_i64, _c_i64, _c_vp, _c_vp]),
     "offq_sorted_grouping": (_c_int, [_c_vp, _c_i64, _c_i32, _c_vp]),
     "offq_fuse_rotation": (_c_int, [_c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i32, _c_vp, _c_vp]),
+    "offq_rope_heads": (_c_int, [_c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i64, _c_vp, _c_vp, _c_i64, _c_i32, _c_vp,
+                                 _c_f32, _c_i32, _c_vp, _c_int, _c_i64, _c_vp]),
+    "offq_kv4_paged_write": (_c_int, [_c_vp, _c_vp, _c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64, _c_i64,
+                                      _c_i64, _c_vp, _c_vp, _c_i64, _c_i32, _c_vp, _c_vp, _c_f32, _c_i32, _c_vp,
+                                      _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_vp, _c_int, _c_i64, _c_vp]),
+    "offq_kv4_paged_read": (_c_int, [_c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_i32, _c_i32, _c_vp, _c_i64,
+                                     _c_i32, _c_vp, _c_vp, _c_int, _c_i64, _c_i64, _c_vp]),
+    "offq_paged_attention": (_c_int, [_c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64, _c_vp, _c_vp, _c_vp,
+                                      _c_vp, _c_i64, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i32, _c_i32, _c_f32,
+                                      _c_vp, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "offq_paged_attention_workspace": (_c_i64, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "offq_prompt_attention": (_c_int, [_c_vp, _c_vp, _c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64, _c_i64,
+                                       _c_i64, _c_vp, _c_i32, _c_f32, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp]),
 }
 
 _lib = None
@@ -618,3 +633,253 @@ def prepare_weight_mx(w: torch.Tensor, g: int, rotate: bool = True):
     offsum = torch.empty((K // g, N), dtype=torch.float32, device=dev)
     offq_prepare_weight_mx(w.contiguous(), N, K, g, 1 if rotate else 0, codes, shifts, scale, offsum)
     return codes, shifts, scale, offsum
+
+
+# ---------------------------------------------------------------------------
+# Between the projections and attention: norm, rotary positions and H3 of heads,
+# the paged 4-bit cache, attention
+# ---------------------------------------------------------------------------
+
+class KV4Cache(NamedTuple):
+    """The paged 4-bit cache of one layer: codes [pages, H, page_size, hd / 2] uint8 and
+    (scale, offset) pairs [pages, H, page_size, 2] float32 of keys and of values."""
+    k_codes: torch.Tensor
+    k_params: torch.Tensor
+    v_codes: torch.Tensor
+    v_params: torch.Tensor
+
+
+def kv4_cache(pages: int, heads: int, head_dim: int = 128, page_size: int = 64, device=None) -> KV4Cache:
+    """Uninitialised pages (a slot means something once a token was written to it)."""
+    def codes():
+        return torch.empty((pages, heads, page_size, head_dim // 2), dtype=torch.uint8, device=device or "cuda")
+
+    def params():
+        return torch.empty((pages, heads, page_size, 2), dtype=torch.float32, device=device or "cuda")
+    return KV4Cache(codes(), params(), codes(), params())
+
+
+def rope_table(max_pos: int, rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+               original_len: int = 4096, beta_fast: float = 32.0, beta_slow: float = 1.0, device=None) -> torch.Tensor:
+    """Rotary table [max_pos, rot_dim] float32: cosines of rot_dim / 2 angles, then their sines, computed in float64.
+
+    Frequencies are f_m = base^(-2m / rot_dim). Contexts ``factor`` times longer than the trained ``original_len``:
+      linear  positions divided by factor;
+      ntk     base * factor^(rot_dim / (rot_dim - 2)): the slowest frequency is divided by factor, the fastest kept;
+      yarn    f_m / factor where the trained length holds fewer than beta_slow turns, f_m where it holds more than
+              beta_fast, a linear ramp between, and cosines and sines times 0.1 ln(factor) + 1.
+    """
+    if rot_dim < 2 or rot_dim % 2 or max_pos < 1:
+        raise ValueError("rope_table needs max_pos >= 1 and an even rot_dim >= 2")
+    if scaling not in ("none", "linear", "ntk", "yarn") or factor < 1.0:
+        raise ValueError(f"unknown scaling {scaling!r} or factor below 1")
+    m = torch.arange(rot_dim // 2, dtype=torch.float64)
+    if scaling == "ntk":
+        if rot_dim < 4:
+            raise ValueError("ntk scaling needs rot_dim >= 4")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    freq = base ** (-2.0 * m / rot_dim)
+    amp = 1.0
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "yarn":
+        def at(turns):  # the m whose frequency makes that many turns over the trained length
+            return rot_dim * math.log(original_len / (2 * math.pi * turns)) / (2 * math.log(base))
+        lo, hi = max(0.0, math.floor(at(beta_fast))), min(rot_dim - 1.0, math.ceil(at(beta_slow)))
+        ramp = ((m - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+        freq = freq / factor * ramp + freq * (1.0 - ramp)
+        amp = 0.1 * math.log(factor) + 1.0
+    a = torch.arange(max_pos, dtype=torch.float64)[:, None] * freq
+    return torch.cat([a.cos() * amp, a.sin() * amp], 1).to(torch.float32).to(device or "cuda")
+
+
+def offq_rope_heads(x: torch.Tensor, T: int, H: int, head_dim: int, ld_token: int, positions: Optional[torch.Tensor],
+                    table: Optional[torch.Tensor], max_pos: int, rot_dim: int, norm: Optional[torch.Tensor], eps: float,
+                    flags: int, out: torch.Tensor, ld_out: int, stream=None) -> None:
+    _check("offq_rope_heads", load_library().offq_rope_heads(
+        _ptr(x), _dtype_code(x), T, H, head_dim, ld_token, _ptr(positions), _ptr(table), max_pos, rot_dim, _ptr(norm),
+        eps, flags, _ptr(out), _dtype_code(out), ld_out, _stream(stream)))
+
+
+def offq_kv4_paged_write(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, T: int, Hq: int, H: int,
+                         head_dim: int, ld_q: int, ld_k: int, ld_v: int, positions: Optional[torch.Tensor],
+                         table: Optional[torch.Tensor], max_pos: int, rot_dim: int, q_norm: Optional[torch.Tensor],
+                         k_norm: Optional[torch.Tensor], eps: float, flags: int, slots: torch.Tensor,
+                         cache: KV4Cache, pages: int, page_size: int, q_out: Optional[torch.Tensor], ld_q_out: int,
+                         stream=None) -> None:
+    _check("offq_kv4_paged_write", load_library().offq_kv4_paged_write(
+        _ptr(q), _ptr(k), _ptr(v), _dtype_code(k), T, Hq, H, head_dim, ld_q, ld_k, ld_v, _ptr(positions), _ptr(table),
+        max_pos, rot_dim, _ptr(q_norm), _ptr(k_norm), eps, flags, _ptr(slots), _ptr(cache.k_codes),
+        _ptr(cache.k_params), _ptr(cache.v_codes), _ptr(cache.v_params), pages, page_size, _ptr(q_out),
+        _dtype_code(q_out) if q_out is not None else OFFQ_F32, ld_q_out, _stream(stream)))
+
+
+def offq_kv4_paged_read(cache: KV4Cache, pages: int, page_size: int, H: int, head_dim: int, slots: torch.Tensor, T: int,
+                        flags: int, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], out_dtype: int,
+                        ld_k: int, ld_v: int, stream=None) -> None:
+    _check("offq_kv4_paged_read", load_library().offq_kv4_paged_read(
+        _ptr(cache.k_codes), _ptr(cache.k_params), _ptr(cache.v_codes), _ptr(cache.v_params), pages, page_size, H,
+        head_dim, _ptr(slots), T, flags, _ptr(k_out), _ptr(v_out), out_dtype, ld_k, ld_v, _stream(stream)))
+
+
+def offq_paged_attention(q: torch.Tensor, Tq: int, Hq: int, H: int, head_dim: int, ld_q: int, cache: KV4Cache,
+                         pages: int, page_size: int, block_table: torch.Tensor, ld_table: int, lens: torch.Tensor,
+                         cu_q: torch.Tensor, B: int, max_q: int, scale: float, out: torch.Tensor, ld_out: int,
+                         lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor], workspace_bytes: int,
+                         stream=None) -> None:
+    _check("offq_paged_attention", load_library().offq_paged_attention(
+        _ptr(q), _dtype_code(q), Tq, Hq, H, head_dim, ld_q, _ptr(cache.k_codes), _ptr(cache.k_params),
+        _ptr(cache.v_codes), _ptr(cache.v_params), pages, page_size, _ptr(block_table), ld_table, _ptr(lens),
+        _ptr(cu_q), B, max_q, scale, _ptr(out), ld_out, _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def paged_attention_workspace(Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int) -> int:
+    return load_library().offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q)
+
+
+def offq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: int, Hq: int, H: int, head_dim: int,
+                          ld_q: int, ld_k: int, ld_v: int, cu: torch.Tensor, B: int, scale: float, causal: bool,
+                          out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor], stream=None) -> None:
+    _check("offq_prompt_attention", load_library().offq_prompt_attention(
+        _ptr(q), _ptr(k), _ptr(v), _dtype_code(q), T, Hq, H, head_dim, ld_q, ld_k, ld_v, _ptr(cu), B, scale,
+        1 if causal else 0, _ptr(out), ld_out, _ptr(lse), _stream(stream)))
+
+
+def _heads(x: torch.Tensor) -> Tuple[int, int, int, int]:
+    """(T, H, hd, ld_token) of x [T, H, hd] with contiguous heads."""
+    T, H, hd = x.shape
+    if x.stride(2) != 1 or (H > 1 and x.stride(1) != hd):
+        raise ValueError("heads of a token must be contiguous")
+    return T, H, hd, x.stride(0) if T > 1 else max(x.stride(0), H * hd)
+
+
+def _like(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape) -> None:
+    """t is a contiguous tensor of that type and shape, or None."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+
+
+def _rotary(positions, table, T):
+    """(max_pos, rot_dim) of a rotary table, (0, 0) without one."""
+    if table is None:
+        return 0, 0
+    _like("positions", positions, torch.int32, (T,))
+    if positions is None or table.dim() != 2:
+        raise ValueError("a rotary table [max_pos, rot_dim] goes with positions [T]")
+    _like("table", table, torch.float32, table.shape)
+    return table.shape
+
+
+def _cache_shape(cache: KV4Cache, H: Optional[int], hd: Optional[int]):
+    pages, heads, page_size, half = cache.k_codes.shape
+    if (H is not None and heads != H) or (hd is not None and 2 * half != hd):
+        raise ValueError(f"the cache holds {heads} heads of {2 * half}")
+    for t in (cache.k_codes, cache.v_codes):
+        _like("cache codes", t, torch.uint8, (pages, heads, page_size, half))
+    for t in (cache.k_params, cache.v_params):
+        _like("cache params", t, torch.float32, (pages, heads, page_size, 2))
+    return pages, heads, page_size, 2 * half
+
+
+def rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+               norm: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, rotate: bool = False,
+               out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x [T, H, hd]: RMS norm (norm [H, hd]), rotary positions (rope_table) and H3, each if asked for, in one pass."""
+    T, H, hd, ld = _heads(x)
+    max_pos, rot = _rotary(positions, table, T)
+    _like("norm", norm, torch.float32, (H, hd))
+    if out is None:
+        out = torch.empty((T, H, hd), dtype=out_dtype or x.dtype, device=x.device)
+    elif out.shape != x.shape:
+        raise ValueError("out has x's shape")
+    flags = (OFFQ_ROTATE if rotate else 0) | (OFFQ_INTERLEAVED if interleaved else 0)
+    offq_rope_heads(x, T, H, hd, ld, positions, table, max_pos, rot, norm, eps, flags, out, _heads(out)[3], stream)
+    return out
+
+
+def kv4_paged_write(cache: KV4Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
+                    positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+                    q: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
+                    k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                    rotate: bool = True, rotate_v: bool = False, offset: bool = True,
+                    out_dtype: Optional[torch.dtype] = None, stream=None) -> Optional[torch.Tensor]:
+    """Keys and values [T, H, hd] into the slots [T] (int64) of the cache, the keys after k_norm, rotary positions and
+    H3; returns the queries q [T, Hq, hd] after the same (None without q)."""
+    T, H, hd, ld_k = _heads(k)
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("keys and values have one shape and type")
+    pages, _, page_size, _ = _cache_shape(cache, H, hd)
+    max_pos, rot = _rotary(positions, table, T)
+    _like("slots", slots, torch.int64, (T,))
+    _like("k_norm", k_norm, torch.float32, (H, hd))
+    Hq, ld_q, q_out = 0, 0, None
+    if q is not None:
+        Tq, Hq, hq, ld_q = _heads(q)
+        if (Tq, hq) != (T, hd) or q.dtype != k.dtype:
+            raise ValueError("queries have the keys' tokens, head size and type")
+        _like("q_norm", q_norm, torch.float32, (Hq, hd))
+        q_out = torch.empty((T, Hq, hd), dtype=out_dtype or q.dtype, device=q.device)
+    flags = ((OFFQ_ROTATE if rotate else 0) | (OFFQ_OFFSET if offset else 0) | (OFFQ_INTERLEAVED if interleaved else 0)
+             | (OFFQ_ROTATE_V if rotate_v else 0))
+    offq_kv4_paged_write(q, k, v, T, Hq, H, hd, ld_q, ld_k, _heads(v)[3], positions, table, max_pos, rot, q_norm, k_norm,
+                         eps, flags, slots, cache, pages, page_size, q_out, Hq * hd, stream)
+    return q_out
+
+
+def kv4_paged_read(cache: KV4Cache, slots: torch.Tensor, rotate: bool = True, rotate_v: bool = False,
+                   out_dtype: torch.dtype = torch.bfloat16, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys (H3 undone with rotate) and values [T, H, hd] of the tokens in slots [T] (int64)."""
+    pages, H, page_size, hd = _cache_shape(cache, None, None)
+    T = slots.shape[0]
+    _like("slots", slots, torch.int64, (T,))
+    kv = torch.empty((2, T, H, hd), dtype=out_dtype, device=slots.device)
+    k, v = kv[0], kv[1]
+    flags = (OFFQ_ROTATE if rotate else 0) | (OFFQ_ROTATE_V if rotate_v else 0)
+    offq_kv4_paged_read(cache, pages, page_size, H, hd, slots, T, flags, k, v, _dtype_code(k), H * hd, H * hd, stream)
+    return k, v
+
+
+def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, lens: torch.Tensor,
+                    cu_q: torch.Tensor, max_q: int, scale: Optional[float] = None, lse: bool = False,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """New tokens' queries q [Tq, Hq, hd] over the pages block_table [B, width] (int32) of lens [B] cached tokens;
+    sequence b's queries are rows cu_q[b] .. cu_q[b + 1] - 1 and its last tokens. Returns out, or (out, lse [Tq, Hq])."""
+    Tq, Hq, hd, ld_q = _heads(q)
+    pages, H, page_size, _ = _cache_shape(cache, None, hd)
+    B = lens.shape[0]
+    _like("lens", lens, torch.int32, (B,))
+    _like("cu_q", cu_q, torch.int32, (B + 1,))
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or             (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table must be int32 [B, width] with contiguous rows")
+    if out is None:
+        out = torch.empty((Tq, Hq, hd), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out has q's shape and type")
+    need = paged_attention_workspace(Tq, Hq, H, hd, B, max_q)
+    if workspace is None and need > 0:
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+    stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
+    ld_table = block_table.stride(0) if B > 1 else block_table.shape[1]
+    offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table, ld_table, lens, cu_q, B, max_q,
+                         scale if scale is not None else hd ** -0.5, out, _heads(out)[3], stats, workspace,
+                         workspace.numel() * workspace.element_size() if workspace is not None else 0, stream)
+    return (out, stats) if lse else out
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, scale: Optional[float] = None,
+                     causal: bool = True, lse: bool = False, out: Optional[torch.Tensor] = None, stream=None):
+    """Attention inside packed sequences: rows cu[b] .. cu[b + 1] - 1 of q [T, Hq, hd] and k, v [T, H, hd] are sequence
+    b. Returns out, or (out, lse [T, Hq])."""
+    T, Hq, hd, ld_q = _heads(q)
+    Tk, H, hk, ld_k = _heads(k)
+    if (Tk, hk) != (T, hd) or v.shape != k.shape or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("queries, keys and values have the same tokens, head size and type")
+    _like("cu", cu, torch.int32, (cu.shape[0],))
+    if out is None:
+        out = torch.empty((T, Hq, hd), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out has q's shape and type")
+    stats = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if lse else None
+    offq_prompt_attention(q, k, v, T, Hq, H, hd, ld_q, ld_k, _heads(v)[3], cu, cu.shape[0] - 1,
+                          scale if scale is not None else hd ** -0.5, causal, out, _heads(out)[3], stats, stream)
+    return (out, stats) if lse else out
