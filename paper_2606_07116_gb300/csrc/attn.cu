@@ -4,48 +4,15 @@
 // out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j - m_i),  lse_i = m_i + log sum_j p_ij
 // over the keys j that query i sees. A warp takes one query of one head; a lane scores one key of
 // each 32, and the running maximum, sum and output are rescaled once per 32 keys, in fp32.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
-#include <type_traits>
 
-#include "offq.h"
-#include "offq_device.cuh"
-#include "offq_host.h"
+#include "attn.cuh"
 
 namespace {
 
 using namespace offq;
 
 constexpr int kRowWarps = 4;
-constexpr uint32_t kAll = 0xFFFFFFFFu;
-
-struct AttnArgs {
-  const void* q;
-  int64_t ld_q;
-  int64_t Tq;
-  int Hq, H;
-  const void* k;  // prompts
-  const void* v;
-  int64_t ld_k, ld_v;
-  const uint8_t* codes[2];  // paged
-  const float* params[2];
-  int64_t pages;
-  int page_shift;
-  const int32_t* table;
-  int64_t ld_table;
-  const int32_t* lens;
-  const int32_t* cu;
-  int B;
-  int max_q;
-  int causal;
-  float scale;
-  void* out;
-  int64_t ld_out;
-  float* lse;
-  int* status;
-};
 
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
@@ -57,12 +24,13 @@ __device__ __forceinline__ float element(const AttnArgs& a, int which, int b, in
     const int64_t page = a.table[b * a.ld_table + (j >> a.page_shift)];
     if (page < 0 || page >= a.pages) {
       *a.status = OFFQ_ERR_INVALID_ARG;
-      return 0.f;
+      return which ? 0.f : -INFINITY;
     }
     const int64_t row = ((page * a.H + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-    const uint32_t c = a.codes[which][row * (D / 2) + d / 2];
+    const uint32_t c = (which ? a.v_codes : a.k_codes)[row * (D / 2) + d / 2];
+    const float* par = (which ? a.v_params : a.k_params) + 2 * row;
     const int u = static_cast<int>((d & 1) ? c >> 4 : c & 15u) - 8;
-    return static_cast<float>(u) * a.params[which][2 * row] + a.params[which][2 * row + 1];
+    return static_cast<float>(u) * par[0] + par[1];
   } else {
     const T* x = static_cast<const T*>(which ? a.v : a.k);
     return to_f(x[(start + j) * (which ? a.ld_v : a.ld_k) + static_cast<int64_t>(h) * D + d]);
@@ -77,19 +45,18 @@ __global__ void __launch_bounds__(kRowWarps * 32) attention_rows_kernel(const At
   griddep_launch_dependents();
   const int64_t r = static_cast<int64_t>(blockIdx.x) * kRowWarps + warp;
   const int64_t t = r / a.Hq;
-  const int hq = static_cast<int>(r % a.Hq), h = hq / (a.Hq / a.H);
+  const int hq = static_cast<int>(r % a.Hq), h = hq / a.G;
   if (t >= a.Tq) return;
   int b = 0;
   while (b < a.B && t >= a.cu[b + 1]) ++b;
   if (b == a.B || t < a.cu[b]) return;
   const int64_t start = a.cu[b], end = min(static_cast<int64_t>(a.cu[b + 1]), a.Tq);
-  const int i = static_cast<int>(t - start), n = static_cast<int>(end - start);
-  int len = n;
+  int i = static_cast<int>(t - start), n = static_cast<int>(end - start), len = n;
   if constexpr (kPaged) {
-    const int64_t most = a.ld_table << a.page_shift;
-    len = static_cast<int>(min(static_cast<int64_t>(a.lens[b]), most));
-    if (a.cu[b + 1] > a.Tq || n > a.max_q || a.lens[b] > most) *a.status = OFFQ_ERR_INVALID_ARG;
-    if (n > a.max_q) return;
+    const PagedSeq s = paged_seq(a, b);
+    if (s.bad) *a.status = OFFQ_ERR_INVALID_ARG;
+    if (s.n * a.G <= a.few_rows) return;
+    len = s.len;
   } else if (a.cu[b + 1] > a.Tq) {
     *a.status = OFFQ_ERR_INVALID_ARG;
   }
@@ -102,28 +69,35 @@ __global__ void __launch_bounds__(kRowWarps * 32) attention_rows_kernel(const At
     float s = -INFINITY;
     if (j0 + lane < seen) {
       s = 0.f;
-      for (int d = 0; d < D; ++d) s = fmaf(qs[warp][d], element<D, T, kPaged>(a, 0, b, start, j0 + lane, h, d), s);
+      for (int d = 0; d < D; ++d) {
+        const float k = element<D, T, kPaged>(a, 0, b, start, j0 + lane, h, d);
+        if (kPaged && k == -INFINITY) {
+          s = k;
+          break;
+        }
+        s = fmaf(qs[warp][d], k, s);
+      }
       s *= a.scale;
     }
     float top = s;
 #pragma unroll
-    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, k));
+    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, k));
     const float next = fmaxf(m, top), keep = next == -INFINITY ? 1.f : __expf(m - next);
-    const float p = j0 + lane < seen && next != -INFINITY ? __expf(s - next) : 0.f;
+    const float p = s != -INFINITY && next != -INFINITY ? __expf(s - next) : 0.f;
     m = next;
     sum = sum * keep + p;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) acc[e] *= keep;
     const int most = min(32, seen - j0);
     for (int k = 0; k < most; ++k) {
-      const float pk = __shfl_sync(kAll, p, k);
+      const float pk = __shfl_sync(kAllLanes, p, k);
 #pragma unroll
       for (int e = 0; e < D / 32; ++e)
         acc[e] = fmaf(pk, element<D, T, kPaged>(a, 1, b, start, j0 + k, h, lane + 32 * e), acc[e]);
     }
   }
 #pragma unroll
-  for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(kAll, sum, k);
+  for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(kAllLanes, sum, k);
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
@@ -164,7 +138,7 @@ extern "C" int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_
   if (check_attention(nullptr, OFFQ_BF16, Tq, Hq, H, head_dim, int64_t{1} << 40, B, 1.f, int64_t{1} << 40) != OFFQ_OK ||
       max_q < 0)
     return -1;
-  return 0;
+  return Tq == 0 || B == 0 || max_q == 0 ? 0 : paged_few_workspace(head_dim);
 }
 
 extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
@@ -191,10 +165,11 @@ extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_
   a.Tq = Tq;
   a.Hq = Hq;
   a.H = H;
-  a.codes[0] = k_codes;
-  a.codes[1] = v_codes;
-  a.params[0] = k_params;
-  a.params[1] = v_params;
+  a.G = Hq / H;
+  a.k_codes = k_codes;
+  a.v_codes = v_codes;
+  a.k_params = k_params;
+  a.v_params = v_params;
   a.pages = pages;
   a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
   a.table = block_table;
@@ -209,8 +184,14 @@ extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_
   a.ld_out = ld_out;
   a.lse = lse;
   a.status = device_status_ptr();
-  if (a.status == nullptr) return OFFQ_ERR_CUDA;
-  return launch_rows<true>(a, dtype, head_dim, static_cast<cudaStream_t>(stream));
+  const int64_t need = paged_few_workspace(head_dim);
+  if (a.status == nullptr || need < 0) return OFFQ_ERR_CUDA;
+  if (workspace == nullptr || workspace_bytes < need) return OFFQ_ERR_INVALID_ARG;
+  a.workspace = workspace;
+  a.few_rows = kFewRows;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (const int rc = paged_few(a, dtype, head_dim, s); rc != OFFQ_OK) return rc;
+  return static_cast<int64_t>(max_q) * a.G > kFewRows ? launch_rows<true>(a, dtype, head_dim, s) : OFFQ_OK;
 }
 
 extern "C" int offq_prompt_attention(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq,
@@ -231,6 +212,7 @@ extern "C" int offq_prompt_attention(const void* q, const void* k, const void* v
   a.Tq = T;
   a.Hq = Hq;
   a.H = H;
+  a.G = Hq / H;
   a.k = k;
   a.v = v;
   a.ld_k = ld_k;

@@ -1,0 +1,85 @@
+// What the attention kernels share: their arguments, the checks of what stands in device buffers, and
+// the pieces of a softmax.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "offq.h"
+#include "offq_device.cuh"
+#include "offq_host.h"
+
+namespace offq {
+
+constexpr uint32_t kAllLanes = 0xFFFFFFFFu;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// A running maximum is left where it is until a score passes it by this much (in powers of two):
+// weights then reach 2^8 at most, far from any overflow, and a rescaling of the sums is rare.
+constexpr float kLazy = 8.0f;
+
+struct AttnArgs {
+  const void* q;
+  int64_t ld_q;
+  int64_t Tq;
+  int Hq, H, G;   // query heads, key heads, query heads per key head
+  const void* k;  // prompts
+  const void* v;
+  int64_t ld_k, ld_v;
+  const uint8_t* k_codes;  // paged
+  const uint8_t* v_codes;
+  const float* k_params;
+  const float* v_params;
+  int64_t pages;
+  int page_shift;
+  const int32_t* table;
+  int64_t ld_table;
+  const int32_t* lens;
+  const int32_t* cu;
+  int B;
+  int max_q;
+  int few_rows;   // sequences with at most this many rows n * G take the few-row form
+  int causal;
+  float scale;
+  void* out;
+  int64_t ld_out;
+  float* lse;
+  void* workspace;
+  int* status;
+};
+
+// A sequence of the paged call: its first query row, queries and cached tokens. One whose entries are out of
+// range (negative or too long counts) has no queries; `bad` says so.
+struct PagedSeq {
+  int first, n, len;
+  bool bad;
+};
+
+__device__ __forceinline__ PagedSeq paged_seq(const AttnArgs& a, int b) {
+  const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1), l = __ldg(a.lens + b);
+  const int64_t most = min(a.ld_table << a.page_shift, static_cast<int64_t>(0x7FFFFFC0));
+  PagedSeq s;
+  s.first = c0;
+  s.n = c1 - c0;
+  s.len = static_cast<int>(min(static_cast<int64_t>(max(l, 0)), most));
+  s.bad = l < 0 || l > most;
+  if (c0 < 0 || c1 < c0 || c1 > a.Tq || s.n > a.max_q) {
+    s.bad = true;
+    s.n = 0;
+  }
+  return s;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The few-row form of offq_paged_attention (csrc/attn_few.cu): rows n * G of a sequence that it takes, its
+// workspace, and its launch with arguments already checked.
+constexpr int kFewRows = 16;
+int64_t paged_few_workspace(int head_dim);
+int paged_few(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
+
+}  // namespace offq

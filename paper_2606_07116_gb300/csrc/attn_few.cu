@@ -1,0 +1,723 @@
+// Attention of few query rows over the paged 4-bit cache (offq_paged_attention with up to 16 rows
+// n * Hq / H per sequence and key head: single tokens, drafted tokens).
+//
+// Every cached byte is read once for all rows of its key head, so the cache bounds it: D + 16 bytes per
+// token and head (144 at D = 128) against 4 D multiply-adds per row.
+//
+// Work is a list of 32-token stages, sequence by sequence, head by head. The CTAs (one per SM) take equal
+// contiguous shares of it, the warps of a CTA equal shares of those: any mix of lengths loads the chip
+// evenly and in one wave. A warp that holds a whole (sequence, head) writes its output; parts are joined
+// in shared memory at the CTA's end, and what crosses CTAs in a second small kernel (at most a first and a
+// last part per CTA: the workspace does not grow with the batch).
+//
+// A warp stages its tokens itself: one lane issues bulk copies (a head's tokens of a page are contiguous) into
+// a ring of its own, and all lanes read fragments for warp-level MMAs of 16 tokens:
+//   S^T [tokens x rows]  = codes K [16 x 16 channels] * Q^T [16 channels x 8 rows]
+//   O^T [channels x rows] += codes V^T [16 channels x 16 tokens] * P^T [16 tokens x 8 rows]
+// with the rows on the MMA's 8-wide side, as there are few. Channels may be contracted in any order and tokens
+// too, so fragments are what a lane finds in its 16-byte reads: a code needs half a shift and half a logical
+// operation. The nibble u = q + 8 becomes the 16-bit float 16 + u (its bits placed below the exponent of
+// 16.0): exact, and the 24 on top of q leaves as -24 * sum(query) and -24 * sum(weights).
+//   z_j = s_j (acc_j - 24 Q) + o_j Q,  Q = sum of the query;   out = (O - 24 sum P' + sum p o_v) / sum p,
+// P' = p s_v rounded to bf16 (in two bf16 parts, 16 bits, for half-precision outputs: s_v has no range that a
+// half could hold).
+#include <algorithm>
+#include <type_traits>
+
+#include "attn.cuh"
+
+namespace {
+
+using namespace offq;
+
+constexpr int kTile = 32;   // tokens per stage
+constexpr float kBias = 24.0f;
+
+template <int D, int NT>
+struct FewLayout {
+  static constexpr int kWarps = 8;
+  static constexpr int kStages = 4;
+  static constexpr int kCodeBytes = kTile * D / 2;
+  static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kTile * 8;
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kRing = kStages * kStageBytes;            // a warp's ring; its last part goes there too
+  static constexpr int kPartFloats = kRows * (D + 2);            // O, then m and l
+  static constexpr int kPartBytes = kPartFloats * 4;
+  static constexpr int kPartOff = kWarps * kRing;                // the warps' first parts
+  static constexpr int kCtrlOff = kPartOff + kWarps * kPartBytes;
+  static constexpr int kBytes = kCtrlOff + 1024;
+  static_assert(kPartBytes <= kRing, "a part fits into its warp's ring");
+  static_assert(kBytes <= 232448 && kWarps * kStages * 8 + 512 <= 1024, "shared memory");
+};
+
+// Control block behind the parts.
+template <int D, int NT>
+struct FewCtrl {
+  uint64_t full[FewLayout<D, NT>::kWarps * FewLayout<D, NT>::kStages];
+  long long scan[FewLayout<D, NT>::kWarps];
+  long long start[FewLayout<D, NT>::kWarps];  // unit offset inside sequence seq
+  int seq[FewLayout<D, NT>::kWarps];
+  int4 part[2 * FewLayout<D, NT>::kWarps];    // (sequence or -1, head, first stage, last stage) of each part
+  int abort;
+};
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool half) {
+  if (half)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Nibbles n (0..3) of both 16-bit halves of w as two 16-bit floats 16 + u: the bits land below the exponent
+// of 16.0 (mantissa weight 1 is bit 3 in bf16, bit 6 in f16).
+template <bool HALF>
+__device__ __forceinline__ uint32_t widen(uint32_t w, int n) {
+  constexpr int kAt = HALF ? 6 : 3;
+  constexpr uint32_t kMask = (0xFu << kAt) * 0x10001u, kMagic = HALF ? 0x4C004C00u : 0x41804180u;
+  const int sh = kAt - 4 * n;
+  const uint32_t x = sh >= 0 ? w << sh : w >> -sh;
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "n"(kMask), "n"(kMagic));  // (x & mask) | magic
+  return r;
+}
+
+// The same less 24: the signed codes q, in bf16.
+__device__ __forceinline__ uint32_t widen_signed(uint32_t w, int n) {
+  const uint32_t x = widen<false>(w, n), bias = 0x41C041C0u;  // 24.0 twice
+  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&bias));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+template <int W>
+struct Words {
+  uint32_t w[W];
+};
+template <int W>
+__device__ __forceinline__ Words<W> lds(uint32_t addr) {
+  Words<W> r;
+  if constexpr (W == 4)
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "r"(addr) : "memory");
+  else if constexpr (W == 2)
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "r"(addr) : "memory");
+  else
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r.w[0]) : "r"(addr) : "memory");
+  return r;
+}
+
+// Stages of a sequence: none without queries (or with more rows than this form takes), one at least with.
+__device__ __forceinline__ int stages_of(const AttnArgs& a, const PagedSeq& s) {
+  if (s.n == 0 || s.n * a.G > a.few_rows) return 0;
+  return max(1, (s.len + kTile - 1) / kTile);
+}
+
+// Header of a part that crosses CTAs: b < 0 for none; `ends` where it reaches its sequence's last stage.
+struct PartHead {
+  int b, h, ends, pad;
+};
+
+// The workspace: per CTA two headers (a part begun by an earlier CTA, a part left to later ones), then their
+// sums, rows x D floats, maxima and weight sums.
+template <int D, int NT>
+__device__ __forceinline__ PartHead* part_head(void* ws, int cta, int which) {
+  return static_cast<PartHead*>(ws) + 2 * cta + which;
+}
+template <int D, int NT>
+__device__ __forceinline__ float* part_sums(void* ws, int ctas, int cta, int which) {
+  return reinterpret_cast<float*>(static_cast<PartHead*>(ws) + 2 * ctas) +
+         static_cast<int64_t>(2 * cta + which) * FewLayout<D, NT>::kPartFloats;
+}
+
+// Channels d .. d + 7 of row r of (sequence starting at query row `first`, head h).
+template <int D, typename T>
+__device__ __forceinline__ void write_out8(const AttnArgs& a, int first, int h, int r, int d, const float (&v)[8]) {
+  const int64_t t = static_cast<int64_t>(first) + r / a.G;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    } else {
+      const __half2 x = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+  }
+  *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + static_cast<int64_t>(h * a.G + r % a.G) * D + d) =
+      make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ void write_lse(const AttnArgs& a, int first, int h, int r, float m, float l) {
+  if (a.lse == nullptr) return;
+  a.lse[(static_cast<int64_t>(first) + r / a.G) * a.Hq + h * a.G + r % a.G] =
+      l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+}
+
+template <int D, int NT, typename T>
+__global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_kernel(const AttnArgs a) {
+  using L = FewLayout<D, NT>;
+  constexpr bool kHalf = std::is_same<T, __half>::value;
+  constexpr int kThreads = L::kWarps * 32;
+  constexpr int kMt = D / 16;    // 16-channel tiles of O^T
+  constexpr int kKw = D / 32;    // words of 8 codes a lane holds of a key
+  constexpr int kVw = D / 64;    // and of a value
+  extern __shared__ __align__(16) uint8_t smem[];
+  auto* ctrl = reinterpret_cast<FewCtrl<D, NT>*>(smem + L::kCtrlOff);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  const uint32_t ring = smem_u32(smem) + warp * L::kRing;
+  const uint32_t bars = smem_u32(ctrl->full + warp * L::kStages);
+  if (lane == 0) {
+    for (int i = 0; i < L::kStages; ++i) mbar_init(bars + 8 * i, 1);
+    mbar_fence_init();
+  }
+  if (tid < 2 * L::kWarps) ctrl->part[tid] = make_int4(-1, 0, 0, 0);
+  if (tid == 0) ctrl->abort = 0;
+  griddep_wait();
+  griddep_launch_dependents();
+
+  // The whole work, this CTA's share and its warps' places in it.
+  long long mine = 0;
+  for (int b = tid; b < a.B; b += kThreads) {
+    const PagedSeq s = paged_seq(a, b);
+    if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+    mine += static_cast<long long>(stages_of(a, s)) * a.H;
+  }
+  auto warp_sum = [&](long long v) {
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(kAllLanes, v, m);
+    return v;
+  };
+  const long long wsum = warp_sum(mine);
+  if (lane == 0) ctrl->scan[warp] = wsum;
+  __syncthreads();
+  long long total = 0;
+#pragma unroll
+  for (int i = 0; i < L::kWarps; ++i) total += ctrl->scan[i];
+  // Less work than CTAs: the first ones take a stage each, so that parts of a head lie in neighbouring CTAs.
+  const long long ctas = min(total, static_cast<long long>(gridDim.x));
+  const long long lo = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
+  const long long hi = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
+  PartHead* heads = part_head<D, NT>(a.workspace, blockIdx.x, 0);
+  if (lo == hi) {
+    if (tid < 2) heads[tid] = PartHead{-1, 0, 0, 0};
+    return;
+  }
+  long long before = 0;
+  for (int base = 0; base < a.B && before < hi; base += kThreads) {
+    long long val = 0;
+    if (base + tid < a.B) val = static_cast<long long>(stages_of(a, paged_seq(a, base + tid))) * a.H;
+    long long incl = val;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const long long o = __shfl_up_sync(kAllLanes, incl, m);
+      if (lane >= m) incl += o;
+    }
+    __syncthreads();
+    if (lane == 31) ctrl->scan[warp] = incl;
+    __syncthreads();
+    long long chunk = 0;
+#pragma unroll
+    for (int i = 0; i < L::kWarps; ++i) {
+      if (i < warp) incl += ctrl->scan[i];
+      chunk += ctrl->scan[i];
+    }
+    const long long first = before + incl - val;
+#pragma unroll 1
+    for (int k = 0; k < L::kWarps; ++k) {
+      const long long at = lo + (hi - lo) * k / L::kWarps;
+      if (at >= first && at < first + val) {
+        ctrl->seq[k] = base + tid;
+        ctrl->start[k] = at - first;
+      }
+    }
+    before += chunk;
+  }
+  __syncthreads();
+
+  const long long w0 = lo + (hi - lo) * warp / L::kWarps, w1 = lo + (hi - lo) * (warp + 1) / L::kWarps;
+  int todo = static_cast<int>(w1 - w0), ahead = todo;  // stages to compute, to issue
+  if (todo > 0) {
+    int b = ctrl->seq[warp];
+    PagedSeq s = paged_seq(a, b);
+    int stages = stages_of(a, s);
+    int h = static_cast<int>(ctrl->start[warp] / stages), t = static_cast<int>(ctrl->start[warp] % stages);
+
+    // Where the copies are: they run ahead across heads and sequences.
+    int pb = b, ph = h, pt = t, pstages = stages, plen = s.len, window = -64, entry = 0;
+    uint32_t missing = 0;  // bit 2 slot + half: that half of the slot's stage has no page
+    auto issue = [&](int slot) {
+      const uint32_t stage = ring + slot * L::kStageBytes, bar = bars + 8 * slot;
+      const int halves = a.page_shift >= 5 ? 1 : 2, tokens = kTile / halves;
+      uint32_t bytes = 0;
+      int64_t row[2];
+      missing &= ~(3u << (2 * slot));
+      for (int i = 0; i < halves; ++i) {
+        const int tok = pt * kTile + i * tokens;
+        if (tok >= plen) break;
+        const int index = tok >> a.page_shift;
+        if (index < window || index >= window + 32) {
+          window = index;
+          entry = static_cast<int64_t>(index + lane) << a.page_shift < plen
+                      ? __ldg(a.table + static_cast<int64_t>(pb) * a.ld_table + index + lane) : 0;
+        }
+        const int page = __shfl_sync(kAllLanes, entry, index - window);
+        if (page < 0 || page >= a.pages) {
+          missing |= (halves == 1 ? 3u : 1u << i) << (2 * slot);
+          if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+          row[i] = -1;
+        } else {
+          row[i] = ((static_cast<int64_t>(page) * a.H + ph) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
+          bytes += tokens * (D + 16);
+        }
+      }
+      if (lane == 0) {
+        mbar_arrive_expect_tx(bar, bytes);
+        for (int i = 0; i < halves; ++i) {
+          const int tok = i * tokens;
+          if (pt * kTile + tok >= plen) break;
+          if (row[i] < 0) continue;
+          bulk_load(stage + tok * (D / 2), a.k_codes + row[i] * (D / 2), tokens * (D / 2), bar);
+          bulk_load(stage + L::kCodeBytes + tok * (D / 2), a.v_codes + row[i] * (D / 2), tokens * (D / 2), bar);
+          bulk_load(stage + 2 * L::kCodeBytes + tok * 8, a.k_params + row[i] * 2, tokens * 8, bar);
+          bulk_load(stage + 2 * L::kCodeBytes + kTile * 8 + tok * 8, a.v_params + row[i] * 2, tokens * 8, bar);
+        }
+      }
+      if (--ahead > 0 && ++pt == pstages) {
+        pt = 0;
+        if (++ph == a.H) {
+          ph = 0;
+          PagedSeq n;
+          do {
+            n = paged_seq(a, ++pb);
+            pstages = stages_of(a, n);
+          } while (pstages == 0);
+          plen = n.len;
+          window = -64;
+        }
+      }
+    };
+    for (int i = 0; i < L::kStages && ahead > 0; ++i) issue(i);
+
+    const int tok_k = (g & ~1) + ((g & 1) ^ ((g >> 1) & 1));              // token of score row g (of 8)
+    const int tok_v0 = 2 * c + (c & 1), tok_v1 = 2 * c + 1 - (c & 1);     // tokens of weight rows 2c, 2c + 1
+    const float sc = a.scale * kLog2e;
+    uint32_t qf[NT][2 * (D / 16)];
+    float qs[NT][2], m[NT][2], l[NT][2], w[NT][2], o[NT][kMt][4];
+    int sees[NT][2], sees_least = 0, t_first = t, rows = 0;
+    bool begin = true, first_part = true;
+#pragma unroll 1
+    for (int it = 0; it < todo; ++it) {
+      const int slot = it % L::kStages;
+      if (begin) {
+        begin = false;
+        t_first = t;
+        rows = s.n * a.G;
+        sees_least = max(0, s.len - s.n + 1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int r = 8 * nt + g;
+          const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first) + r / a.G) * a.ld_q +
+                         static_cast<int64_t>(h * a.G + r % a.G) * D + c * (D / 4);
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < kKw; ++i) {
+            const uint4 u = r < rows ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0u, 0u, 0u, 0u);
+            qf[nt][4 * i] = __byte_perm(u.x, u.z, 0x5410);
+            qf[nt][4 * i + 1] = __byte_perm(u.x, u.z, 0x7632);
+            qf[nt][4 * i + 2] = __byte_perm(u.y, u.w, 0x5410);
+            qf[nt][4 * i + 3] = __byte_perm(u.y, u.w, 0x7632);
+            const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if constexpr (kHalf) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[k]));
+                sum += f.x + f.y;
+              } else {
+                sum += __uint_as_float(x[k] << 16) + __uint_as_float(x[k] & 0xFFFF0000u);
+              }
+            }
+          }
+          sum += __shfl_xor_sync(kAllLanes, sum, 1);
+          sum += __shfl_xor_sync(kAllLanes, sum, 2);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            qs[nt][j] = __shfl_sync(kAllLanes, sum, 4 * (2 * c + j));
+            m[nt][j] = -INFINITY;
+            l[nt][j] = w[nt][j] = 0.f;
+            const int rr = 8 * nt + 2 * c + j;
+            sees[nt][j] = rr < rows ? max(0, min(s.len, s.len - s.n + rr / a.G + 1)) : 0;
+          }
+#pragma unroll
+          for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[nt][mt][k] = 0.f;
+        }
+      }
+      // All lanes go on together or none does.
+      if (!__all_sync(kAllLanes, mbar_wait(bars + 8 * slot, (it / L::kStages) & 1, &ctrl->abort))) break;
+      const uint32_t stage = ring + slot * L::kStageBytes;
+      const uint32_t gone = missing >> (2 * slot) & 3u;
+
+      // Scores of 32 tokens: rows g and g + 8 of each 16, columns 2c and 2c + 1 of each 8 query rows.
+      float z[2][NT][4];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t at = stage + (half * 16 + tok_k) * (D / 2) + c * (D / 8);
+        const Words<kKw> k0 = lds<kKw>(at), k1 = lds<kKw>(at + 8 * (D / 2));
+        float acc[2][NT][4] = {};
+#pragma unroll
+        for (int i = 0; i < kKw; ++i) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const uint32_t f[4] = {widen<kHalf>(k0.w[i], 2 * p), widen<kHalf>(k1.w[i], 2 * p),
+                                   widen<kHalf>(k0.w[i], 2 * p + 1), widen<kHalf>(k1.w[i], 2 * p + 1)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816(acc[p][nt], f, qf[nt][4 * i + 2 * p], qf[nt][4 * i + 2 * p + 1], kHalf);
+          }
+        }
+        const uint32_t par = stage + 2 * L::kCodeBytes + (half * 16 + tok_k) * 8;
+        const Words<2> p0 = lds<2>(par), p1 = lds<2>(par + 64);
+        const float s0 = __uint_as_float(p0.w[0]) * sc, s1 = __uint_as_float(p1.w[0]) * sc;
+        const float b0 = fmaf(-kBias, s0, __uint_as_float(p0.w[1]) * sc), b1 = fmaf(-kBias, s1, __uint_as_float(p1.w[1]) * sc);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            z[half][nt][j] = fmaf(s0, acc[0][nt][j] + acc[1][nt][j], b0 * qs[nt][j]);
+            z[half][nt][2 + j] = fmaf(s1, acc[0][nt][2 + j] + acc[1][nt][2 + j], b1 * qs[nt][j]);
+          }
+        }
+      }
+      const bool whole = (t + 1) * kTile <= sees_least && gone == 0;
+      if (!whole) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int tok = t * kTile + half * 16 + tok_k;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              if (tok >= sees[nt][j] || (gone >> half & 1u)) z[half][nt][j] = -INFINITY;
+              if (tok + 8 >= sees[nt][j] || (gone >> half & 1u)) z[half][nt][2 + j] = -INFINITY;
+            }
+        }
+      }
+
+      bool higher = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float top = fmaxf(fmaxf(z[0][nt][j], z[0][nt][2 + j]), fmaxf(z[1][nt][j], z[1][nt][2 + j]));
+          higher |= top > m[nt][j] + kLazy;
+        }
+      if (__any_sync(kAllLanes, higher)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float keep[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float top = fmaxf(fmaxf(z[0][nt][j], z[0][nt][2 + j]), fmaxf(z[1][nt][j], z[1][nt][2 + j]));
+#pragma unroll
+            for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, k));
+            top = fmaxf(top, m[nt][j]);
+            keep[j] = m[nt][j] == -INFINITY ? 0.f : ex2(m[nt][j] - top);
+            m[nt][j] = top;
+            l[nt][j] *= keep[j];
+            w[nt][j] *= keep[j];
+          }
+#pragma unroll
+          for (int mt = 0; mt < kMt; ++mt) {
+            o[nt][mt][0] *= keep[0];
+            o[nt][mt][1] *= keep[1];
+            o[nt][mt][2] *= keep[0];
+            o[nt][mt][3] *= keep[1];
+          }
+        }
+      }
+
+      // Weights, their sums, and O^T += V^T P^T.
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t par = stage + 2 * L::kCodeBytes + kTile * 8 + (half * 16 + tok_k) * 8;
+        const Words<2> p0 = lds<2>(par), p1 = lds<2>(par + 64);
+        float s0 = __uint_as_float(p0.w[0]), s1 = __uint_as_float(p1.w[0]);
+        float b0 = __uint_as_float(p0.w[1]), b1 = __uint_as_float(p1.w[1]);
+        if (!whole) {  // what no query sees may hold anything
+          const int tok = t * kTile + half * 16 + tok_k;
+          const bool out = gone >> half & 1u;
+          if (tok >= s.len || out) s0 = b0 = 0.f;
+          if (tok + 8 >= s.len || out) s1 = b1 = 0.f;
+        }
+        uint32_t hi[NT][2], low[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float pv[4];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float mm = m[nt][j] == -INFINITY ? 0.f : m[nt][j];
+            const float pa = ex2(z[half][nt][j] - mm), pb2 = ex2(z[half][nt][2 + j] - mm);
+            l[nt][j] += pa + pb2;
+            w[nt][j] = fmaf(pa, b0, fmaf(pb2, b1, w[nt][j]));
+            pv[j] = pa * s0;
+            pv[2 + j] = pb2 * s1;
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t x = pack_bf16(pv[2 * i], pv[2 * i + 1]);
+            hi[nt][i] = transpose8x8(x);
+            if constexpr (kHalf)
+              low[nt][i] = transpose8x8(pack_bf16(pv[2 * i] - __uint_as_float(x << 16),
+                                                  pv[2 * i + 1] - __uint_as_float(x & 0xFFFF0000u)));
+          }
+        }
+        const uint32_t at = stage + L::kCodeBytes + half * 16 * (D / 2) + g * (D / 16);
+        const Words<kVw> va = lds<kVw>(at + tok_v0 * (D / 2)), vb = lds<kVw>(at + tok_v1 * (D / 2));
+        const Words<kVw> vc = lds<kVw>(at + (tok_v0 + 8) * (D / 2)), vd = lds<kVw>(at + (tok_v1 + 8) * (D / 2));
+#pragma unroll
+        for (int i = 0; i < kVw; ++i) {
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+            const uint32_t x = __byte_perm(va.w[i], vb.w[i], part ? 0x7632 : 0x5410);
+            const uint32_t y = __byte_perm(vc.w[i], vd.w[i], part ? 0x7632 : 0x5410);
+#pragma unroll
+            for (int n = 0; n < 4; n += 2) {
+              const uint32_t f[4] = {widen_signed(x, n), widen_signed(x, n + 1), widen_signed(y, n), widen_signed(y, n + 1)};
+              const int mt = 4 * i + 2 * part + n / 2;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                mma16816(o[nt][mt], f, hi[nt][0], hi[nt][1], false);
+                if constexpr (kHalf) mma16816(o[nt][mt], f, low[nt][0], low[nt][1], false);
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (ahead > 0) issue(slot);
+
+      ++t;
+      if (t < stages && it + 1 < todo) continue;
+      // The end of this head's stages, or of the warp's.
+      const bool complete = t_first == 0 && t == stages;
+      float* part = reinterpret_cast<float*>(first_part ? smem + L::kPartOff + warp * L::kPartBytes
+                                                        : smem + warp * L::kRing);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int k = 4; k < 32; k <<= 1) {
+            l[nt][j] += __shfl_xor_sync(kAllLanes, l[nt][j], k);
+            w[nt][j] += __shfl_xor_sync(kAllLanes, w[nt][j], k);
+          }
+          const int r = 8 * nt + 2 * c + j;
+          if (complete) {
+            if (r < rows) {
+              const float inv = l[nt][j] > 0.f ? __fdividef(1.f, l[nt][j]) : 0.f;
+#pragma unroll
+              for (int q8 = 0; q8 < kMt / 4; ++q8) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (o[nt][4 * q8 + e / 2][j + 2 * (e & 1)] + w[nt][j]) * inv;
+                write_out8<D, T>(a, s.first, h, r, g * (D / 8) + 8 * q8, v);
+              }
+              if (g == 0) write_lse(a, s.first, h, r, m[nt][j], l[nt][j]);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < D / 8; ++e) part[r * D + g * (D / 8) + e] = o[nt][e / 2][j + 2 * (e & 1)] + w[nt][j];
+            if (g == 0) {
+              part[L::kRows * D + r] = m[nt][j];
+              part[L::kRows * D + L::kRows + r] = l[nt][j];
+            }
+          }
+        }
+      }
+      if (!complete && lane == 0) ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, h, t_first, t == stages ? -1 : t);
+      first_part = false;
+      begin = true;
+      if (it + 1 < todo) {
+        t = 0;
+        if (++h == a.H) {
+          h = 0;
+          do {
+            s = paged_seq(a, ++b);
+            stages = stages_of(a, s);
+          } while (stages == 0);
+        }
+      }
+    }
+    if (ctrl->abort) {  // copies in flight land before the CTA ends
+      if (lane == 0) {
+        for (int i = 0; i < L::kStages; ++i) {
+          const int last = (todo - ahead - 1 - i) / L::kStages;  // uses of slot i issued so far, less one
+          if (todo - ahead > i) mbar_wait_teardown(bars + 8 * i, last & 1);
+        }
+        *a.status = OFFQ_ERR_TIMEOUT;
+      }
+    }
+  }
+
+  // Parts of the same head, in order of their stages, into one: an output where they are all of it, else a part
+  // for the joining kernel.
+  __syncthreads();
+  bool have0 = false, have1 = false;
+  for (int i = 0; i < 2 * L::kWarps;) {
+    const int4 p = ctrl->part[i];
+    if (p.x < 0) {
+      ++i;
+      continue;
+    }
+    int end = i + 1, last = p.w;
+    for (int k = i + 1; k < 2 * L::kWarps; ++k) {
+      const int4 n = ctrl->part[k];
+      if (n.x < 0) continue;
+      if (n.x != p.x || n.y != p.y) break;
+      end = k + 1;
+      last = n.w;
+    }
+    const bool complete = p.z == 0 && last < 0;
+    const int which = p.z == 0 ? 1 : 0;
+    float* dst = part_sums<D, NT>(a.workspace, gridDim.x, blockIdx.x, which);
+    if (!complete) (which ? have1 : have0) = true;
+    if (!complete && tid == 0) heads[which] = PartHead{p.x, p.y, last < 0, 0};
+    const PagedSeq s = paged_seq(a, p.x);
+    for (int u = tid; u < L::kRows * (D / 8); u += kThreads) {
+      const int r = u / (D / 8), d = u % (D / 8) * 8;
+      float top = -INFINITY, sum = 0.f, v[8] = {};
+      for (int k = i; k < end; ++k) {
+        if (ctrl->part[k].x < 0) continue;
+        const float* src = reinterpret_cast<const float*>(k & 1 ? smem + (k >> 1) * L::kRing
+                                                                : smem + L::kPartOff + (k >> 1) * L::kPartBytes);
+        const float mk = src[L::kRows * D + r], next = fmaxf(top, mk);
+        const float x = top == -INFINITY ? 0.f : ex2(top - next), y = mk == -INFINITY ? 0.f : ex2(mk - next);
+        sum = sum * x + src[L::kRows * D + L::kRows + r] * y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = v[e] * x + src[r * D + d + e] * y;
+        top = next;
+      }
+      if (complete) {
+        if (r < s.n * a.G) {
+          const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= inv;
+          write_out8<D, T>(a, s.first, p.y, r, d, v);
+          if (d == 0) write_lse(a, s.first, p.y, r, top, sum);
+        }
+      } else {
+        reinterpret_cast<float4*>(dst + r * D + d)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(dst + r * D + d)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        if (d == 0) {
+          dst[L::kRows * D + r] = top;
+          dst[L::kRows * D + L::kRows + r] = sum;
+        }
+      }
+    }
+    i = end;
+  }
+  if (tid == 0) {
+    if (!have0) heads[0] = PartHead{-1, 0, 0, 0};
+    if (!have1) heads[1] = PartHead{-1, 0, 0, 0};
+  }
+}
+
+// A head that crosses CTAs: begun at the end of CTA c, then the first parts of the CTAs after it up to its last.
+template <int D, int NT, typename T>
+__global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int ctas) {
+  using L = FewLayout<D, NT>;
+  __shared__ int s_last;
+  const int cta = blockIdx.x, tid = threadIdx.x;
+  if (tid == 0) s_last = 0x7FFFFFFF;
+  griddep_wait();
+  griddep_launch_dependents();
+  const PartHead p = *part_head<D, NT>(a.workspace, cta, 1);
+  if (p.b < 0) return;
+  __syncthreads();
+  for (int k = cta + 1 + tid; k < ctas; k += blockDim.x) {
+    const PartHead n = *part_head<D, NT>(a.workspace, k, 0);
+    if (n.b == p.b && n.h == p.h && n.ends) atomicMin(&s_last, k);
+  }
+  __syncthreads();
+  const int last = s_last;
+  if (last >= ctas) return;  // a CTA gave up: the status word says so
+  const PagedSeq s = paged_seq(a, p.b);
+  const int rows = s.n * a.G;
+  for (int u = tid; u < rows * (D / 8); u += blockDim.x) {
+    const int r = u / (D / 8), d = u % (D / 8) * 8;
+    float top = -INFINITY, sum = 0.f, v[8] = {};
+#pragma unroll 4
+    for (int k = cta; k <= last; ++k) {
+      const float* src = part_sums<D, NT>(a.workspace, ctas, k, k == cta ? 1 : 0);
+      const float mk = src[L::kRows * D + r], lk = src[L::kRows * D + L::kRows + r];
+      const float4 x0 = reinterpret_cast<const float4*>(src + r * D + d)[0];
+      const float4 x1 = reinterpret_cast<const float4*>(src + r * D + d)[1];
+      const float next = fmaxf(top, mk);
+      const float x = top == -INFINITY ? 0.f : ex2(top - next), y = mk == -INFINITY ? 0.f : ex2(mk - next);
+      sum = sum * x + lk * y;
+      const float n[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = v[e] * x + n[e] * y;
+      top = next;
+    }
+    const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= inv;
+    write_out8<D, T>(a, s.first, p.h, r, d, v);
+    if (d == 0) write_lse(a, s.first, p.h, r, top, sum);
+  }
+}
+
+template <int D, int NT, typename T>
+int launch_few(const AttnArgs& a, cudaStream_t s) {
+  using L = FewLayout<D, NT>;
+  static_assert(sizeof(FewCtrl<D, NT>) <= 1024, "control block");
+  const int sms = device_sms();
+  if (sms == 0 || !smem_optin<paged_few_kernel<D, NT, T>>(L::kBytes)) return OFFQ_ERR_CUDA;
+  if (const int rc = launch_pdl(paged_few_kernel<D, NT, T>, dim3(sms), dim3(L::kWarps * 32), L::kBytes, s, a);
+      rc != OFFQ_OK)
+    return rc;
+  return launch_pdl(join_parts_kernel<D, NT, T>, dim3(sms), dim3(256), 0, s, a, sms);
+}
+
+template <int D>
+int launch_few_d(const AttnArgs& a, int dtype, cudaStream_t s) {
+  const bool two = std::min<int64_t>(static_cast<int64_t>(a.max_q) * a.G, a.few_rows) > 8;
+  if (dtype == OFFQ_BF16) return two ? launch_few<D, 2, __nv_bfloat16>(a, s) : launch_few<D, 1, __nv_bfloat16>(a, s);
+  return two ? launch_few<D, 2, __half>(a, s) : launch_few<D, 1, __half>(a, s);
+}
+
+}  // namespace
+
+namespace offq {
+
+int64_t paged_few_workspace(int head_dim) {
+  const int sms = device_sms();
+  const int64_t floats = kFewRows * (head_dim + 2);
+  return sms == 0 ? -1 : 2 * static_cast<int64_t>(sms) * (static_cast<int64_t>(sizeof(PartHead)) + 4 * floats);
+}
+
+int paged_few(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
+  return head_dim == 128 ? launch_few_d<128>(a, dtype, s) : launch_few_d<64>(a, dtype, s);
+}
+
+}  // namespace offq
