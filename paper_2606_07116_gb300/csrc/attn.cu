@@ -226,5 +226,5 @@ extern "C" int offq_prompt_attention(const void* q, const void* k, const void* v
   a.lse = lse;
   a.status = device_status_ptr();
   if (a.status == nullptr) return OFFQ_ERR_CUDA;
-  return launch_rows<false>(a, dtype, head_dim, static_cast<cudaStream_t>(stream));
+  return prompt_tc(a, dtype, head_dim, static_cast<cudaStream_t>(stream));
 }

@@ -82,4 +82,7 @@ constexpr int kFewRows = 16;
 int64_t paged_few_workspace(int head_dim);
 int paged_few(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
 
+// Prompts on the tensor cores (csrc/attn_prompt.cu), arguments already checked.
+int prompt_tc(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
+
 }  // namespace offq

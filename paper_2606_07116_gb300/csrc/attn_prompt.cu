@@ -1,0 +1,409 @@
+// Attention inside packed prompts (offq_prompt_attention) on the tensor cores.
+//
+// A CTA takes two tiles of 128 query rows: the same 128 tokens of two heads that share their keys, or
+// 256 tokens of one head where the heads per key head are odd. Per block of 128 keys a tile runs
+//   S = Q K^T (operands in shared memory), weights P = 2^(scale log2(e) S - m) by one thread per row,
+//   O += P V (P in tensor memory, V as it lies: its rows are contracted).
+// S and O stay in tensor memory (2 x 128 + 2 x D columns); P takes the place of its S. While one tile's
+// rows are in the softmax the other's products run, so the tensor cores wait only where the softmax is
+// the longer of the two.
+//
+// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 the TMA copies.
+// The maximum is moved only when a score passes it by 2^8 (kLazy), so O is rescaled rarely and by the
+// softmax threads themselves: when S is complete, so is every product issued before it, O's among them.
+//
+// Rows past a sequence's end are the next sequence's. As queries they are not written, as keys their
+// scores are replaced, and as values they are zeroed in shared memory (0 times infinity is not 0).
+#include <algorithm>
+
+#include "attn_tc.cuh"
+
+namespace {
+
+using namespace offq;
+
+constexpr int kThreads = 384;  // two softmax warpgroups, one of single warps
+// Registers: 168 a thread at launch, 3 x 168 >= 2 x 216 + 72.
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "register shares");
+
+template <int D>
+struct PromptLayout {
+  static constexpr int kTileBytes = kKt * D * 2;
+  static constexpr int kSlots = D == 128 ? 5 : 8;           // keys and values in turn
+  static constexpr int kRing = 2 * kTileBytes;              // behind the two query tiles
+  static constexpr int kCtrl = kRing + kSlots * kTileBytes;
+  static constexpr int kBytes = kCtrl + 256 + 1024;         // barriers; alignment to 1024
+  static_assert(kBytes <= 232448, "shared memory");
+};
+
+struct PromptCtrl {
+  uint64_t q_full, tail, done;
+  uint64_t full[8], empty[8];
+  uint64_t s_full[2], p_ready[2];
+  uint32_t tmem;
+  int abort;
+  int seq, tile;
+};
+static_assert(sizeof(PromptCtrl) <= 256, "control block");
+
+// Queries of sequence b (its first row in `first`); none where its entries are out of range.
+__device__ __forceinline__ int prompt_seq(const AttnArgs& a, int b, int& first, bool& bad) {
+  const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
+  first = c0;
+  bad = c0 < 0 || c1 < c0 || c1 > a.Tq;
+  return bad ? 0 : c1 - c0;
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+              const __grid_constant__ CUtensorMap vmap) {
+  using L = PromptLayout<D>;
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+  auto* ctrl = reinterpret_cast<PromptCtrl*>(smem + L::kCtrl);
+  volatile int* abort = &ctrl->abort;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool two_heads = (a.G & 1) == 0;
+  const int units = two_heads ? a.Hq / 2 : a.Hq;       // per query tile
+  const int step = two_heads ? kQt : 2 * kQt;          // tokens per query tile
+  if (tid == 0) {
+    mbar_init(smem_u32(&ctrl->q_full), 1);
+    mbar_init(smem_u32(&ctrl->tail), 1);
+    mbar_init(smem_u32(&ctrl->done), 1);
+    for (int i = 0; i < 8; ++i) {
+      mbar_init(smem_u32(&ctrl->full[i]), 1);
+      mbar_init(smem_u32(&ctrl->empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&ctrl->s_full[i]), 1);
+      mbar_init(smem_u32(&ctrl->p_ready[i]), 4);
+    }
+    ctrl->abort = 0;
+    mbar_fence_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(smem_u32(&ctrl->tmem), 512);
+    tmem_relinquish();
+  }
+  griddep_wait();
+  griddep_launch_dependents();
+  if (warp == 9) {
+    // The CTA's query tile: the last ones first, as the later rows of a causal sequence see the most.
+    int total = 0;
+    for (int base = 0; base < a.B; base += 32) {
+      int n = 0, first;
+      bool bad = false;
+      if (base + lane < a.B) n = prompt_seq(a, base + lane, first, bad);
+      if (bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+      total += (n + step - 1) / step;
+    }
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) total += __shfl_xor_sync(kAllLanes, total, m);
+    const int at = total - 1 - static_cast<int>(blockIdx.x / units);
+    if (lane == 0) ctrl->seq = -1;
+    __syncwarp();
+    int before = 0;
+    for (int base = 0; base < a.B && at >= before && at >= 0; base += 32) {
+      int n = 0, first;
+      bool bad = false;
+      if (base + lane < a.B) n = prompt_seq(a, base + lane, first, bad);
+      const int tiles = (n + step - 1) / step;
+      int incl = tiles;
+#pragma unroll
+      for (int m = 1; m < 32; m <<= 1) {
+        const int o = __shfl_up_sync(kAllLanes, incl, m);
+        if (lane >= m) incl += o;
+      }
+      const int start = before + incl - tiles;
+      if (at >= start && at < start + tiles) {
+        ctrl->seq = base + lane;
+        ctrl->tile = at - start;
+      }
+      before += __shfl_sync(kAllLanes, incl, 31);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctrl->tmem;
+  const int seq = ctrl->seq;
+  if (seq >= 0) {
+    int first;
+    bool bad;
+    const int n = prompt_seq(a, seq, first, bad);
+    const int unit = static_cast<int>(blockIdx.x % units);
+    int head[2], row0[2], blocks[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      head[i] = two_heads ? 2 * unit + i : unit;
+      row0[i] = ctrl->tile * step + (two_heads ? 0 : i * kQt);
+      const int sees = a.causal ? min(row0[i] + kQt, n) : n;
+      blocks[i] = row0[i] < n ? (sees + kKt - 1) / kKt : 0;
+    }
+    const int kv_head = head[0] / a.G;
+    const int most = max(blocks[0], blocks[1]);
+    const uint32_t q_s = smem_u32(smem), ring = q_s + L::kRing;
+    const uint32_t full = smem_u32(ctrl->full), empty = smem_u32(ctrl->empty);
+
+    if (warp >= 8) {
+      fewer_registers<kOtherRegs>();
+      if (warp == 9) {
+        // Copies: both query tiles, then K0 V0 K1 V1 ...
+        int issued = 0;
+        bool ok = true;
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&ctrl->q_full);
+          mbar_arrive_expect_tx(bar, (blocks[1] > 0 ? 2 : 1) * L::kTileBytes);
+          for (int i = 0; i < 2; ++i) {
+            if (blocks[i] == 0) continue;
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_2d(q_s + i * L::kTileBytes + c * kAtom, &qmap, bar, head[i] * D + 64 * c, first + row0[i]);
+          }
+        }
+        const int left = n - (most - 1) * kKt;  // keys of the last block
+        for (int it = 0; it < 2 * most && ok; ++it) {
+          const int slot = it % L::kSlots;
+          const bool is_v = it & 1, tail = is_v && it / 2 == most - 1 && left < kKt;
+          if (it >= L::kSlots) ok = mbar_wait(empty + 8 * slot, ((it / L::kSlots) - 1) & 1, abort);
+          ok = __all_sync(kAllLanes, ok);
+          if (!ok) break;
+          const uint32_t dst = ring + slot * L::kTileBytes, bar = tail ? smem_u32(&ctrl->tail) : full + 8 * slot;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar, L::kTileBytes);
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_2d(dst + c * kAtom, is_v ? &vmap : &kmap, bar, kv_head * D + 64 * c, first + it / 2 * kKt);
+          }
+          __syncwarp();
+          issued = it + 1;
+          if (tail) {
+            ok = __all_sync(kAllLanes, mbar_wait(bar, 0, abort));
+            if (!ok) break;
+            for (int i = lane; i < (kKt - left) * (D / 8); i += 32) {
+              const int r = left + i / (D / 8), ch = i % (D / 8);
+              sts_zero16(dst + (ch >> 3) * kAtom + r * 128 + (ch & 7) * 16);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8 * slot);
+          }
+        }
+        if (*abort && lane == 0) {  // copies in flight land before the CTA ends
+          mbar_wait_teardown(smem_u32(&ctrl->q_full), 0);
+          for (int it = std::max(0, issued - L::kSlots); it < issued; ++it) {
+            const bool tail = (it & 1) && it / 2 == most - 1 && left < kKt;
+            mbar_wait_teardown(tail ? smem_u32(&ctrl->tail) : full + 8 * (it % L::kSlots), tail ? 0 : (it / L::kSlots) & 1);
+          }
+        }
+        __syncwarp();
+      } else if (warp == 8) {
+        // Products. The whole warp runs the loop; an elected lane issues.
+        constexpr uint32_t kIdescS = idesc_16<T>(128, kKt, false), kIdescO = idesc_16<T>(128, D, true);
+        auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(kAllLanes, mbar_wait(bar, parity, abort)); };
+        auto scores = [&](int i, int j) {  // S_i = Q_i K_j^T
+          const uint64_t qd = smem_desc_sw128(q_s + i * L::kTileBytes);
+          const uint64_t kd = smem_desc_sw128(ring + (2 * j) % L::kSlots * L::kTileBytes);
+  #pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = ((kk >> 2) * kAtom + (kk & 3) * 32) >> 4;
+            mma_bf16(tmem + i * 128, qd + off, kd + off, kIdescS, kk != 0);
+          }
+          mma_commit(smem_u32(&ctrl->s_full[i]));
+        };
+        auto outputs = [&](int i, int j) {  // O_i += P_i V_j
+          const uint64_t vd = smem_desc_rows_contracted(ring + (2 * j + 1) % L::kSlots * L::kTileBytes);
+  #pragma unroll
+          for (int kk = 0; kk < kKt / 16; ++kk)
+            mma_16_ts(tmem + 256 + i * D, tmem + i * 128 + kk * 8, vd + ((kk * 16 * 128) >> 4), kIdescO, (j | kk) != 0);
+        };
+        bool ok = wait(smem_u32(&ctrl->q_full), 0) && wait(full, 0);
+        if (ok) {
+          tc_fence_after();
+          if (elect_one()) {
+            for (int i = 0; i < 2; ++i)
+              if (blocks[i] > 0) scores(i, 0);
+            mma_commit(empty);
+          }
+          __syncwarp();
+        }
+        for (int j = 0; j < most && ok; ++j) {
+          const int vs = 2 * j + 1, ks = 2 * j + 2;
+          ok = wait(full + 8 * (vs % L::kSlots), (vs / L::kSlots) & 1);
+          if (ok && j + 1 < most) ok = wait(full + 8 * (ks % L::kSlots), (ks / L::kSlots) & 1);
+          for (int i = 0; i < 2 && ok; ++i) {
+            if (j >= blocks[i]) continue;
+            ok = wait(smem_u32(&ctrl->p_ready[i]), j & 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              outputs(i, j);
+              if (j + 1 < blocks[i]) scores(i, j + 1);
+              else mma_commit(smem_u32(&ctrl->s_full[i]));  // the last phase says that O is complete
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
+          if (j + 1 < most && elect_one()) {  // nobody waits for the last block's buffer: no arrival may outlive the CTA
+            mma_commit(empty + 8 * (vs % L::kSlots));
+            mma_commit(empty + 8 * (ks % L::kSlots));
+          }
+          __syncwarp();
+        }
+        if (__any_sync(kAllLanes, *abort)) {  // products in flight end before tensor memory is released
+          if (elect_one()) {
+            mma_commit(smem_u32(&ctrl->done));
+            mbar_wait_teardown(smem_u32(&ctrl->done), 0);
+          }
+          __syncwarp();
+        }
+      }
+    } else {
+      more_registers<kSoftmaxRegs>();
+      const int i = warp >> 2;
+      if (blocks[i] > 0) {
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
+        const int row = row0[i] + (warp & 3) * 32 + lane;   // in the sequence
+        const float sc = a.scale * kLog2e;
+        float m = -INFINITY, sum = 0.f;
+        bool ok = true;
+        for (int j = 0; j < blocks[i]; ++j) {
+          ok = __all_sync(kAllLanes, mbar_wait(smem_u32(&ctrl->s_full[i]), j & 1, abort));
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t s[kKt];
+          tmem_ld_128cols(s_tm, s);
+          if ((j + 1) * kKt > (a.causal ? min(row0[i] + 1, n) : n)) {
+            const int valid = (a.causal ? min(row + 1, n) : n) - j * kKt;
+#pragma unroll
+            for (int e = 0; e < kKt; ++e)
+              if (e >= valid) s[e] = 0xFF800000u;  // -inf
+          }
+          float top = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < kKt; e += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+          top *= sc;
+          const bool move = top > m + kLazy;
+          if (__any_sync(kAllLanes, move)) {
+            const float next = move ? top : m;
+            const float keep = m == -INFINITY ? 0.f : ex2(m - next);
+            m = next;
+            sum *= keep;
+            if (j > 0) {
+#pragma unroll
+              for (int q = 0; q < D / 16; ++q) {
+                uint32_t o[16];
+                tmem_ld_16cols(o_tm + 16 * q, o);
+                tmem_ld_wait_for(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                tmem_st_16cols(o_tm + 16 * q, o);
+              }
+            }
+          }
+          const float mm = m == -INFINITY ? 0.f : m;
+          const uint64_t sc2 = pack2(sc, sc), m2 = pack2(-mm, -mm);
+          uint64_t part[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              float x, y;
+              unpack2(fma2v(pack2(__uint_as_float(s[32 * q + e]), __uint_as_float(s[32 * q + e + 1])), sc2, m2), x, y);
+              x = ex2(x);
+              y = ex2(y);
+              part[(e >> 1) & 3] = add2_rn(part[(e >> 1) & 3], pack2(x, y));
+              p[e / 2] = pack_16<T>(x, y);
+            }
+            tmem_st_16cols(s_tm + 16 * q, p);
+          }
+          float x, y;
+          unpack2(add2_rn(add2_rn(part[0], part[1]), add2_rn(part[2], part[3])), x, y);
+          sum += x + y;
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_ready[i]));
+        }
+        if (ok) ok = __all_sync(kAllLanes, mbar_wait(smem_u32(&ctrl->s_full[i]), blocks[i] & 1, abort));
+        if (ok) {
+          tc_fence_after();
+          const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+          const int64_t t = static_cast<int64_t>(first) + row;
+#pragma unroll
+          for (int q = 0; q < D / 32; ++q) {
+            uint32_t o[32];
+            tmem_ld_32cols(o_tm + 32 * q, o);
+            tmem_ld_wait_for(o);
+            if (row < n) {
+              uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out +
+                                                    static_cast<int64_t>(head[i]) * D + 32 * q);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  w[k] = pack_16<T>(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
+                dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            }
+            __syncwarp();
+          }
+          if (row < n && a.lse != nullptr) a.lse[t * a.Hq + head[i]] = sum > 0.f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (tid == 0 && ctrl->abort) *a.status = OFFQ_ERR_TIMEOUT;
+  if (warp == 8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+int heads_map(CUtensorMap* map, const void* x, int dtype, int64_t rows, int64_t width, int64_t ld) {
+  const auto enc = tensor_map_encoder();
+  if (enc == nullptr) return OFFQ_ERR_CUDA;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[2] = {64, 128};
+  const cuuint32_t elem_strides[2] = {1, 1};
+  const CUresult r = enc(map, dtype == OFFQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                         const_cast<void*>(x), dims, strides, box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? OFFQ_OK : OFFQ_ERR_CUDA;
+}
+
+template <int D, typename T>
+int launch_prompt(const AttnArgs& a, int dtype, cudaStream_t s) {
+  using L = PromptLayout<D>;
+  if (!smem_optin<prompt_kernel<D, T>>(L::kBytes)) return OFFQ_ERR_CUDA;
+  CUtensorMap q, k, v;
+  if (heads_map(&q, a.q, dtype, a.Tq, static_cast<int64_t>(a.Hq) * D, a.ld_q) != OFFQ_OK ||
+      heads_map(&k, a.k, dtype, a.Tq, static_cast<int64_t>(a.H) * D, a.ld_k) != OFFQ_OK ||
+      heads_map(&v, a.v, dtype, a.Tq, static_cast<int64_t>(a.H) * D, a.ld_v) != OFFQ_OK)
+    return OFFQ_ERR_CUDA;
+  const bool two_heads = (a.G & 1) == 0;
+  const int64_t step = two_heads ? kQt : 2 * kQt;
+  const int64_t tiles = a.Tq / step + std::min<int64_t>(a.B, a.Tq);  // at most: a whole one per step, a ragged one per sequence
+  const int64_t grid = tiles * (two_heads ? a.Hq / 2 : a.Hq);
+  if (grid > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
+  return launch_pdl(prompt_kernel<D, T>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), L::kBytes, s, a, q, k, v);
+}
+
+}  // namespace
+
+namespace offq {
+
+int prompt_tc(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
+  if (head_dim == 128)
+    return dtype == OFFQ_BF16 ? launch_prompt<128, __nv_bfloat16>(a, dtype, s) : launch_prompt<128, __half>(a, dtype, s);
+  return dtype == OFFQ_BF16 ? launch_prompt<64, __nv_bfloat16>(a, dtype, s) : launch_prompt<64, __half>(a, dtype, s);
+}
+
+}  // namespace offq
