@@ -82,6 +82,9 @@ constexpr int kFewRows = 16;
 int64_t paged_few_workspace(int head_dim);
 int paged_few(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
 
+// The many-row form (csrc/attn_chunk.cu): sequences with more rows.
+int64_t paged_chunk_workspace(int head_dim);
+int paged_chunk(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
 // Prompts on the tensor cores (csrc/attn_prompt.cu), arguments already checked.
 int prompt_tc(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
 
