@@ -15,12 +15,15 @@
 //   S^T [tokens x rows]  = codes K [16 x 16 channels] * Q^T [16 channels x 8 rows]
 //   O^T [channels x rows] += codes V^T [16 channels x 16 tokens] * P^T [16 tokens x 8 rows]
 // with the rows on the MMA's 8-wide side, as there are few. Channels may be contracted in any order and tokens
-// too, so fragments are what a lane finds in its 16-byte reads: a code needs half a shift and half a logical
-// operation. The nibble u = q + 8 becomes the 16-bit float 16 + u (its bits placed below the exponent of
-// 16.0): exact, and the 24 on top of q leaves as -24 * sum(query) and -24 * sum(weights).
-//   z_j = s_j (acc_j - 24 Q) + o_j Q,  Q = sum of the query;   out = (O - 24 sum P' + sum p o_v) / sum p,
-// P' = p s_v rounded to bf16 (in two bf16 parts, 16 bits, for half-precision outputs: s_v has no range that a
-// half could hold).
+// too, so fragments are what a lane finds in its 16-byte reads. A key's nibble u = q + 8 becomes the 16-bit float
+// 16 + u (its bits placed below the exponent of 16.0), exact: half a shift and half a logical operation a code; the 24
+// on top of q leaves as -24 times the query's sum. A value's becomes 1024 + u or 1024 + 16 u as a half (one shift
+// for 8 codes) and one packed multiply-add takes it to q: left in, the bias would be summed over the whole context, and
+// what is left of values that average out would be its rounding errors.
+//   z_j = s_j (acc_j - 24 Q) + o_j Q,  Q = sum of the query;   out = (O + sum p o_v) / sum p,
+// O summed with P' = p s_v as halves, p = 2^(z - m). The reference m follows the largest z_j + log2(s_v), so that P'
+// fits a half whatever the values' size; it moves only when some P' passes 2^8 (or p 2^32). Scores are taken relative
+// to it as they are made; a stage that must move it, or has tokens that some row does not see, does its softmax again.
 #include <algorithm>
 #include <type_traits>
 
@@ -35,8 +38,8 @@ constexpr float kBias = 24.0f;
 
 template <int D, int NT>
 struct FewLayout {
-  static constexpr int kWarps = 8;
-  static constexpr int kStages = 4;
+  static constexpr int kWarps = NT == 1 ? 12 : 8;   // as many as registers and rings allow
+  static constexpr int kStages = NT == 1 ? 3 : 4;
   static constexpr int kCodeBytes = kTile * D / 2;
   static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kTile * 8;
   static constexpr int kRows = 8 * NT;
@@ -47,7 +50,7 @@ struct FewLayout {
   static constexpr int kCtrlOff = kPartOff + kWarps * kPartBytes;
   static constexpr int kBytes = kCtrlOff + 1024;
   static_assert(kPartBytes <= kRing, "a part fits into its warp's ring");
-  static_assert(kBytes <= 232448 && kWarps * kStages * 8 + 512 <= 1024, "shared memory");
+  static_assert(kBytes <= 232448, "shared memory");
 };
 
 // Control block behind the parts.
@@ -85,11 +88,13 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, int n) {
   return r;
 }
 
-// The same less 24: the signed codes q, in bf16.
-__device__ __forceinline__ uint32_t widen_signed(uint32_t w, int n) {
-  const uint32_t x = widen<false>(w, n), bias = 0x41C041C0u;  // 24.0 twice
-  const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&bias));
-  return *reinterpret_cast<const uint32_t*>(&v);
+// Nibbles 0 and 1 of both halves of w as signed codes q in f16 (2 and 3 of w shifted right by 8).
+__device__ __forceinline__ void widen_signed(uint32_t w, uint32_t& even, uint32_t& odd) {
+  uint32_t x, y;
+  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x) : "r"(w));  // 1024 + u
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(y) : "r"(w));  // 1024 + 16 u
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(even) : "r"(x), "r"(0x64086408u));                        // - 1032
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(odd) : "r"(y), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
 }
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
@@ -100,6 +105,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
@@ -158,8 +167,7 @@ __device__ __forceinline__ void write_out8(const AttnArgs& a, int first, int h, 
     if constexpr (std::is_same<T, __nv_bfloat16>::value) {
       w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
     } else {
-      const __half2 x = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&x);
+      w[i] = pack_f16(v[2 * i], v[2 * i + 1]);
     }
   }
   *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + static_cast<int64_t>(h * a.G + r % a.G) * D + d) =
@@ -263,55 +271,60 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
 
     // Where the copies are: they run ahead across heads and sequences.
     int pb = b, ph = h, pt = t, pstages = stages, plen = s.len, window = -64, entry = 0;
-    uint32_t missing = 0;  // bit 2 slot + half: that half of the slot's stage has no page
+    int64_t page_row = -1;   // first row of the page the copies are in
+    bool turn = true;        // that page is not known yet
+    uint32_t missing = 0;    // bit 2 slot + half: that half of the slot's stage has no page
+    auto find_page = [&](int tok) {  // first row of the page of token tok, or -1
+      const int index = tok >> a.page_shift;
+      if (index < window || index >= window + 32) {
+        window = index;
+        entry = static_cast<int64_t>(index + lane) << a.page_shift < plen
+                    ? __ldg(a.table + static_cast<int64_t>(pb) * a.ld_table + index + lane) : 0;
+      }
+      const int page = __shfl_sync(kAllLanes, entry, index - window);
+      if (page >= 0 && page < a.pages) return (static_cast<int64_t>(page) * a.H + ph) << a.page_shift;
+      if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+      return static_cast<int64_t>(-1);
+    };
+    auto copy = [&](uint32_t stage, uint32_t bar, int at, int tokens, int64_t row) {
+      bulk_load(stage + at * (D / 2), a.k_codes + row * (D / 2), tokens * (D / 2), bar);
+      bulk_load(stage + L::kCodeBytes + at * (D / 2), a.v_codes + row * (D / 2), tokens * (D / 2), bar);
+      bulk_load(stage + 2 * L::kCodeBytes + at * 8, a.k_params + row * 2, tokens * 8, bar);
+      bulk_load(stage + 2 * L::kCodeBytes + kTile * 8 + at * 8, a.v_params + row * 2, tokens * 8, bar);
+    };
     auto issue = [&](int slot) {
       const uint32_t stage = ring + slot * L::kStageBytes, bar = bars + 8 * slot;
-      const int halves = a.page_shift >= 5 ? 1 : 2, tokens = kTile / halves;
-      uint32_t bytes = 0;
-      int64_t row[2];
+      const int tok = pt * kTile, in_page = tok & ((1 << a.page_shift) - 1);
       missing &= ~(3u << (2 * slot));
-      for (int i = 0; i < halves; ++i) {
-        const int tok = pt * kTile + i * tokens;
-        if (tok >= plen) break;
-        const int index = tok >> a.page_shift;
-        if (index < window || index >= window + 32) {
-          window = index;
-          entry = static_cast<int64_t>(index + lane) << a.page_shift < plen
-                      ? __ldg(a.table + static_cast<int64_t>(pb) * a.ld_table + index + lane) : 0;
+      if (a.page_shift >= 5) {
+        if (turn || in_page == 0) page_row = tok < plen ? find_page(tok) : -1;
+        turn = false;
+        if (page_row < 0) missing |= 3u << (2 * slot);
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar, page_row < 0 ? 0 : kTile * (D + 16));
+          if (page_row >= 0) copy(stage, bar, 0, kTile, page_row + in_page);
         }
-        const int page = __shfl_sync(kAllLanes, entry, index - window);
-        if (page < 0 || page >= a.pages) {
-          missing |= (halves == 1 ? 3u : 1u << i) << (2 * slot);
-          if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-          row[i] = -1;
-        } else {
-          row[i] = ((static_cast<int64_t>(page) * a.H + ph) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
-          bytes += tokens * (D + 16);
-        }
-      }
-      if (lane == 0) {
-        mbar_arrive_expect_tx(bar, bytes);
-        for (int i = 0; i < halves; ++i) {
-          const int tok = i * tokens;
-          if (pt * kTile + tok >= plen) break;
-          if (row[i] < 0) continue;
-          bulk_load(stage + tok * (D / 2), a.k_codes + row[i] * (D / 2), tokens * (D / 2), bar);
-          bulk_load(stage + L::kCodeBytes + tok * (D / 2), a.v_codes + row[i] * (D / 2), tokens * (D / 2), bar);
-          bulk_load(stage + 2 * L::kCodeBytes + tok * 8, a.k_params + row[i] * 2, tokens * 8, bar);
-          bulk_load(stage + 2 * L::kCodeBytes + kTile * 8 + tok * 8, a.v_params + row[i] * 2, tokens * 8, bar);
+      } else {  // two pages of 16 tokens
+        const int64_t r0 = tok < plen ? find_page(tok) : -1, r1 = tok + 16 < plen ? find_page(tok + 16) : -1;
+        missing |= ((r0 < 0 ? 1u : 0u) | (r1 < 0 ? 2u : 0u)) << (2 * slot);
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar, (r0 < 0 ? 0 : 16 * (D + 16)) + (r1 < 0 ? 0 : 16 * (D + 16)));
+          if (r0 >= 0) copy(stage, bar, 0, 16, r0);
+          if (r1 >= 0) copy(stage, bar, 16, 16, r1);
         }
       }
       if (--ahead > 0 && ++pt == pstages) {
         pt = 0;
+        turn = true;
         if (++ph == a.H) {
           ph = 0;
+          window = -64;
           PagedSeq n;
           do {
             n = paged_seq(a, ++pb);
             pstages = stages_of(a, n);
           } while (pstages == 0);
           plen = n.len;
-          window = -64;
         }
       }
     };
@@ -378,65 +391,75 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
       const uint32_t gone = missing >> (2 * slot) & 3u;
 
       // Scores of 32 tokens: rows g and g + 8 of each 16, columns 2c and 2c + 1 of each 8 query rows.
-      float z[2][NT][4];
+      float acc[2][NT][4] = {}, p[2][NT][4], pv[2][NT][4];
+      float sk[2][2], bk[2][2], sv[2][2], ov[2][2];   // [half][row]: z = sk acc + bk Q; value scale and offset
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const uint32_t at = stage + (half * 16 + tok_k) * (D / 2) + c * (D / 8);
         const Words<kKw> k0 = lds<kKw>(at), k1 = lds<kKw>(at + 8 * (D / 2));
-        float acc[2][NT][4] = {};
 #pragma unroll
         for (int i = 0; i < kKw; ++i) {
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const uint32_t f[4] = {widen<kHalf>(k0.w[i], 2 * p), widen<kHalf>(k1.w[i], 2 * p),
-                                   widen<kHalf>(k0.w[i], 2 * p + 1), widen<kHalf>(k1.w[i], 2 * p + 1)};
+          for (int n = 0; n < 4; n += 2) {
+            const uint32_t f[4] = {widen<kHalf>(k0.w[i], n), widen<kHalf>(k1.w[i], n), widen<kHalf>(k0.w[i], n + 1),
+                                   widen<kHalf>(k1.w[i], n + 1)};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816(acc[p][nt], f, qf[nt][4 * i + 2 * p], qf[nt][4 * i + 2 * p + 1], kHalf);
+            for (int nt = 0; nt < NT; ++nt) mma16816(acc[half][nt], f, qf[nt][4 * i + n], qf[nt][4 * i + n + 1], kHalf);
           }
         }
         const uint32_t par = stage + 2 * L::kCodeBytes + (half * 16 + tok_k) * 8;
-        const Words<2> p0 = lds<2>(par), p1 = lds<2>(par + 64);
-        const float s0 = __uint_as_float(p0.w[0]) * sc, s1 = __uint_as_float(p1.w[0]) * sc;
-        const float b0 = fmaf(-kBias, s0, __uint_as_float(p0.w[1]) * sc), b1 = fmaf(-kBias, s1, __uint_as_float(p1.w[1]) * sc);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int i = 0; i < 2; ++i) {
+          const Words<2> k = lds<2>(par + 64 * i), v = lds<2>(par + kTile * 8 + 64 * i);
+          sk[half][i] = __uint_as_float(k.w[0]) * sc;
+          bk[half][i] = fmaf(-kBias, sk[half][i], __uint_as_float(k.w[1]) * sc);
+          sv[half][i] = __uint_as_float(v.w[0]);
+          ov[half][i] = __uint_as_float(v.w[1]);
+        }
+      }
+      bool redo = (t + 1) * kTile > sees_least || gone != 0;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            z[half][nt][j] = fmaf(s0, acc[0][nt][j] + acc[1][nt][j], b0 * qs[nt][j]);
-            z[half][nt][2 + j] = fmaf(s1, acc[0][nt][2 + j] + acc[1][nt][2 + j], b1 * qs[nt][j]);
+      for (int nt = 0; nt < NT; ++nt) {
+        float top = -INFINITY, most = 0.f;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x = fmaf(sk[half][k >> 1], acc[half][nt][k], fmaf(bk[half][k >> 1], qs[nt][k & 1], -m[nt][k & 1]));
+            top = fmaxf(top, x);
+            p[half][nt][k] = ex2(x);
+            pv[half][nt][k] = p[half][nt][k] * sv[half][k >> 1];
+            most = fmaxf(most, pv[half][nt][k]);
           }
-        }
+        redo |= !(top <= 32.f) || !(most <= 256.f);
       }
-      const bool whole = (t + 1) * kTile <= sees_least && gone == 0;
-      if (!whole) {
+      if (__any_sync(kAllLanes, redo)) {
+        float lift[2][2];
+        bool none[2][2];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int tok = t * kTile + half * 16 + tok_k;
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              if (tok >= sees[nt][j] || (gone >> half & 1u)) z[half][nt][j] = -INFINITY;
-              if (tok + 8 >= sees[nt][j] || (gone >> half & 1u)) z[half][nt][2 + j] = -INFINITY;
-            }
-        }
-      }
-
-      bool higher = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float top = fmaxf(fmaxf(z[0][nt][j], z[0][nt][2 + j]), fmaxf(z[1][nt][j], z[1][nt][2 + j]));
-          higher |= top > m[nt][j] + kLazy;
-        }
-      if (__any_sync(kAllLanes, higher)) {
+          for (int i = 0; i < 2; ++i) {  // what nobody sees may hold anything
+            none[half][i] = t * kTile + half * 16 + tok_k + 8 * i >= s.len || (gone >> half & 1u);
+            if (none[half][i]) sv[half][i] = ov[half][i] = 0.f;
+            lift[half][i] = fmaxf(__log2f(sv[half][i]), -24.f);
+          }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float keep[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float top = fmaxf(fmaxf(z[0][nt][j], z[0][nt][2 + j]), fmaxf(z[1][nt][j], z[1][nt][2 + j]));
+            float top = -INFINITY;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int k = 2 * i + j;
+                float z = fmaf(sk[half][i], acc[half][nt][k], bk[half][i] * qs[nt][j]);
+                if (none[half][i] || t * kTile + half * 16 + tok_k + 8 * i >= sees[nt][j]) z = -INFINITY;
+                acc[half][nt][k] = z;
+                top = fmaxf(top, z + lift[half][i]);
+              }
 #pragma unroll
             for (int k = 4; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, k));
             top = fmaxf(top, m[nt][j]);
@@ -444,6 +467,15 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             m[nt][j] = top;
             l[nt][j] *= keep[j];
             w[nt][j] *= keep[j];
+            const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int k = 2 * i + j;
+                p[half][nt][k] = ex2(acc[half][nt][k] - ref);
+                pv[half][nt][k] = p[half][nt][k] * sv[half][i];
+              }
           }
 #pragma unroll
           for (int mt = 0; mt < kMt; ++mt) {
@@ -455,40 +487,19 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         }
       }
 
-      // Weights, their sums, and O^T += V^T P^T.
+      // Sums, and O^T += V^T P^T.
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const uint32_t par = stage + 2 * L::kCodeBytes + kTile * 8 + (half * 16 + tok_k) * 8;
-        const Words<2> p0 = lds<2>(par), p1 = lds<2>(par + 64);
-        float s0 = __uint_as_float(p0.w[0]), s1 = __uint_as_float(p1.w[0]);
-        float b0 = __uint_as_float(p0.w[1]), b1 = __uint_as_float(p1.w[1]);
-        if (!whole) {  // what no query sees may hold anything
-          const int tok = t * kTile + half * 16 + tok_k;
-          const bool out = gone >> half & 1u;
-          if (tok >= s.len || out) s0 = b0 = 0.f;
-          if (tok + 8 >= s.len || out) s1 = b1 = 0.f;
-        }
-        uint32_t hi[NT][2], low[NT][2];
+        uint32_t pt0[NT], pt1[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float pv[4];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float mm = m[nt][j] == -INFINITY ? 0.f : m[nt][j];
-            const float pa = ex2(z[half][nt][j] - mm), pb2 = ex2(z[half][nt][2 + j] - mm);
-            l[nt][j] += pa + pb2;
-            w[nt][j] = fmaf(pa, b0, fmaf(pb2, b1, w[nt][j]));
-            pv[j] = pa * s0;
-            pv[2 + j] = pb2 * s1;
+          for (int k = 0; k < 4; ++k) {
+            l[nt][k & 1] += p[half][nt][k];
+            w[nt][k & 1] = fmaf(p[half][nt][k], ov[half][k >> 1], w[nt][k & 1]);
           }
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t x = pack_bf16(pv[2 * i], pv[2 * i + 1]);
-            hi[nt][i] = transpose8x8(x);
-            if constexpr (kHalf)
-              low[nt][i] = transpose8x8(pack_bf16(pv[2 * i] - __uint_as_float(x << 16),
-                                                  pv[2 * i + 1] - __uint_as_float(x & 0xFFFF0000u)));
-          }
+          pt0[nt] = transpose8x8(pack_f16(pv[half][nt][0], pv[half][nt][1]));
+          pt1[nt] = transpose8x8(pack_f16(pv[half][nt][2], pv[half][nt][3]));
         }
         const uint32_t at = stage + L::kCodeBytes + half * 16 * (D / 2) + g * (D / 16);
         const Words<kVw> va = lds<kVw>(at + tok_v0 * (D / 2)), vb = lds<kVw>(at + tok_v1 * (D / 2));
@@ -500,14 +511,13 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             const uint32_t x = __byte_perm(va.w[i], vb.w[i], part ? 0x7632 : 0x5410);
             const uint32_t y = __byte_perm(vc.w[i], vd.w[i], part ? 0x7632 : 0x5410);
 #pragma unroll
-            for (int n = 0; n < 4; n += 2) {
-              const uint32_t f[4] = {widen_signed(x, n), widen_signed(x, n + 1), widen_signed(y, n), widen_signed(y, n + 1)};
-              const int mt = 4 * i + 2 * part + n / 2;
+            for (int n = 0; n < 2; ++n) {
+              uint32_t f[4];
+              widen_signed(n ? x >> 8 : x, f[0], f[1]);
+              widen_signed(n ? y >> 8 : y, f[2], f[3]);
+              const int mt = 4 * i + 2 * part + n;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                mma16816(o[nt][mt], f, hi[nt][0], hi[nt][1], false);
-                if constexpr (kHalf) mma16816(o[nt][mt], f, low[nt][0], low[nt][1], false);
-              }
+              for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][mt], f, pt0[nt], pt1[nt], true);
             }
           }
         }

@@ -161,12 +161,12 @@ def _ptr(t: Optional[torch.Tensor]):
         return None
     if not t.is_cuda:
         raise ValueError("tensors passed to liboffq must live on a CUDA device")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+def _stream(stream):
+    if stream is None:  # the current stream's handle, without an object around it (3 us of a 20 us call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
@@ -748,14 +748,15 @@ def offq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: 
 def _heads(x: torch.Tensor) -> Tuple[int, int, int, int]:
     """(T, H, hd, ld_token) of x [T, H, hd] with contiguous heads."""
     T, H, hd = x.shape
-    if x.stride(2) != 1 or (H > 1 and x.stride(1) != hd):
+    ld, between, inner = x.stride()
+    if inner != 1 or (H > 1 and between != hd):
         raise ValueError("heads of a token must be contiguous")
-    return T, H, hd, x.stride(0) if T > 1 else max(x.stride(0), H * hd)
+    return T, H, hd, ld if T > 1 else max(ld, H * hd)
 
 
-def _like(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape) -> None:
+def _like(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple) -> None:
     """t is a contiguous tensor of that type and shape, or None."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+    if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
 
 
@@ -763,21 +764,22 @@ def _rotary(positions, table, T):
     """(max_pos, rot_dim) of a rotary table, (0, 0) without one."""
     if table is None:
         return 0, 0
-    _like("positions", positions, torch.int32, (T,))
     if positions is None or table.dim() != 2:
         raise ValueError("a rotary table [max_pos, rot_dim] goes with positions [T]")
+    _like("positions", positions, torch.int32, (T,))
     _like("table", table, torch.float32, table.shape)
     return table.shape
 
 
 def _cache_shape(cache: KV4Cache, H: Optional[int], hd: Optional[int]):
-    pages, heads, page_size, half = cache.k_codes.shape
+    kc, kp, vc, vp = cache
+    pages, heads, page_size, half = shape = kc.shape
     if (H is not None and heads != H) or (hd is not None and 2 * half != hd):
         raise ValueError(f"the cache holds {heads} heads of {2 * half}")
-    for t in (cache.k_codes, cache.v_codes):
-        _like("cache codes", t, torch.uint8, (pages, heads, page_size, half))
-    for t in (cache.k_params, cache.v_params):
-        _like("cache params", t, torch.float32, (pages, heads, page_size, 2))
+    _like("cache codes", kc, torch.uint8, shape)
+    _like("cache codes", vc, torch.uint8, shape)
+    _like("cache params", kp, torch.float32, (pages, heads, page_size, 2))
+    _like("cache params", vp, torch.float32, (pages, heads, page_size, 2))
     return pages, heads, page_size, 2 * half
 
 
@@ -788,12 +790,15 @@ def rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor] = None, table:
     T, H, hd, ld = _heads(x)
     max_pos, rot = _rotary(positions, table, T)
     _like("norm", norm, torch.float32, (H, hd))
+    ld_out = H * hd
     if out is None:
         out = torch.empty((T, H, hd), dtype=out_dtype or x.dtype, device=x.device)
     elif out.shape != x.shape:
         raise ValueError("out has x's shape")
+    else:
+        ld_out = _heads(out)[3]
     flags = (OFFQ_ROTATE if rotate else 0) | (OFFQ_INTERLEAVED if interleaved else 0)
-    offq_rope_heads(x, T, H, hd, ld, positions, table, max_pos, rot, norm, eps, flags, out, _heads(out)[3], stream)
+    offq_rope_heads(x, T, H, hd, ld, positions, table, max_pos, rot, norm, eps, flags, out, ld_out, stream)
     return out
 
 
@@ -832,8 +837,8 @@ def kv4_paged_read(cache: KV4Cache, slots: torch.Tensor, rotate: bool = True, ro
     pages, H, page_size, hd = _cache_shape(cache, None, None)
     T = slots.shape[0]
     _like("slots", slots, torch.int64, (T,))
-    kv = torch.empty((2, T, H, hd), dtype=out_dtype, device=slots.device)
-    k, v = kv[0], kv[1]
+    k = torch.empty((T, H, hd), dtype=out_dtype, device=slots.device)
+    v = torch.empty((T, H, hd), dtype=out_dtype, device=slots.device)
     flags = (OFFQ_ROTATE if rotate else 0) | (OFFQ_ROTATE_V if rotate_v else 0)
     offq_kv4_paged_read(cache, pages, page_size, H, hd, slots, T, flags, k, v, _dtype_code(k), H * hd, H * hd, stream)
     return k, v
@@ -849,20 +854,27 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
     B = lens.shape[0]
     _like("lens", lens, torch.int32, (B,))
     _like("cu_q", cu_q, torch.int32, (B + 1,))
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or             (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+    if block_table.dim() != 2:
         raise ValueError("block_table must be int32 [B, width] with contiguous rows")
+    listed, width = block_table.shape
+    ld_table, inner = block_table.stride()
+    if block_table.dtype is not torch.int32 or listed != B or (width > 1 and inner != 1):
+        raise ValueError("block_table must be int32 [B, width] with contiguous rows")
+    ld_out = Hq * hd
     if out is None:
         out = torch.empty((Tq, Hq, hd), dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out has q's shape and type")
+    else:
+        ld_out = _heads(out)[3]
     need = paged_attention_workspace(Tq, Hq, H, hd, B, max_q)
     if workspace is None and need > 0:
         workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
     stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
-    ld_table = block_table.stride(0) if B > 1 else block_table.shape[1]
-    offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table, ld_table, lens, cu_q, B, max_q,
-                         scale if scale is not None else hd ** -0.5, out, _heads(out)[3], stats, workspace,
-                         workspace.numel() * workspace.element_size() if workspace is not None else 0, stream)
+    offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table,
+                         ld_table if B > 1 else width, lens, cu_q, B, max_q,
+                         scale if scale is not None else hd ** -0.5, out, ld_out, stats, workspace,
+                         workspace.nbytes if workspace is not None else 0, stream)
     return (out, stats) if lse else out
 
 
@@ -874,12 +886,15 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
     Tk, H, hk, ld_k = _heads(k)
     if (Tk, hk) != (T, hd) or v.shape != k.shape or k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("queries, keys and values have the same tokens, head size and type")
-    _like("cu", cu, torch.int32, (cu.shape[0],))
+    _like("cu", cu, torch.int32, cu.shape[:1])
+    ld_out = Hq * hd
     if out is None:
         out = torch.empty((T, Hq, hd), dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out has q's shape and type")
+    else:
+        ld_out = _heads(out)[3]
     stats = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if lse else None
     offq_prompt_attention(q, k, v, T, Hq, H, hd, ld_q, ld_k, _heads(v)[3], cu, cu.shape[0] - 1,
-                          scale if scale is not None else hd ** -0.5, causal, out, _heads(out)[3], stats, stream)
+                          scale if scale is not None else hd ** -0.5, causal, out, ld_out, stats, stream)
     return (out, stats) if lse else out
