@@ -374,10 +374,10 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             qs[nt][j] = __shfl_sync(kAllLanes, sum, 4 * (2 * c + j));
-            m[nt][j] = -INFINITY;
             l[nt][j] = w[nt][j] = 0.f;
             const int rr = 8 * nt + 2 * c + j;
             sees[nt][j] = rr < rows ? max(0, min(s.len, s.len - s.n + rr / a.G + 1)) : 0;
+            m[nt][j] = sees[nt][j] > 0 ? -INFINITY : 0.f;  // a row without keys has no maximum to wait for
           }
 #pragma unroll
           for (int mt = 0; mt < kMt; ++mt)
