@@ -35,11 +35,12 @@ using namespace offq;
 
 constexpr int kTile = 32;   // tokens per stage
 constexpr float kBias = 24.0f;
+constexpr int kLeastStages = 8;   // of a CTA
 
 template <int D, int NT>
 struct FewLayout {
-  static constexpr int kWarps = NT == 1 ? 12 : 8;   // as many as registers and rings allow
-  static constexpr int kStages = NT == 1 ? 3 : 4;
+  static constexpr int kWarps = NT == 1 ? 16 : 8;   // as many as registers allow
+  static constexpr int kStages = NT == 1 ? 2 : 4;
   static constexpr int kCodeBytes = kTile * D / 2;
   static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kTile * 8;
   static constexpr int kRows = 8 * NT;
@@ -48,7 +49,7 @@ struct FewLayout {
   static constexpr int kPartBytes = kPartFloats * 4;
   static constexpr int kPartOff = kWarps * kRing;                // the warps' first parts
   static constexpr int kCtrlOff = kPartOff + kWarps * kPartBytes;
-  static constexpr int kBytes = kCtrlOff + 1024;
+  static constexpr int kBytes = kCtrlOff + 2048;
   static_assert(kPartBytes <= kRing, "a part fits into its warp's ring");
   static_assert(kBytes <= 232448, "shared memory");
 };
@@ -140,9 +141,10 @@ __device__ __forceinline__ int stages_of(const AttnArgs& a, const PagedSeq& s) {
   return max(1, (s.len + kTile - 1) / kTile);
 }
 
-// Header of a part that crosses CTAs: b < 0 for none; `ends` where it reaches its sequence's last stage.
+// Header of a part that crosses CTAs: its head's (sequence, head) as one number, negative for none, whether it reaches
+// its sequence's last stage, and the sequence's first query row and rows per key head.
 struct PartHead {
-  int b, h, ends, pad;
+  int id, ends, first, rows;
 };
 
 // The workspace: per CTA two headers (a part begun by an earlier CTA, a part left to later ones), then their
@@ -220,8 +222,8 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   long long total = 0;
 #pragma unroll
   for (int i = 0; i < L::kWarps; ++i) total += ctrl->scan[i];
-  // Less work than CTAs: the first ones take a stage each, so that parts of a head lie in neighbouring CTAs.
-  const long long ctas = min(total, static_cast<long long>(gridDim.x));
+  // Little work goes to fewer CTAs, some stages each: their warps take them at once, and joining inside a CTA is cheaper.
+  const long long ctas = min((total + kLeastStages - 1) / kLeastStages, static_cast<long long>(gridDim.x));
   const long long lo = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
   const long long hi = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
   PartHead* heads = part_head<D, NT>(a.workspace, blockIdx.x, 0);
@@ -589,34 +591,31 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   }
 
   // Parts of the same head, in order of their stages, into one: an output where they are all of it, else a part
-  // for the joining kernel.
+  // for the joining kernel. Each warp looks at all of them at once, a lane a part.
   __syncthreads();
+  constexpr int kParts = 2 * L::kWarps;
+  static_assert(kParts <= 32, "a lane for each part");
+  const int4 mypart = lane < kParts ? ctrl->part[lane] : make_int4(-1, 0, 0, 0);
+  const int my_id = mypart.x < 0 ? -1 : mypart.x * a.H + mypart.y;
+  uint32_t left = __ballot_sync(kAllLanes, my_id >= 0);
   bool have0 = false, have1 = false;
-  for (int i = 0; i < 2 * L::kWarps;) {
-    const int4 p = ctrl->part[i];
-    if (p.x < 0) {
-      ++i;
-      continue;
-    }
-    int end = i + 1, last = p.w;
-    for (int k = i + 1; k < 2 * L::kWarps; ++k) {
-      const int4 n = ctrl->part[k];
-      if (n.x < 0) continue;
-      if (n.x != p.x || n.y != p.y) break;
-      end = k + 1;
-      last = n.w;
-    }
-    const bool complete = p.z == 0 && last < 0;
-    const int which = p.z == 0 ? 1 : 0;
+  while (left != 0) {
+    const int i = __ffs(left) - 1;
+    const int id = __shfl_sync(kAllLanes, my_id, i), b = __shfl_sync(kAllLanes, mypart.x, i);
+    const uint32_t same = __ballot_sync(kAllLanes, my_id == id);
+    const int begins = __shfl_sync(kAllLanes, mypart.z, i), last = __shfl_sync(kAllLanes, mypart.w, 31 - __clz(same));
+    left &= ~same;
+    const bool complete = begins == 0 && last < 0;
+    const int which = begins == 0 ? 1 : 0, h = id - b * a.H;
     float* dst = part_sums<D, NT>(a.workspace, gridDim.x, blockIdx.x, which);
+    const PagedSeq s = paged_seq(a, b);
     if (!complete) (which ? have1 : have0) = true;
-    if (!complete && tid == 0) heads[which] = PartHead{p.x, p.y, last < 0, 0};
-    const PagedSeq s = paged_seq(a, p.x);
+    if (!complete && tid == 0) heads[which] = PartHead{id, last < 0, s.first, s.n * a.G};
     for (int u = tid; u < L::kRows * (D / 8); u += kThreads) {
       const int r = u / (D / 8), d = u % (D / 8) * 8;
       float top = -INFINITY, sum = 0.f, v[8] = {};
-      for (int k = i; k < end; ++k) {
-        if (ctrl->part[k].x < 0) continue;
+      for (uint32_t rest = same; rest != 0; rest &= rest - 1) {
+        const int k = __ffs(rest) - 1;
         const float* src = reinterpret_cast<const float*>(k & 1 ? smem + (k >> 1) * L::kRing
                                                                 : smem + L::kPartOff + (k >> 1) * L::kPartBytes);
         const float mk = src[L::kRows * D + r], next = fmaxf(top, mk);
@@ -631,8 +630,8 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
           const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= inv;
-          write_out8<D, T>(a, s.first, p.y, r, d, v);
-          if (d == 0) write_lse(a, s.first, p.y, r, top, sum);
+          write_out8<D, T>(a, s.first, h, r, d, v);
+          if (d == 0) write_lse(a, s.first, h, r, top, sum);
         }
       } else {
         reinterpret_cast<float4*>(dst + r * D + d)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -643,7 +642,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         }
       }
     }
-    i = end;
+    __syncwarp();
   }
   if (tid == 0) {
     if (!have0) heads[0] = PartHead{-1, 0, 0, 0};
@@ -660,47 +659,76 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int c
   if (tid == 0) s_last = 0x7FFFFFFF;
   griddep_wait();
   griddep_launch_dependents();
+  // This CTA's last part and the first parts of all CTAs after it, in one go.
   const PartHead p = *part_head<D, NT>(a.workspace, cta, 1);
-  if (p.b < 0) return;
+  PartHead n = {-1, 0, 0, 0};
+  const int k = cta + 1 + tid;
+  if (k < ctas) n = *part_head<D, NT>(a.workspace, k, 0);
   __syncthreads();
-  for (int k = cta + 1 + tid; k < ctas; k += blockDim.x) {
-    const PartHead n = *part_head<D, NT>(a.workspace, k, 0);
-    if (n.b == p.b && n.h == p.h && n.ends) atomicMin(&s_last, k);
+  if (p.id < 0) return;
+  if (n.id == p.id && n.ends) atomicMin(&s_last, k);
+  for (int far = k + blockDim.x; far < ctas; far += blockDim.x) {
+    n = *part_head<D, NT>(a.workspace, far, 0);
+    if (n.id == p.id && n.ends) atomicMin(&s_last, far);
   }
   __syncthreads();
   const int last = s_last;
   if (last >= ctas) return;  // a CTA gave up: the status word says so
-  const PagedSeq s = paged_seq(a, p.b);
-  const int rows = s.n * a.G;
+  const int rows = p.rows, h = p.id % a.H;
   for (int u = tid; u < rows * (D / 8); u += blockDim.x) {
     const int r = u / (D / 8), d = u % (D / 8) * 8;
     float top = -INFINITY, sum = 0.f, v[8] = {};
-#pragma unroll 4
-    for (int k = cta; k <= last; ++k) {
-      const float* src = part_sums<D, NT>(a.workspace, ctas, k, k == cta ? 1 : 0);
-      const float mk = src[L::kRows * D + r], lk = src[L::kRows * D + L::kRows + r];
-      const float4 x0 = reinterpret_cast<const float4*>(src + r * D + d)[0];
-      const float4 x1 = reinterpret_cast<const float4*>(src + r * D + d)[1];
-      const float next = fmaxf(top, mk);
-      const float x = top == -INFINITY ? 0.f : ex2(top - next), y = mk == -INFINITY ? 0.f : ex2(mk - next);
-      sum = sum * x + lk * y;
-      const float n[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+    constexpr int kAtOnce = 8;  // parts whose loads are in flight together
+    for (int k0 = cta; k0 <= last; k0 += kAtOnce) {
+      float mk[kAtOnce], lk[kAtOnce];
+      float4 x0[kAtOnce], x1[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = v[e] * x + n[e] * y;
+      for (int j = 0; j < kAtOnce; ++j) {
+        mk[j] = -INFINITY;
+        lk[j] = 0.f;
+        x0[j] = x1[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k0 + j <= last) {
+          const float* src = part_sums<D, NT>(a.workspace, ctas, k0 + j, k0 + j == cta ? 1 : 0);
+          mk[j] = src[L::kRows * D + r];
+          lk[j] = src[L::kRows * D + L::kRows + r];
+          x0[j] = reinterpret_cast<const float4*>(src + r * D + d)[0];
+          x1[j] = reinterpret_cast<const float4*>(src + r * D + d)[1];
+        }
+      }
+      float next = top;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) next = fmaxf(next, mk[j]);
+      const float x = top == -INFINITY ? 0.f : ex2(top - next);
+      sum *= x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= x;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float y = mk[j] == -INFINITY ? 0.f : ex2(mk[j] - next);
+        sum = fmaf(lk[j], y, sum);
+        v[0] = fmaf(x0[j].x, y, v[0]);
+        v[1] = fmaf(x0[j].y, y, v[1]);
+        v[2] = fmaf(x0[j].z, y, v[2]);
+        v[3] = fmaf(x0[j].w, y, v[3]);
+        v[4] = fmaf(x1[j].x, y, v[4]);
+        v[5] = fmaf(x1[j].y, y, v[5]);
+        v[6] = fmaf(x1[j].z, y, v[6]);
+        v[7] = fmaf(x1[j].w, y, v[7]);
+      }
       top = next;
     }
     const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= inv;
-    write_out8<D, T>(a, s.first, p.h, r, d, v);
-    if (d == 0) write_lse(a, s.first, p.h, r, top, sum);
+    write_out8<D, T>(a, p.first, h, r, d, v);
+    if (d == 0) write_lse(a, p.first, h, r, top, sum);
   }
 }
 
 template <int D, int NT, typename T>
 int launch_few(const AttnArgs& a, cudaStream_t s) {
   using L = FewLayout<D, NT>;
-  static_assert(sizeof(FewCtrl<D, NT>) <= 1024, "control block");
+  static_assert(sizeof(FewCtrl<D, NT>) <= 2048, "control block");
   const int sms = device_sms();
   if (sms == 0 || !smem_optin<paged_few_kernel<D, NT, T>>(L::kBytes)) return OFFQ_ERR_CUDA;
   if (const int rc = launch_pdl(paged_few_kernel<D, NT, T>, dim3(sms), dim3(L::kWarps * 32), L::kBytes, s, a);
