@@ -14,8 +14,10 @@
 //   * out = (O + sum p o_v) / sum p: the values' offsets add the same to every channel.
 //   * Work is the list of (row pair tile, block) steps; the CTAs take equal shares of it, and what crosses CTAs
 //     is joined by a second kernel from at most two parts per CTA.
-// For half-precision outputs P' is a half; the reference of the exponentials then carries the largest scale of the
-// block, so that P' stays in range whatever the values' size is.
+// P' is a half, and the values q are: the reference m of the exponentials carries the largest value scale of the block,
+// so that P' stays in range whatever the values' size is. A block is weighed against the reference it meets; only
+// where some score passes it by 2^kLazy (or keys are hidden) the maxima are taken and the block weighed again: S is still
+// in tensor memory, as the weights wait in registers until the whole block is through.
 //
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 finds the CTA's work, warps
 // 12-15 widen.
@@ -119,19 +121,13 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, int n) {
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "n"(kMask), "n"(kMagic));
   return r;
 }
-template <typename T>
-__device__ __forceinline__ uint32_t widen_signed(uint32_t w, int n) {
-  const uint32_t x = widen<T>(w, n);
-  if constexpr (std::is_same<T, __half>::value) {
-    const uint32_t bias = 0x4E004E00u;  // 24.0 twice
-    const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&bias));
-    return *reinterpret_cast<const uint32_t*>(&v);
-  } else {
-    const uint32_t bias = 0x41C041C0u;
-    const __nv_bfloat162 v =
-        __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&bias));
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
+// Nibbles 0 and 1 of both halves of w as signed codes q in f16 (2 and 3 of w shifted right by 8).
+__device__ __forceinline__ void widen_signed(uint32_t w, uint32_t& even, uint32_t& odd) {
+  uint32_t x, y;
+  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x) : "r"(w));  // 1024 + u
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(y) : "r"(w));  // 1024 + 16 u
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(even) : "r"(x), "r"(0x64086408u));                        // - 1032
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(odd) : "r"(y), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
 }
 
 // Byte offset of 16-byte chunk ch (8 channels) of row r in a swizzled tile.
@@ -265,37 +261,53 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     const int par_row = row + kRowsPer * c;
     uint4 kc[kReps], vc[kReps];
     float2 kp, vp;
-    int page[kReps];
+    int page[kReps], next_page[kReps];
     uint32_t absent = 0;  // reps whose rows have no page
-    Walk at;              // the block in the registers, or the next one once its pages are being found
-    auto find_pages = [&]() {
+    Walk at;              // the block whose pages were found last
+    int head = 0, first = 0, len = 0, next_head = 0, next_first = 0, next_len = 0;  // of the block to load, and after it
+    auto find_pages = [&]() {  // of block `at`
+      next_head = at.h;
+      next_first = at.blk * kKt;
+      next_len = at.s.len;
 #pragma unroll
       for (int i = 0; i < kReps; ++i) {
-        const int tok = at.blk * kKt + kRowsPer * i + (row & ~7);
-        page[i] = tok < at.s.len ? __ldg(a.table + static_cast<int64_t>(at.b) * a.ld_table + (tok >> a.page_shift)) : -1;
+        const int tok = next_first + kRowsPer * i + (row & ~7);
+        next_page[i] = tok < next_len ? __ldg(a.table + static_cast<int64_t>(at.b) * a.ld_table + (tok >> a.page_shift)) : -1;
       }
     };
-    auto slot_of = [&](int i, int tok) {
-      return ((static_cast<int64_t>(page[i]) * a.H + at.h) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
+    auto take_pages = [&]() {
+      head = next_head;
+      first = next_first;
+      len = next_len;
+#pragma unroll
+      for (int i = 0; i < kReps; ++i) page[i] = next_page[i];
+    };
+    auto step = [&]() {
+      if (++at.blk == at.blocks) at.next_tile(a);
+      find_pages();
+    };
+    auto slot_of = [&](int i) {
+      const int tok = first + kRowsPer * i + row;
+      return ((static_cast<int64_t>(page[i]) * a.H + head) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
     };
     auto load_keys = [&]() {  // and both parameters
       absent = 0;
       kp = vp = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kReps; ++i) {
-        const int tok = at.blk * kKt + kRowsPer * i + row;
+        const int tok = first + kRowsPer * i + row;
         kc[i] = make_uint4(0u, 0u, 0u, 0u);
         if (page[i] < 0 || page[i] >= a.pages) {
           page[i] = -1;
-          if ((tok & ~7) < at.s.len) {
+          if ((tok & ~7) < len) {
             absent |= 1u << i;
             *a.status = OFFQ_ERR_INVALID_ARG;
           }
           continue;
         }
-        const int64_t r = slot_of(i, tok);
+        const int64_t r = slot_of(i);
         kc[i] = __ldg(reinterpret_cast<const uint4*>(a.k_codes + r * (D / 2)) + c);
-        if (i == c && tok < at.s.len) {
+        if (i == c && tok < len) {
           kp = __ldg(reinterpret_cast<const float2*>(a.k_params) + r);
           vp = __ldg(reinterpret_cast<const float2*>(a.v_params) + r);
         }
@@ -306,23 +318,22 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       for (int i = 0; i < kReps; ++i) {
         vc[i] = make_uint4(0u, 0u, 0u, 0u);
         if (page[i] >= 0)
-          vc[i] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + slot_of(i, at.blk * kKt + kRowsPer * i + row) * (D / 2)) + c);
+          vc[i] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + slot_of(i) * (D / 2)) + c);
       }
     };
     const float sc = a.scale * kLog2e;
     if (count > 0) {
       at.start(a, ctrl);
       find_pages();
+      take_pages();
       load_keys();
       load_values();
+      if (count > 1) step();
     }
     for (int gb = 0; gb < count; ++gb) {
       const int slot = gb & 1;
       const bool more = gb + 1 < count;
-      if (more) {
-        if (++at.blk == at.blocks) at.next_tile(a);
-        find_pages();
-      }
+      if (more) take_pages();
       if (gb >= 2 && !wait(&ctrl->k_empty[slot], (gb >> 1) - 1)) break;
       const uint32_t kt = base + L::kKeys + slot * L::kTileBytes, vt = base + L::kValues + slot * L::kTileBytes;
       // Words in an order that spreads a warp's 16-byte stores over all banks.
@@ -332,10 +343,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t to = tile + tile_off(row + kRowsPer * i, 4 * c + (k ^ (swap ? 2 : 0)));
-          if (is_v)
-            sts128(to, widen_signed<T>(wd[k], 0), widen_signed<T>(wd[k], 1), widen_signed<T>(wd[k], 2), widen_signed<T>(wd[k], 3));
-          else
+          if (is_v) {
+            uint32_t q[4];
+            widen_signed(wd[k], q[0], q[1]);
+            widen_signed(wd[k] >> 8, q[2], q[3]);
+            sts128(to, q[0], q[1], q[2], q[3]);
+          } else {
             sts128(to, widen<T>(wd[k], 0), widen<T>(wd[k], 1), widen<T>(wd[k], 2), widen<T>(wd[k], 3));
+          }
         }
       };
 #pragma unroll
@@ -348,12 +363,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
         pv[0] = vp.x;
         pv[2] = vp.y;
       }
-      if constexpr (kHalf) {
-        float top = vp.x;
+      float top = vp.x;
 #pragma unroll
-        for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, m));
-        if (lane == 0) ctrl->smax[slot][w] = top;
-      }
+      for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, m));
+      if (lane == 0) ctrl->smax[slot][w] = top;
       if (lane % (8 * kChunks) == 0) {
 #pragma unroll
         for (int i = 0; i < kReps; ++i) ctrl->missing[slot][(kRowsPer * i + row) >> 3] = absent >> i & 1u;
@@ -362,6 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctrl->k_full[slot]));
       if (more) load_keys();
+      if (gb + 2 < count) step();
       if (gb >= 2 && !wait(&ctrl->v_empty[slot], (gb >> 1) - 1)) break;
 #pragma unroll
       for (int i = 0; i < kReps; ++i) widened(vt, vc[i], i, true);
@@ -374,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     fewer_registers<kIssueRegs>();
     if (warp == 8 && count > 0) {
       // ---- Products. The whole warp runs the loop; an elected lane issues ----
-      constexpr uint32_t kIdescS = idesc_16<T>(128, kKt, false), kIdescO = idesc_16<T>(128, D, true);
+      constexpr uint32_t kIdescS = idesc_16<T>(128, kKt, false), kIdescO = idesc_16<__half>(128, D, true);
       Walk w;
       w.start(a, ctrl);
       int gb = 0, left = count, nq[2] = {0, 0}, np[2] = {0, 0};
@@ -452,8 +466,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
         const int row0 = w.p * kPairRows + i * kQt + quad * 32;   // of this warp
         const bool active = w.p * kPairRows + i * kQt < rows;
         float m[4], qs[4];
-        uint64_t l2[4], w2[4];
-        int sees[4], least = 0;
+        float l[4], off[4];
+        int least = 0;
         if (active) {
           // This warp's query rows, in the widened channel order, and their sums.
           constexpr int kCh = D / 8, kPer = 32 / kCh;
@@ -490,9 +504,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           for (int x = 0; x < 4; ++x) {
             const int r = 8 * x + g, gr = row0 + r;   // x = 2 hh + ii
             qs[x] = sums[r];
-            m[x] = -INFINITY;
-            l2[x] = w2[x] = 0;
-            sees[x] = min(w.s.len, max(0, w.s.len - w.s.n + gr / a.G + 1));
+            l[x] = off[x] = 0.f;
+            m[x] = w.s.len - w.s.n + gr / a.G + 1 > 0 ? -INFINITY : 0.f;  // a row without keys has no maximum to wait for
           }
         }
         for (int j = 0; j < nb; ++j, ++gb) {
@@ -502,69 +515,96 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           if (!ok) break;
           if (active) {
             tc_fence_after();
-            uint32_t s[128];
-            tmem_ld_fragments(s_tm, s);
             const uint32_t pk = base + L::kParK + slot * 1024 + c * 16, pv = base + L::kParV + slot * 1024 + c * 16;
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float4 p = lds128f(pk + k * 64);
-              const uint64_t a2 = pack2(p.x, p.y), b2 = pack2(p.z, p.w);
-#pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                const int e = 64 * (x >> 1) + 4 * k + 2 * (x & 1);
-                float z0, z1;
-                unpack2(fma2v(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), a2, mul2v(b2, pack2(qs[x], qs[x]))), z0, z1);
-                s[e] = __float_as_uint(z0);
-                s[e + 1] = __float_as_uint(z1);
-              }
-            }
             const int key0 = (w.blk + j) * kKt;
             const uint4 gone = *reinterpret_cast<const uint4*>(ctrl->missing[slot]);
-            if (key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u) {
+            const float4 sm = *reinterpret_cast<const float4*>(ctrl->smax[slot]);
+            // log2 of the block's largest value scale, rounded up: weights times scales stay below 2^kLazy.
+            const float big = fmaxf(fmaxf(sm.x, sm.y), fmaxf(sm.z, sm.w));
+            const float lift = static_cast<float>(min(64, max(-24, static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
+            const bool masked = key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u;
+            int sees[4] = {0, 0, 0, 0};
+            if (masked) {
 #pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const uint32_t word = k < 4 ? gone.x : k < 8 ? gone.y : k < 12 ? gone.z : gone.w;
-                const bool out = (word >> (8 * (k & 3)) & 0xFFu) != 0u;
+              for (int x = 0; x < 4; ++x) sees[x] = min(w.s.len, w.s.len - w.s.n + (row0 + 8 * x + g) / a.G + 1);
+            }
+            auto hidden = [&](int k, int e, int x) {  // element e of rep k of row x
+              if (!masked) return false;
+              const uint32_t word = k < 4 ? gone.x : k < 8 ? gone.y : k < 12 ? gone.z : gone.w;
+              return (word >> (8 * (k & 3)) & 0xFFu) != 0u || key0 + 8 * k + 2 * c + e >= sees[x];
+            };
+            // Scores relative to m, weights and sums of the whole block; the largest relative score.
+            uint32_t p[2][2][16];
+            uint64_t lb[4], wb[4];
+            auto weigh = [&](auto with_mask) {
+              uint64_t m2[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                  for (int e = 0; e < 2; ++e)
-                    if (out || key0 + 8 * k + 2 * c + e >= sees[x]) s[64 * (x >> 1) + 4 * k + 2 * (x & 1) + e] = 0xFF800000u;
+              for (int x = 0; x < 4; ++x) {
+                const float mm = m[x] == -INFINITY && with_mask ? 0.f : -m[x];
+                m2[x] = pack2(mm, mm);
+                lb[x] = wb[x] = 0;
               }
-            }
-            float top[4];
-            bool higher = false;
-            float lift = 0.f;  // log2 of the block's largest value scale, rounded up (half-precision weights)
-            if constexpr (kHalf) {
-              const float4 sm = *reinterpret_cast<const float4*>(ctrl->smax[slot]);
-              const float big = fmaxf(fmaxf(sm.x, sm.y), fmaxf(sm.z, sm.w));
-              lift = static_cast<float>(min(64, max(-24, static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
-            }
+              float top = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              top[x] = -INFINITY;
+              for (int q = 0; q < 2; ++q) {
+                uint32_t s[2][32];
+                tmem_ld_fragments_pair(s_tm + 64 * q, s[0], s[1]);
 #pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const int e = 64 * (x >> 1) + 4 * k + 2 * (x & 1);
-                top[x] = fmaxf(top[x], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                for (int k = 0; k < 8; ++k) {
+                  const float4 f = lds128f(pk + (8 * q + k) * 64), v = lds128f(pv + (8 * q + k) * 64);
+                  const uint64_t a2 = pack2(f.x, f.y), b2 = pack2(f.z, f.w), s2 = pack2(v.x, v.y), o2 = pack2(v.z, v.w);
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
+                    const uint32_t* e = &s[x >> 1][4 * k + 2 * (x & 1)];
+                    float y0, y1;
+                    unpack2(fma2v(pack2(__uint_as_float(e[0]), __uint_as_float(e[1])), a2, fma2v(b2, pack2(qs[x], qs[x]), m2[x])), y0, y1);
+                    if (with_mask) {
+                      if (hidden(8 * q + k, 0, x)) y0 = -INFINITY;
+                      if (hidden(8 * q + k, 1, x)) y1 = -INFINITY;
+                    } else {
+                      top = fmaxf(top, fmaxf(y0, y1));
+                    }
+                    const uint64_t p2 = pack2(ex2(y0), ex2(y1));
+                    lb[x] = add2_rn(lb[x], p2);
+                    wb[x] = fma2v(p2, o2, wb[x]);
+                    unpack2(mul2v(p2, s2), y0, y1);
+                    p[q][x >> 1][2 * k + (x & 1)] = pack_16<__half>(y0, y1);
+                  }
+                }
               }
-              top[x] += lift;
-              higher |= top[x] > m[x] + kLazy;
-            }
-            if (__any_sync(kAllLanes, higher)) {
-              float keep[4];
+              return top;
+            };
+            bool again = masked;
+            if (!masked) again = __any_sync(kAllLanes, !(weigh(std::false_type{}) <= kLazy - lift));
+            if (again) {  // some row's reference moves, or some keys are hidden
+              float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, keep[4];
+#pragma unroll 1
+              for (int q = 0; q < 2; ++q) {
+                uint32_t s[2][32];
+                tmem_ld_fragments_pair(s_tm + 64 * q, s[0], s[1]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const float4 f = lds128f(pk + (8 * q + k) * 64);
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
+                    const uint32_t* e = &s[x >> 1][4 * k + 2 * (x & 1)];
+                    const float z0 = fmaf(__uint_as_float(e[0]), f.x, f.z * qs[x]), z1 = fmaf(__uint_as_float(e[1]), f.y, f.w * qs[x]);
+                    if (!hidden(8 * q + k, 0, x)) top[x] = fmaxf(top[x], z0);
+                    if (!hidden(8 * q + k, 1, x)) top[x] = fmaxf(top[x], z1);
+                  }
+                }
+              }
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
                 top[x] = fmaxf(top[x], __shfl_xor_sync(kAllLanes, top[x], 1));
                 top[x] = fmaxf(top[x], __shfl_xor_sync(kAllLanes, top[x], 2));
-                top[x] = fmaxf(top[x], m[x]);
+                top[x] = fmaxf(top[x] + lift, m[x]);
                 keep[x] = m[x] == -INFINITY ? 0.f : ex2(m[x] - top[x]);
                 m[x] = top[x];
-                const uint64_t k2 = pack2(keep[x], keep[x]);
-                l2[x] = mul2v(l2[x], k2);
-                w2[x] = mul2v(w2[x], k2);
+                l[x] *= keep[x];
+                off[x] *= keep[x];
               }
-              if (j > 0) {
+              if (j > 0 && __any_sync(kAllLanes, keep[0] != 1.f || keep[1] != 1.f || keep[2] != 1.f || keep[3] != 1.f)) {
 #pragma unroll
                 for (int q = 0; q < D / 64; ++q)
 #pragma unroll
@@ -577,34 +617,20 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                     tmem_st_fragments_part(at, o);
                   }
               }
+              weigh(std::true_type{});
             }
-            uint64_t m2[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              const float mm = m[x] == -INFINITY ? 0.f : -m[x];
-              m2[x] = pack2(mm, mm);
+              float y0, y1;
+              unpack2(lb[x], y0, y1);
+              l[x] += y0 + y1;
+              unpack2(wb[x], y0, y1);
+              off[x] += y0 + y1;
             }
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-              uint32_t p[2][16];
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float4 v = lds128f(pv + (8 * q + k) * 64);
-                const uint64_t s2 = pack2(v.x, v.y), o2 = pack2(v.z, v.w);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  const int e = 64 * (x >> 1) + 4 * (8 * q + k) + 2 * (x & 1);
-                  float y0, y1;
-                  unpack2(add2_rn(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), m2[x]), y0, y1);
-                  const uint64_t p2 = pack2(ex2(y0), ex2(y1));
-                  l2[x] = add2_rn(l2[x], p2);
-                  w2[x] = fma2v(p2, o2, w2[x]);
-                  unpack2(mul2v(p2, s2), y0, y1);
-                  p[x >> 1][2 * k + (x & 1)] = pack_16<T>(y0, y1);
-                }
-              }
-              tmem_st_pairs(s_tm + 32 * q, p[0]);
-              tmem_st_pairs(s_tm + 32 * q + (16u << 16), p[1]);
+              tmem_st_pairs(s_tm + 32 * q, p[q][0]);
+              tmem_st_pairs(s_tm + 32 * q + (16u << 16), p[q][1]);
             }
             tmem_st_wait();
             tc_fence_before();
@@ -621,14 +647,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           const bool complete = w.blk == 0 && nb == w.blocks;
           const int which = w.blk == 0 ? 1 : 0;
           float* part = part_data<D>(a.workspace, gridDim.x, blockIdx.x, which);
-          float l[4], off[4], inv[4];
+          float inv[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            float y0, y1;
-            unpack2(l2[x], y0, y1);
-            l[x] = y0 + y1;
-            unpack2(w2[x], y0, y1);
-            off[x] = y0 + y1;
 #pragma unroll
             for (int k = 1; k < 4; k <<= 1) {
               l[x] += __shfl_xor_sync(kAllLanes, l[x], k);
