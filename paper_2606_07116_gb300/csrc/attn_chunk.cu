@@ -15,9 +15,10 @@
 //   * Work is the list of (row pair tile, block) steps; the CTAs take equal shares of it, and what crosses CTAs
 //     is joined by a second kernel from at most two parts per CTA.
 // P' is a half, and the values q are: the reference m of the exponentials carries the largest value scale of the block,
-// so that P' stays in range whatever the values' size is. A block is weighed against the reference it meets; only
-// where some score passes it by 2^kLazy (or keys are hidden) the maxima are taken and the block weighed again: S is still
-// in tensor memory, as the weights wait in registers until the whole block is through.
+// so that P' stays in range whatever the values' size is. 32 keys at a time are weighed against the reference they meet;
+// only where some score passes it by 2^kLazy the maxima are taken, what was summed and stored so far is rescaled and
+// the 32 are weighed again. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
+// memory leave (four reloads in a row cost more than the products of a block).
 //
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 finds the CTA's work, warps
 // 12-15 widen.
@@ -32,8 +33,8 @@ using namespace offq;
 
 constexpr int kThreads = 512;
 constexpr int kPairRows = 2 * kQt;
-// Registers: 128 a thread at launch, 2 x 184 + 56 + 88 = 4 x 128.
-constexpr int kSoftmaxRegs = 184, kIssueRegs = 56, kWidenRegs = 88;
+// Registers: 128 a thread at launch, 2 x 144 + 96 + 128 = 4 x 128.
+constexpr int kSoftmaxRegs = 144, kIssueRegs = 96, kWidenRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kWidenRegs <= 4 * 128, "register shares");
 
 struct PartHead {  // a part that crosses CTAs: sequence (negative: none), head, row pair tile, whether it is its last
@@ -143,19 +144,21 @@ __device__ __forceinline__ float4 lds128f(uint32_t addr) {
   return v;
 }
 
-// Row `row` of a (sequence, key head): channels 8 k + c and 8 k + c + 4 in (x, y) of the four lanes c of a row; each
-// lane writes channels 8 k + 2 c and the next. The lanes of a warp take part together.
+// Where row `row` of a (sequence, key head) goes.
 template <int D, typename T>
-__device__ __forceinline__ void write_pair(const AttnArgs& a, const PagedSeq& s, int h, int row, bool live, int k, int lane,
-                                           float x, float y) {
+__device__ __forceinline__ T* out_row(const AttnArgs& a, const PagedSeq& s, int h, int row) {
+  return static_cast<T*>(a.out) + (static_cast<int64_t>(s.first) + row / a.G) * a.ld_out +
+         static_cast<int64_t>(h * a.G + row % a.G) * D;
+}
+// The four lanes c of a row hold its channels 8 k + c and 8 k + c + 4 in (x, y); each writes channels 8 k + 2 c and the
+// next. The lanes of a warp take part together; a row without a place is not written.
+template <typename T>
+__device__ __forceinline__ void write_pair(T* row, int k, int lane, float x, float y) {
   const int c = lane & 3;
   const uint32_t u = pack_16<T>(x, y);
   const uint32_t v0 = __shfl_sync(kAllLanes, u, (lane & ~3) | ((2 * c) & 3));
   const uint32_t v1 = __shfl_sync(kAllLanes, u, (lane & ~3) | ((2 * c + 1) & 3));
-  if (!live) return;
-  const int64_t t = static_cast<int64_t>(s.first) + row / a.G;
-  *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.ld_out + static_cast<int64_t>(h * a.G + row % a.G) * D +
-                               8 * k + 2 * c) = __byte_perm(v0, v1, c < 2 ? 0x5410 : 0x7632);
+  if (row != nullptr) *reinterpret_cast<uint32_t*>(row + 8 * k + 2 * c) = __byte_perm(v0, v1, c < 2 ? 0x5410 : 0x7632);
 }
 __device__ __forceinline__ void write_lse(const AttnArgs& a, const PagedSeq& s, int h, int row, float m, float l) {
   if (a.lse == nullptr) return;
@@ -502,10 +505,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           least = min(w.s.len, max(0, w.s.len - w.s.n + row0 / a.G + 1));
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const int r = 8 * x + g, gr = row0 + r;   // x = 2 hh + ii
-            qs[x] = sums[r];
+            qs[x] = sums[8 * x + g];   // x = 2 hh + ii
             l[x] = off[x] = 0.f;
-            m[x] = w.s.len - w.s.n + gr / a.G + 1 > 0 ? -INFINITY : 0.f;  // a row without keys has no maximum to wait for
+            m[x] = -INFINITY;
           }
         }
         for (int j = 0; j < nb; ++j, ++gb) {
@@ -526,111 +528,119 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             int sees[4] = {0, 0, 0, 0};
             if (masked) {
 #pragma unroll
-              for (int x = 0; x < 4; ++x) sees[x] = min(w.s.len, w.s.len - w.s.n + (row0 + 8 * x + g) / a.G + 1);
+              for (int x = 0; x < 4; ++x) sees[x] = min(w.s.len, w.s.len - w.s.n + (row0 + 8 * x + g) / a.G + 1) - key0 - 2 * c;
             }
-            auto hidden = [&](int k, int e, int x) {  // element e of rep k of row x
-              if (!masked) return false;
-              const uint32_t word = k < 4 ? gone.x : k < 8 ? gone.y : k < 12 ? gone.z : gone.w;
-              return (word >> (8 * (k & 3)) & 0xFFu) != 0u || key0 + 8 * k + 2 * c + e >= sees[x];
-            };
-            // Scores relative to m, weights and sums of the whole block; the largest relative score.
-            uint32_t p[2][2][16];
-            uint64_t lb[4], wb[4];
-            auto weigh = [&](auto with_mask) {
-              uint64_t m2[4];
+            // 32 keys at a time: scores relative to m, weights, sums; the weights take the place of scores already read.
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              uint32_t s[2][16], p[2][8];
+              uint64_t lb[4], wb[4];
+              tmem_ld_fragments(s_tm + 32 * q, s[0], s[1]);
+              if (masked) {
+                const uint32_t word = q == 0 ? gone.x : q == 1 ? gone.y : q == 2 ? gone.z : gone.w;
 #pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                const float mm = m[x] == -INFINITY && with_mask ? 0.f : -m[x];
-                m2[x] = pack2(mm, mm);
-                lb[x] = wb[x] = 0;
+                for (int k = 0; k < 4; ++k) {
+                  const bool out = (word >> (8 * k) & 0xFFu) != 0u;
+#pragma unroll
+                  for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                      if (out || 32 * q + 8 * k + e >= sees[x]) s[x >> 1][4 * k + 2 * (x & 1) + e] = 0x7FFFFFFFu;  // NaN: hidden
+                }
               }
-              float top = -INFINITY;
+              const uint32_t pkq = pk + q * 256, pvq = pv + q * 256;
+              auto weigh = [&](auto hide) {
+                float top = -INFINITY;
+                uint64_t m2[4];
 #pragma unroll
-              for (int q = 0; q < 2; ++q) {
-                uint32_t s[2][32];
-                tmem_ld_fragments_pair(s_tm + 64 * q, s[0], s[1]);
+                for (int x = 0; x < 4; ++x) {
+                  m2[x] = pack2(-m[x], -m[x]);
+                  lb[x] = wb[x] = 0;
+                }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const float4 f = lds128f(pk + (8 * q + k) * 64), v = lds128f(pv + (8 * q + k) * 64);
+                for (int k = 0; k < 4; ++k) {
+                  const float4 f = lds128f(pkq + k * 64), v = lds128f(pvq + k * 64);
                   const uint64_t a2 = pack2(f.x, f.y), b2 = pack2(f.z, f.w), s2 = pack2(v.x, v.y), o2 = pack2(v.z, v.w);
 #pragma unroll
                   for (int x = 0; x < 4; ++x) {
                     const uint32_t* e = &s[x >> 1][4 * k + 2 * (x & 1)];
                     float y0, y1;
                     unpack2(fma2v(pack2(__uint_as_float(e[0]), __uint_as_float(e[1])), a2, fma2v(b2, pack2(qs[x], qs[x]), m2[x])), y0, y1);
-                    if (with_mask) {
-                      if (hidden(8 * q + k, 0, x)) y0 = -INFINITY;
-                      if (hidden(8 * q + k, 1, x)) y1 = -INFINITY;
-                    } else {
-                      top = fmaxf(top, fmaxf(y0, y1));
+                    if constexpr (hide.value) {
+                      if (e[0] == 0x7FFFFFFFu) y0 = -INFINITY;
+                      if (e[1] == 0x7FFFFFFFu) y1 = -INFINITY;
                     }
+                    top = fmaxf(top, fmaxf(y0, y1));
                     const uint64_t p2 = pack2(ex2(y0), ex2(y1));
                     lb[x] = add2_rn(lb[x], p2);
                     wb[x] = fma2v(p2, o2, wb[x]);
                     unpack2(mul2v(p2, s2), y0, y1);
-                    p[q][x >> 1][2 * k + (x & 1)] = pack_16<__half>(y0, y1);
+                    p[x >> 1][2 * k + (x & 1)] = pack_16<__half>(y0, y1);
                   }
                 }
-              }
-              return top;
-            };
-            bool again = masked;
-            if (!masked) again = __any_sync(kAllLanes, !(weigh(std::false_type{}) <= kLazy - lift));
-            if (again) {  // some row's reference moves, or some keys are hidden
-              float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, keep[4];
-#pragma unroll 1
-              for (int q = 0; q < 2; ++q) {
-                uint32_t s[2][32];
-                tmem_ld_fragments_pair(s_tm + 64 * q, s[0], s[1]);
+                return top;
+              };
+              const bool fits = (masked ? weigh(std::true_type{}) : weigh(std::false_type{})) <= kLazy - lift;
+              if (__any_sync(kAllLanes, !fits)) {  // some row's reference moves
+                float keep[4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const float4 f = lds128f(pk + (8 * q + k) * 64);
+                for (int x = 0; x < 4; ++x) {
+                  float top = -INFINITY;
 #pragma unroll
-                  for (int x = 0; x < 4; ++x) {
+                  for (int k = 0; k < 4; ++k) {
+                    const float4 f = lds128f(pkq + k * 64);
                     const uint32_t* e = &s[x >> 1][4 * k + 2 * (x & 1)];
                     const float z0 = fmaf(__uint_as_float(e[0]), f.x, f.z * qs[x]), z1 = fmaf(__uint_as_float(e[1]), f.y, f.w * qs[x]);
-                    if (!hidden(8 * q + k, 0, x)) top[x] = fmaxf(top[x], z0);
-                    if (!hidden(8 * q + k, 1, x)) top[x] = fmaxf(top[x], z1);
+                    top = fmaxf(top, fmaxf(z0, z1));  // hidden keys are NaN and do not count
+                  }
+                  top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, 1));
+                  top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, 2));
+                  top = fmaxf(top + lift, m[x]);
+                  keep[x] = m[x] == -INFINITY ? 0.f : ex2(m[x] - top);
+                  m[x] = top;
+                  l[x] *= keep[x];
+                  off[x] *= keep[x];
+                }
+                if (j > 0) {
+#pragma unroll 1
+                  for (int u = 0; u < D / 32; ++u) {
+                    uint32_t o0[16], o1[16];
+                    tmem_ld_fragments(o_tm + 32 * u, o0, o1);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                      o0[e] = __float_as_uint(__uint_as_float(o0[e]) * keep[e >> 1 & 1]);
+                      o1[e] = __float_as_uint(__uint_as_float(o1[e]) * keep[2 + (e >> 1 & 1)]);
+                    }
+                    tmem_st_fragments(o_tm + 32 * u, o0);
+                    tmem_st_fragments(o_tm + 32 * u + (16u << 16), o1);
                   }
                 }
+                tmem_st_wait();
+#pragma unroll 1
+                for (int u = 0; u < 2 * q; ++u) {  // this block's weights so far
+                  const uint32_t at = s_tm + 16 * (u >> 1) + (static_cast<uint32_t>(16 * (u & 1)) << 16);
+                  uint32_t r[8];
+                  tmem_ld_pairs(at, r);
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) {
+                    const float k = u & 1 ? keep[2 + (e & 1)] : keep[e & 1];
+                    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&r[e]));
+                    r[e] = pack_16<__half>(v.x * k, v.y * k);
+                  }
+                  tmem_st_pairs(at, r);
+                }
+                weigh(std::true_type{});
               }
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
-                top[x] = fmaxf(top[x], __shfl_xor_sync(kAllLanes, top[x], 1));
-                top[x] = fmaxf(top[x], __shfl_xor_sync(kAllLanes, top[x], 2));
-                top[x] = fmaxf(top[x] + lift, m[x]);
-                keep[x] = m[x] == -INFINITY ? 0.f : ex2(m[x] - top[x]);
-                m[x] = top[x];
-                l[x] *= keep[x];
-                off[x] *= keep[x];
+                float y0, y1;
+                unpack2(lb[x], y0, y1);
+                l[x] += y0 + y1;
+                unpack2(wb[x], y0, y1);
+                off[x] += y0 + y1;
               }
-              if (j > 0 && __any_sync(kAllLanes, keep[0] != 1.f || keep[1] != 1.f || keep[2] != 1.f || keep[3] != 1.f)) {
-#pragma unroll
-                for (int q = 0; q < D / 64; ++q)
-#pragma unroll
-                  for (int hh = 0; hh < 2; ++hh) {
-                    uint32_t o[32];
-                    const uint32_t at = o_tm + 64 * q + (static_cast<uint32_t>(16 * hh) << 16);
-                    tmem_ld_fragments_part(at, o);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep[2 * hh + (e >> 1 & 1)]);
-                    tmem_st_fragments_part(at, o);
-                  }
-              }
-              weigh(std::true_type{});
-            }
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              float y0, y1;
-              unpack2(lb[x], y0, y1);
-              l[x] += y0 + y1;
-              unpack2(wb[x], y0, y1);
-              off[x] += y0 + y1;
-            }
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              tmem_st_pairs(s_tm + 32 * q, p[q][0]);
-              tmem_st_pairs(s_tm + 32 * q + (16u << 16), p[q][1]);
+              tmem_st_pairs(s_tm + 16 * q, p[0]);
+              tmem_st_pairs(s_tm + 16 * q + (16u << 16), p[1]);
             }
             tmem_st_wait();
             tc_fence_before();
@@ -648,6 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           const int which = w.blk == 0 ? 1 : 0;
           float* part = part_data<D>(a.workspace, gridDim.x, blockIdx.x, which);
           float inv[4];
+          T* to[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
 #pragma unroll
@@ -657,6 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             }
             inv[x] = l[x] > 0.f ? __fdividef(1.f, l[x]) : 0.f;
             const int r = 8 * x + g;
+            to[x] = row0 + r < rows ? out_row<D, T>(a, w.s, w.h, row0 + r) : nullptr;
             if (c == 0) {
               if (!complete) {
                 part[i * kQt + quad * 32 + r] = m[x];
@@ -667,30 +679,27 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             }
           }
 #pragma unroll 1
-          for (int q = 0; q < D / 64; ++q)
+          for (int q = 0; q < D / 32; ++q) {
+            uint32_t o[2][16];
+            tmem_ld_fragments(o_tm + 32 * q, o[0], o[1]);
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              uint32_t o[32];
-              tmem_ld_fragments_part(o_tm + 64 * q + (static_cast<uint32_t>(16 * hh) << 16), o);
+            for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
+              for (int k = 0; k < 4; ++k) {
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(o[4 * k + e]) + off[2 * hh + (e >> 1)];
+                for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(o[hh][4 * k + e]) + off[2 * hh + (e >> 1)];
                 if (complete) {
 #pragma unroll
-                  for (int ii = 0; ii < 2; ++ii) {
-                    const int r = row0 + 16 * hh + 8 * ii + g;
-                    write_pair<D, T>(a, w.s, w.h, r, r < rows, 8 * q + k, lane, v[2 * ii] * inv[2 * hh + ii],
-                                     v[2 * ii + 1] * inv[2 * hh + ii]);
-                  }
+                  for (int ii = 0; ii < 2; ++ii)
+                    write_pair<T>(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii] * inv[2 * hh + ii], v[2 * ii + 1] * inv[2 * hh + ii]);
                 } else {
-                  reinterpret_cast<float4*>(part + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + 8 * q + k) * 32 + lane] =
+                  reinterpret_cast<float4*>(part + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + 4 * q + k) * 32 + lane] =
                       make_float4(v[0], v[1], v[2], v[3]);
                 }
               }
-              __syncwarp();
-            }
+            __syncwarp();
+          }
           if (!complete && i == 0 && warp == 0 && lane == 0)
             heads[which] = PartHead{w.b, w.h, w.p, w.blk + nb == w.blocks};
           tc_fence_before();
@@ -773,10 +782,10 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
     for (int ii = 0; ii < 2; ++ii) {
       const int x = 2 * hh + ii, r = row0 + 8 * x + g;
       const float inv = sum[x] > 0.f ? __fdividef(1.f, sum[x]) : 0.f;
+      T* to = r < rows ? out_row<D, T>(a, s, p.h, r) : nullptr;
 #pragma unroll
       for (int k = 0; k < kReps; ++k)
-        write_pair<D, T>(a, s, p.h, r, r < rows, q * kReps + k, lane, (ii ? acc[hh][k].z : acc[hh][k].x) * inv,
-                         (ii ? acc[hh][k].w : acc[hh][k].y) * inv);
+        write_pair<T>(to, q * kReps + k, lane, (ii ? acc[hh][k].z : acc[hh][k].x) * inv, (ii ? acc[hh][k].w : acc[hh][k].y) * inv);
       if (q == 0 && c == 0 && r < rows) write_lse(a, s, p.h, r, top[x], sum[x]);
     }
 }
