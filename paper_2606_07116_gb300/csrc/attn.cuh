@@ -14,9 +14,6 @@ namespace offq {
 constexpr uint32_t kAllLanes = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// A running maximum is left where it is until a score passes it by this much (in powers of two):
-// weights then reach 2^8 at most, far from any overflow, and a rescaling of the sums is rare.
-constexpr float kLazy = 8.0f;
 
 struct AttnArgs {
   const void* q;

@@ -16,7 +16,7 @@
 //     is joined by a second kernel from at most two parts per CTA.
 // P' is a half, and the values q are: the reference m of the exponentials carries the largest value scale of the block,
 // so that P' stays in range whatever the values' size is. 32 keys at a time are weighed against the reference they meet;
-// only where some score passes it by 2^kLazy the maxima are taken, what was summed and stored so far is rescaled and
+// only where a row's 32 weights sum to more than 2^kMostLog2 the maxima are taken, what was summed and stored so far is rescaled and
 // the 32 are weighed again. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
 // memory leave (four reloads in a row cost more than the products of a block).
 //
@@ -33,6 +33,8 @@ using namespace offq;
 
 constexpr int kThreads = 512;
 constexpr int kPairRows = 2 * kQt;
+// A weight times its value's scale, as a half, reaches 2^14 before a row's reference is moved (and is 1 at most after it).
+constexpr float kMostLog2 = 14.f;
 // Registers: 128 a thread at launch, 2 x 144 + 96 + 128 = 4 x 128.
 constexpr int kSoftmaxRegs = 144, kIssueRegs = 96, kWidenRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kWidenRegs <= 4 * 128, "register shares");
@@ -138,9 +140,9 @@ __device__ __forceinline__ uint32_t tile_off(int r, int ch) {
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-__device__ __forceinline__ float4 lds128f(uint32_t addr) {
+__device__ __forceinline__ float4 lds128f(const float4* p) {
   float4 v;
-  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(smem_u32(p)) : "memory");
   return v;
 }
 
@@ -258,10 +260,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     constexpr int kRowsPer = 128 / kChunks;     // rows that the 128 threads cover at once
     constexpr int kReps = kKt / kRowsPer;       // 4 (D = 128), 2
     const int t = tid - 12 * 32, w = t >> 5;
-    const int c = t % kChunks, row = t / kChunks;
+    // Lanes that share a bank group in one atom and the other (c and c + 2) take rows whose swizzles differ.
+    const int c = t % kChunks, row = (t / kChunks) ^ (c & 2);
     // The key whose parameters this thread takes is one of its own rows: the c-th.
     static_assert(kChunks == kReps, "a row for each of the lanes that share them");
     const int par_row = row + kRowsPer * c;
+    uint32_t to_chunk[4];  // of this lane's four words in a tile (kRowsPer is a multiple of 8: the swizzle is the same in all reps)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to_chunk[k] = tile_off(row, 4 * c + k);
     uint4 kc[kReps], vc[kReps];
     float2 kp, vp;
     int page[kReps], next_page[kReps];
@@ -339,14 +345,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       if (more) take_pages();
       if (gb >= 2 && !wait(&ctrl->k_empty[slot], (gb >> 1) - 1)) break;
       const uint32_t kt = base + L::kKeys + slot * L::kTileBytes, vt = base + L::kValues + slot * L::kTileBytes;
-      // Words in an order that spreads a warp's 16-byte stores over all banks.
-      const bool swap = (c & 2) != 0;
-      auto widened = [&](uint32_t tile, const uint4& x, int i, bool is_v) {
-        const uint32_t wd[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
+      auto widened = [&](uint32_t tile, const uint4& x, int i, auto is_v) {
+        const uint32_t wd[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t to = tile + tile_off(row + kRowsPer * i, 4 * c + (k ^ (swap ? 2 : 0)));
-          if (is_v) {
+          const uint32_t to = tile + to_chunk[k] + i * kRowsPer * 128;
+          if constexpr (is_v.value) {
             uint32_t q[4];
             widen_signed(wd[k], q[0], q[1]);
             widen_signed(wd[k] >> 8, q[2], q[3]);
@@ -357,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
         }
       };
 #pragma unroll
-      for (int i = 0; i < kReps; ++i) widened(kt, kc[i], i, false);
+      for (int i = 0; i < kReps; ++i) widened(kt, kc[i], i, std::false_type{});
       {
         float* pk = reinterpret_cast<float*>(smem + L::kParK + slot * 1024) + (par_row >> 1) * 4 + (par_row & 1);
         float* pv = reinterpret_cast<float*>(smem + L::kParV + slot * 1024) + (par_row >> 1) * 4 + (par_row & 1);
@@ -381,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       if (gb + 2 < count) step();
       if (gb >= 2 && !wait(&ctrl->v_empty[slot], (gb >> 1) - 1)) break;
 #pragma unroll
-      for (int i = 0; i < kReps; ++i) widened(vt, vc[i], i, true);
+      for (int i = 0; i < kReps; ++i) widened(vt, vc[i], i, std::true_type{});
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctrl->v_full[slot]));
@@ -517,13 +521,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           if (!ok) break;
           if (active) {
             tc_fence_after();
-            const uint32_t pk = base + L::kParK + slot * 1024 + c * 16, pv = base + L::kParV + slot * 1024 + c * 16;
+            const float4* pk = reinterpret_cast<const float4*>(smem + L::kParK + slot * 1024) + c;
+            const float4* pv = reinterpret_cast<const float4*>(smem + L::kParV + slot * 1024) + c;
             const int key0 = (w.blk + j) * kKt;
             const uint4 gone = *reinterpret_cast<const uint4*>(ctrl->missing[slot]);
             const float4 sm = *reinterpret_cast<const float4*>(ctrl->smax[slot]);
-            // log2 of the block's largest value scale, rounded up: weights times scales stay below 2^kLazy.
+            // log2 of the block's largest value scale, rounded up: weights times scales stay below 2^kMostLog2.
             const float big = fmaxf(fmaxf(sm.x, sm.y), fmaxf(sm.z, sm.w));
             const float lift = static_cast<float>(min(64, max(-24, static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
+            const float most = ex2(kMostLog2 - lift);
             const bool masked = key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u;
             int sees[4] = {0, 0, 0, 0};
             if (masked) {
@@ -548,9 +554,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                       if (out || 32 * q + 8 * k + e >= sees[x]) s[x >> 1][4 * k + 2 * (x & 1) + e] = 0x7FFFFFFFu;  // NaN: hidden
                 }
               }
-              const uint32_t pkq = pk + q * 256, pvq = pv + q * 256;
+              const float4 *pkq = pk + q * 16, *pvq = pv + q * 16;
               auto weigh = [&](auto hide) {
-                float top = -INFINITY;
                 uint64_t m2[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -559,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                  const float4 f = lds128f(pkq + k * 64), v = lds128f(pvq + k * 64);
+                  const float4 f = lds128f(pkq + k * 4), v = lds128f(pvq + k * 4);
                   const uint64_t a2 = pack2(f.x, f.y), b2 = pack2(f.z, f.w), s2 = pack2(v.x, v.y), o2 = pack2(v.z, v.w);
 #pragma unroll
                   for (int x = 0; x < 4; ++x) {
@@ -570,7 +575,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                       if (e[0] == 0x7FFFFFFFu) y0 = -INFINITY;
                       if (e[1] == 0x7FFFFFFFu) y1 = -INFINITY;
                     }
-                    top = fmaxf(top, fmaxf(y0, y1));
                     const uint64_t p2 = pack2(ex2(y0), ex2(y1));
                     lb[x] = add2_rn(lb[x], p2);
                     wb[x] = fma2v(p2, o2, wb[x]);
@@ -578,9 +582,21 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                     p[x >> 1][2 * k + (x & 1)] = pack_16<__half>(y0, y1);
                   }
                 }
-                return top;
               };
-              const bool fits = (masked ? weigh(std::true_type{}) : weigh(std::false_type{})) <= kLazy - lift;
+              if (masked)
+                weigh(std::true_type{});
+              else
+                weigh(std::false_type{});
+              // Weights are positive: a sum that is small has no large one in it. (An unset reference gives infinity.)
+              bool fits = true;
+              float row_sum[4];
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                float y0, y1;
+                unpack2(lb[x], y0, y1);
+                row_sum[x] = y0 + y1;
+                fits &= row_sum[x] <= most;
+              }
               if (__any_sync(kAllLanes, !fits)) {  // some row's reference moves
                 float keep[4];
 #pragma unroll
@@ -588,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                   float top = -INFINITY;
 #pragma unroll
                   for (int k = 0; k < 4; ++k) {
-                    const float4 f = lds128f(pkq + k * 64);
+                    const float4 f = lds128f(pkq + k * 4);
                     const uint32_t* e = &s[x >> 1][4 * k + 2 * (x & 1)];
                     const float z0 = fmaf(__uint_as_float(e[0]), f.x, f.z * qs[x]), z1 = fmaf(__uint_as_float(e[1]), f.y, f.w * qs[x]);
                     top = fmaxf(top, fmaxf(z0, z1));  // hidden keys are NaN and do not count
@@ -624,19 +640,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
 #pragma unroll
                   for (int e = 0; e < 8; ++e) {
                     const float k = u & 1 ? keep[2 + (e & 1)] : keep[e & 1];
-                    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&r[e]));
-                    r[e] = pack_16<__half>(v.x * k, v.y * k);
+                    r[e] = scale_16<__half>(r[e], k);
                   }
                   tmem_st_pairs(at, r);
                 }
                 weigh(std::true_type{});
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  float y0, y1;
+                  unpack2(lb[x], y0, y1);
+                  row_sum[x] = y0 + y1;
+                }
               }
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
                 float y0, y1;
-                unpack2(lb[x], y0, y1);
-                l[x] += y0 + y1;
                 unpack2(wb[x], y0, y1);
+                l[x] += row_sum[x];
                 off[x] += y0 + y1;
               }
               tmem_st_pairs(s_tm + 16 * q, p[0]);

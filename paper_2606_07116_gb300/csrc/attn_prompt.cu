@@ -9,8 +9,9 @@
 // the longer of the two.
 //
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 the TMA copies.
-// The maximum is moved only when a score passes it by 2^8 (kLazy), so O is rescaled rarely and by the
-// softmax threads themselves: when S is complete, so is every product issued before it, O's among them.
+// A row's reference maximum is moved only when a score passes it by 2^8 (kLazy), so O is rescaled rarely and
+// by the softmax threads themselves: when S is complete, so is every product issued before it, O's among them. The
+// weights of the first 64 keys go to the products while those of the other 64 are made.
 //
 // Rows past a sequence's end are the next sequence's. As queries they are not written, as keys their
 // scores are replaced, and as values they are zeroed in shared memory (0 times infinity is not 0).
@@ -23,9 +24,12 @@ namespace {
 using namespace offq;
 
 constexpr int kThreads = 384;  // two softmax warpgroups, one of single warps
-// Registers: 168 a thread at launch, 3 x 168 >= 2 x 216 + 72.
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+// Registers: 168 a thread at launch, 3 x 168 >= 2 x 208 + 88.
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * 168, "register shares");
+// A row's reference is left where it is until a score passes it by this much (in powers of two): weights then reach
+// 2^8 at most, far from any overflow, and a rescaling of the sums is rare.
+constexpr float kLazy = 8.0f;
 
 template <int D>
 struct PromptLayout {
@@ -40,7 +44,7 @@ struct PromptLayout {
 struct PromptCtrl {
   uint64_t q_full, tail, done;
   uint64_t full[8], empty[8];
-  uint64_t s_full[2], p_ready[2];
+  uint64_t s_full[2], p_ready[2][2];  // weights of 64 keys at a time
   uint32_t tmem;
   int abort;
   int seq, tile;
@@ -78,7 +82,8 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&ctrl->s_full[i]), 1);
-      mbar_init(smem_u32(&ctrl->p_ready[i]), 4);
+      mbar_init(smem_u32(&ctrl->p_ready[i][0]), 4);
+      mbar_init(smem_u32(&ctrl->p_ready[i][1]), 4);
     }
     ctrl->abort = 0;
     mbar_fence_init();
@@ -211,10 +216,10 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
           }
           mma_commit(smem_u32(&ctrl->s_full[i]));
         };
-        auto outputs = [&](int i, int j) {  // O_i += P_i V_j
+        auto outputs = [&](int i, int j, int part) {  // O_i += P_i V_j, 64 keys of it
           const uint64_t vd = smem_desc_rows_contracted(ring + (2 * j + 1) % L::kSlots * L::kTileBytes);
   #pragma unroll
-          for (int kk = 0; kk < kKt / 16; ++kk)
+          for (int kk = 4 * part; kk < 4 * part + 4; ++kk)
             mma_16_ts(tmem + 256 + i * D, tmem + i * 128 + kk * 8, vd + ((kk * 16 * 128) >> 4), kIdescO, (j | kk) != 0);
         };
         bool ok = wait(smem_u32(&ctrl->q_full), 0) && wait(full, 0);
@@ -233,11 +238,16 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
           if (ok && j + 1 < most) ok = wait(full + 8 * (ks % L::kSlots), (ks / L::kSlots) & 1);
           for (int i = 0; i < 2 && ok; ++i) {
             if (j >= blocks[i]) continue;
-            ok = wait(smem_u32(&ctrl->p_ready[i]), j & 1);
+            ok = wait(smem_u32(&ctrl->p_ready[i][0]), j & 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) outputs(i, j, 0);
+            __syncwarp();
+            ok = wait(smem_u32(&ctrl->p_ready[i][1]), j & 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              outputs(i, j);
+              outputs(i, j, 1);
               if (j + 1 < blocks[i]) scores(i, j + 1);
               else mma_commit(smem_u32(&ctrl->s_full[i]));  // the last phase says that O is complete
             }
@@ -280,10 +290,11 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
             for (int e = 0; e < kKt; ++e)
               if (e >= valid) s[e] = 0xFF800000u;  // -inf
           }
-          float top = -INFINITY;
+          float tops[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int e = 0; e < kKt; e += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
-          top *= sc;
+          for (int e = 0; e < kKt; e += 2)
+            tops[(e >> 1) & 1] = max3(tops[(e >> 1) & 1], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+          const float top = fmaxf(tops[0], tops[1]) * sc;
           const bool move = top > m + kLazy;
           if (__any_sync(kAllLanes, move)) {
             const float next = move ? top : m;
@@ -291,14 +302,14 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
             m = next;
             sum *= keep;
             if (j > 0) {
-#pragma unroll
-              for (int q = 0; q < D / 16; ++q) {
+#pragma unroll 1
+              for (int u = 0; u < D / 16; ++u) {
                 uint32_t o[16];
-                tmem_ld_16cols(o_tm + 16 * q, o);
+                tmem_ld_16cols(o_tm + 16 * u, o);
                 tmem_ld_wait_for(o);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                tmem_st_16cols(o_tm + 16 * q, o);
+                tmem_st_16cols(o_tm + 16 * u, o);
               }
             }
           }
@@ -318,14 +329,16 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
               p[e / 2] = pack_16<T>(x, y);
             }
             tmem_st_16cols(s_tm + 16 * q, p);
+            if (q & 1) {  // the products with these 64 keys may begin
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_ready[i][q >> 1]));
+            }
           }
           float x, y;
           unpack2(add2_rn(add2_rn(part[0], part[1]), add2_rn(part[2], part[3])), x, y);
           sum += x + y;
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_ready[i]));
         }
         if (ok) ok = __all_sync(kAllLanes, mbar_wait(smem_u32(&ctrl->s_full[i]), blocks[i] & 1, abort));
         if (ok) {

@@ -81,6 +81,13 @@ __device__ __forceinline__ void tmem_ld_128cols(uint32_t taddr, uint32_t (&r)[12
       : "memory");
 }
 
+// The largest of three.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // 32 rows x 32 columns as fragments: with g = lane / 4 and c = lane % 4, r{h}[4 k + 2 i + e] is row 16 h + 8 i + g,
 // column 8 k + 2 c + e (k < 4). A thread then meets a quarter of the columns instead of all.
 __device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t (&r0)[16], uint32_t (&r1)[16]) {
@@ -138,6 +145,17 @@ __device__ __forceinline__ uint32_t pack_16(float a, float b) {
   } else {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+
+// A pair of weights times k.
+template <typename T>
+__device__ __forceinline__ uint32_t scale_16(uint32_t w, float k) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    return pack_16<T>(__uint_as_float(w << 16) * k, __uint_as_float(w & 0xFFFF0000u) * k);
+  } else {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return pack_16<T>(v.x * k, v.y * k);
   }
 }
 
