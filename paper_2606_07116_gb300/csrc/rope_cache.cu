@@ -15,7 +15,9 @@
 // A lane owns 8 neighbouring channels (one 16-byte load of a 16-bit type), so a head of 128 takes
 // half a warp and a head of 64 a quarter; sums, maxima and the outer butterflies are xor shuffles.
 // A warp stays with one token and takes several groups of heads, with the token's cosines and sines
-// in registers: they would otherwise be read again for each head, four times the data's own bytes.
+// in registers: they would otherwise be read again for each head, four times the data's own bytes. The reads of
+// two groups (eight of the cache's) are issued before the first is worked on: one 16-byte read a lane in flight
+// does not cover the memory's latency.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -32,10 +34,12 @@ using namespace offq;
 
 constexpr int kE = 8;        // channels per lane
 constexpr int kWarps = 8;    // warps per CTA
+constexpr int kAhead = 2;    // groups of heads read ahead
+constexpr int kMostGroups = 8;  // of a warp
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 struct HeadArgs {
-  // Virtual heads of a token: H[0] queries, H[1] keys, H[2] values.
+  // Heads of a token: H[0] queries, H[1] keys, H[2] values.
   const void* x[3];
   int64_t ld[3];
   int H[3];
@@ -60,15 +64,25 @@ struct HeadArgs {
   int* status;
 };
 
+// 8 channels as they lie in memory, and as floats.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[kE]) {
+struct Raw8 {
+  uint4 u[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ void read8(const T* p, Raw8<T>& r) {
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) r.u[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[kE]) {
   if constexpr (sizeof(T) == 4) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = __uint_as_float(r.u[0].x); v[1] = __uint_as_float(r.u[0].y);
+    v[2] = __uint_as_float(r.u[0].z); v[3] = __uint_as_float(r.u[0].w);
+    v[4] = __uint_as_float(r.u[1].x); v[5] = __uint_as_float(r.u[1].y);
+    v[6] = __uint_as_float(r.u[1].z); v[7] = __uint_as_float(r.u[1].w);
   } else {
-    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (std::is_same<T, __nv_bfloat16>::value) {
@@ -81,6 +95,13 @@ __device__ __forceinline__ void load8(const T* p, float (&v)[kE]) {
       }
     }
   }
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[kE]) {
+  Raw8<T> r;
+  read8(p, r);
+  widen8(r, v);
 }
 
 template <typename T>
@@ -124,31 +145,33 @@ __device__ __forceinline__ float head_absmax(const float (&v)[kE]) {
   return s;
 }
 
-// x H_D, not normalised.
+// x H_D, not normalised. Channels e and e + 4 of a lane go through packed additions together.
 template <int D>
 __device__ __forceinline__ void head_hadamard(float (&v)[kE], int lane) {
+  butterfly2(v[0], v[4], v[1], v[5]);
+  butterfly2(v[2], v[6], v[3], v[7]);
+  butterfly2(v[0], v[4], v[2], v[6]);
+  butterfly2(v[1], v[5], v[3], v[7]);
 #pragma unroll
-  for (int h = 1; h < kE; h <<= 1) {
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      if (e & h) continue;
-      const float a = v[e], b = v[e + h];
-      v[e] = __fadd_rn(a, b);
-      v[e + h] = __fsub_rn(a, b);
-    }
+  for (int e = 0; e < 4; ++e) {
+    const float x = v[e], y = v[e + 4];
+    v[e] = __fadd_rn(x, y);
+    v[e + 4] = __fsub_rn(x, y);
   }
 #pragma unroll
   for (int m = 1; m < D / kE; m <<= 1) {
     const float sign = (lane & m) ? -1.f : 1.f;
+    const uint64_t sign2 = pack2(sign, sign);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const float o = __shfl_xor_sync(kAll, v[e], m);
-      v[e] = __fmaf_rn(sign, v[e], o);  // o + v or o - v: the product with +-1 is exact
+    for (int e = 0; e < 4; ++e) {
+      const uint64_t o = pack2(__shfl_xor_sync(kAll, v[e], m), __shfl_xor_sync(kAll, v[e + 4], m));
+      unpack2(fma2v(sign2, pack2(v[e], v[e + 4]), o), v[e], v[e + 4]);  // o + v or o - v: the product with +-1 is exact
     }
   }
 }
 
-// Cosines and sines of this lane's channels: with neighbouring pairs the first four of each.
+// Cosines and sines of this lane's channels. Pairs of two lanes: x c + y s with the sine's sign taken in, 1 and 0
+// past the rotated channels; neighbouring pairs: the first four of each.
 struct Angles {
   float c[kE], s[kE];
 };
@@ -156,6 +179,11 @@ struct Angles {
 template <int D>
 __device__ __forceinline__ void load_angles(const HeadArgs& a, const float* row, int d0, Angles& t) {
   const int half = a.rot / 2;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    t.c[e] = 1.f;
+    t.s[e] = 0.f;
+  }
   if (d0 >= a.rot) return;
   if (a.interleaved) {
     const float4 c = __ldg(reinterpret_cast<const float4*>(row + d0 / 2));
@@ -166,31 +194,28 @@ __device__ __forceinline__ void load_angles(const HeadArgs& a, const float* row,
     const int f = d0 < half ? d0 : d0 - half;
     load8(row + f, t.c);
     load8(row + half + f, t.s);
+    if (d0 < half) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) t.s[e] = -t.s[e];
+    }
   }
 }
 
+// `partner`: the lane of the other half of this lane's pairs (rot_dim is a multiple of 16: same element).
 template <int D>
-__device__ __forceinline__ void rotary(const HeadArgs& a, const Angles& t, int d0, int lane, float (&v)[kE]) {
-  if (a.rot == 0) return;
-  if (a.interleaved) {
-    if (d0 >= a.rot) return;
+__device__ __forceinline__ void rotary(bool interleaved, const Angles& t, int partner, float (&v)[kE]) {
+  if (interleaved) {
 #pragma unroll
     for (int m = 0; m < kE / 2; ++m) {
       const float x = v[2 * m], y = v[2 * m + 1];
       v[2 * m] = __fsub_rn(__fmul_rn(x, t.c[m]), __fmul_rn(y, t.s[m]));
       v[2 * m + 1] = __fadd_rn(__fmul_rn(y, t.c[m]), __fmul_rn(x, t.s[m]));
     }
-    return;
-  }
-  const int half = a.rot / 2, step = half / kE;  // rot_dim is a multiple of 16: a pair is two lanes, same element
-  const bool first = d0 < half, in = d0 < a.rot;
-  const int src = in ? (first ? lane + step : lane - step) : lane;
+  } else {
 #pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    const float o = __shfl_sync(kAll, v[e], src);
-    if (in) {
-      const float p = __fmul_rn(v[e], t.c[e]), q = __fmul_rn(o, t.s[e]);
-      v[e] = first ? __fsub_rn(p, q) : __fadd_rn(p, q);
+    for (int e = 0; e < kE; ++e) {
+      const float o = __shfl_sync(kAll, v[e], partner);
+      v[e] = __fadd_rn(__fmul_rn(v[e], t.c[e]), __fmul_rn(o, t.s[e]));
     }
   }
 }
@@ -215,12 +240,13 @@ __device__ __forceinline__ void quantize_head(float (&v)[kE], bool rotate, bool 
   }
   const float top = head_absmax<D>(v);
   const float inv = top > 0.f ? __fdiv_rn(7.0f, top) : 0.f;
+  // |r inv| <= 7 (1 + 2^-22), so rounding alone keeps the codes in -7 .. 7. Adding 1.5 * 2^23 + 8 rounds to the nearest
+  // even integer (the spacing there is 1) and leaves u = q + 8 in the low bits; eight are packed by shifted sums, and
+  // what the upper bits add up to is taken off at the end.
   uint32_t w = 0;
 #pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    const float q = fminf(fmaxf(rintf(__fmul_rn(v[e], inv)), -7.f), 7.f);
-    w |= static_cast<uint32_t>(static_cast<int>(q) + 8) << (4 * e);
-  }
+  for (int e = kE - 1; e >= 0; --e) w = (w << 4) + __float_as_uint(__fadd_rn(__fmul_rn(v[e], inv), 12582920.0f));
+  w -= 0x4B400000u * 0x11111111u;
   if (!live) return;
   reinterpret_cast<uint32_t*>(codes)[l] = w;
   if (l == 0) {
@@ -229,73 +255,97 @@ __device__ __forceinline__ void quantize_head(float (&v)[kE], bool rotate, bool 
   }
 }
 
-template <int D, typename Tin, typename Tout>
-__global__ void __launch_bounds__(kWarps * 32) heads_kernel(const HeadArgs a) {
-  constexpr int kLanes = D / kE, kUnits = 32 / kLanes;  // lanes per head, heads per warp
+// `groups` groups of heads of token t, from head h0 on (this lane's first head). KIND 0: queries, 1: keys, 2: values.
+template <int D, typename Tin, typename Tout, int KIND>
+__device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, int groups, int lane) {
+  constexpr int kLanes = D / kE, kUnits = 32 / kLanes;
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
-  const int lane = threadIdx.x & 31, l = lane % kLanes, unit = lane / kLanes;
+  const int l = lane % kLanes, heads = a.H[KIND];
+  const Tin* x = static_cast<const Tin*>(a.x[KIND]) + t * a.ld[KIND] + l * kE;
+  bool ok = true;
+  Angles ang;
+  int partner = lane;
+  if (KIND < 2 && a.rot != 0) {
+    const int64_t p = __ldg(a.pos + t);
+    ok = p >= 0 && p < a.max_pos;
+    if (!ok && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+    load_angles<D>(a, a.table + (ok ? p : 0) * a.rot, l * kE, ang);
+    if (l * kE < a.rot) partner = lane + (l * kE < a.rot / 2 ? a.rot / 2 / kE : -(a.rot / 2 / kE));
+  }
+  uint8_t* codes = nullptr;
+  float* params = nullptr;
+  if (KIND > 0) {
+    const int64_t slot = __ldg(a.slots + t);
+    if (slot >= a.slots_in_cache && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+    ok = ok && slot >= 0 && slot < a.slots_in_cache;
+    const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
+    const int64_t row = ok ? ((page * heads) << a.page_shift) + at : 0;
+    codes = a.codes[KIND - 1] + row * (D / 2);
+    params = a.params[KIND - 1] + row * 2;
+  }
+  const float* norm = KIND < 2 ? a.norm[KIND == 1] : nullptr;
+  for (int base = 0; base < groups; base += kAhead) {
+    Raw8<Tin> raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (base + u < groups) read8(x + min(h0 + (base + u) * kUnits, heads - 1) * D, raw[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (base + u >= groups) break;
+      const int h = h0 + (base + u) * kUnits;
+      const bool live = ok && h < heads;
+      float v[kE];
+      widen8(raw[u], v);
+      if (KIND < 2) {
+        if (norm != nullptr) {
+          float sq[kE], wt[kE];
+          load8(norm + min(h, heads - 1) * D + l * kE, wt);
+#pragma unroll
+          for (int e = 0; e < kE; ++e) sq[e] = __fmul_rn(v[e], v[e]);
+          const float mean = __fmul_rn(head_sum<D>(sq), 1.0f / D);
+          const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(mean, a.eps)));
+#pragma unroll
+          for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(__fmul_rn(v[e], inv), wt[e]);
+        }
+        if (a.rot != 0) rotary<D>(a.interleaved != 0, ang, partner, v);
+      }
+      if constexpr (KIND == 0) {
+        if (a.rotate[0]) {
+          head_hadamard<D>(v, lane);
+#pragma unroll
+          for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(v[e], kRoot);
+        }
+        if (live) store8(static_cast<Tout*>(a.out) + t * a.ld_out + h * D + l * kE, v);
+      } else {
+        const int64_t row = static_cast<int64_t>(live ? h : 0) << a.page_shift;
+        quantize_head<D>(v, a.rotate[KIND] != 0, a.offset != 0, live, lane, codes + row * (D / 2), params + row * 2);
+      }
+    }
+  }
+}
+
+// A warp takes up to `iters` groups of one kind of heads of one token. kCache: keys and values too.
+template <int D, typename Tin, typename Tout, bool kCache>
+__global__ void __launch_bounds__(kWarps * 32) heads_kernel(const HeadArgs a) {
+  constexpr int kUnits = 32 * kE / D;  // heads per warp
+  const int lane = threadIdx.x & 31, unit = lane / (D / kE);
   griddep_wait();
   griddep_launch_dependents();
-  // Groups of kUnits heads of one kind, so that a warp does not mix kinds.
-  const int g0 = (a.H[0] + kUnits - 1) / kUnits, g1 = g0 + (a.H[1] + kUnits - 1) / kUnits;
-  const int groups = g1 + (a.H[2] + kUnits - 1) / kUnits;
-  const int parts = (groups + a.iters - 1) / a.iters;
+  const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
+  const int pq = (gq + a.iters - 1) / a.iters, pk = (gk + a.iters - 1) / a.iters, parts = pq + 2 * pk;
   const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
   const int64_t t = w / parts;
   if (t >= a.T) return;
-  const int first = static_cast<int>(w % parts) * a.iters, last = min(groups, first + a.iters);
-
-  Angles ang = {};
-  bool pos_ok = true;
-  if (a.rot != 0 && first < g1) {
-    const int64_t p = __ldg(a.pos + t);
-    pos_ok = p >= 0 && p < a.max_pos;
-    if (pos_ok) load_angles<D>(a, a.table + p * a.rot, l * kE, ang);
-  }
-  int64_t slot = -1;
-  if (last > g0) {
-    slot = __ldg(a.slots + t);
-    if (slot >= a.slots_in_cache) {
-      slot = -1;
-      if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-    }
-  }
-  if (!pos_ok && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-
-  for (int g = first; g < last; ++g) {
-    const int kind = g < g0 ? 0 : g < g1 ? 1 : 2;
-    const int h = (g - (kind == 0 ? 0 : kind == 1 ? g0 : g1)) * kUnits + unit;
-    bool live = h < a.H[kind];
-    float v[kE];
-    load8(static_cast<const Tin*>(a.x[kind]) + t * a.ld[kind] + static_cast<int64_t>(live ? h : 0) * D + l * kE, v);
-    if (kind < 2) {
-      if (a.norm[kind] != nullptr) {
-        float sq[kE], wt[kE];
-        load8(a.norm[kind] + static_cast<int64_t>(live ? h : 0) * D + l * kE, wt);
-#pragma unroll
-        for (int e = 0; e < kE; ++e) sq[e] = __fmul_rn(v[e], v[e]);
-        const float mean = __fmul_rn(head_sum<D>(sq), 1.0f / D);
-        const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(mean, a.eps)));
-#pragma unroll
-        for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(__fmul_rn(v[e], inv), wt[e]);
-      }
-      rotary<D>(a, ang, l * kE, lane, v);
-      live = live && pos_ok;
-    }
-    if (kind == 0) {
-      if (a.rotate[0]) {
-        head_hadamard<D>(v, lane);
-#pragma unroll
-        for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(v[e], kRoot);
-      }
-      if (live) store8(static_cast<Tout*>(a.out) + t * a.ld_out + static_cast<int64_t>(h) * D + l * kE, v);
-      continue;
-    }
-    live = live && slot >= 0;
-    const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
-    const int64_t row = (((page * a.H[kind]) + h) << a.page_shift) + at;
-    quantize_head<D>(v, a.rotate[kind] != 0, a.offset != 0, live, lane, a.codes[kind - 1] + (live ? row * (D / 2) : 0),
-                     a.params[kind - 1] + (live ? row * 2 : 0));
+  const int part = static_cast<int>(w % parts);
+  const int first = (part < pq ? part : (part - pq) % max(pk, 1)) * a.iters;
+  const int h0 = first * kUnits + unit;
+  if (part < pq) {
+    run_heads<D, Tin, Tout, 0>(a, t, h0, min(a.iters, gq - first), lane);
+  } else if constexpr (kCache) {
+    if (part < pq + pk)
+      run_heads<D, Tin, Tout, 1>(a, t, h0, min(a.iters, gk - first), lane);
+    else
+      run_heads<D, Tin, Tout, 2>(a, t, h0, min(a.iters, gk - first), lane);
   }
 }
 
@@ -320,54 +370,96 @@ __global__ void __launch_bounds__(kWarps * 32) read_kernel(const ReadArgs a) {
   const int lane = threadIdx.x & 31, l = lane % kLanes, unit = lane / kLanes;
   griddep_wait();
   griddep_launch_dependents();
-  const int groups = (a.H + kUnits - 1) / kUnits, parts = (2 * groups + a.iters - 1) / a.iters;
+  const int groups = (a.H + kUnits - 1) / kUnits, per = (groups + a.iters - 1) / a.iters;
   const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  const int64_t t = w / parts;
+  const int64_t t = w / (2 * per);
   if (t >= a.T) return;
-  int64_t slot = __ldg(a.slots + t);
-  if (slot >= a.slots_in_cache) {
-    slot = -1;
-    if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+  const int part = static_cast<int>(w % (2 * per)), kind = part >= per;
+  Tout* out = static_cast<Tout*>(kind ? a.out[1] : a.out[0]);
+  if (out == nullptr) return;
+  const int first = (part - kind * per) * a.iters, count = min(a.iters, groups - first), h0 = first * kUnits + unit;
+  const int64_t slot = __ldg(a.slots + t);
+  if (slot >= a.slots_in_cache && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+  const bool there = slot >= 0 && slot < a.slots_in_cache, rotate = (kind ? a.rotate[1] : a.rotate[0]) != 0;
+  const int64_t row = there ? (((slot >> a.page_shift) * a.H) << a.page_shift) + (slot & ((1 << a.page_shift) - 1)) : 0;
+  const uint32_t* from = reinterpret_cast<const uint32_t*>((kind ? a.codes[1] : a.codes[0]) + row * (D / 2)) + l;
+  const float2* params = reinterpret_cast<const float2*>(kind ? a.params[1] : a.params[0]) + row;
+  out += t * (kind ? a.ld[1] : a.ld[0]) + l * kE;
+  uint32_t codes[kMostGroups];
+  float2 par[kMostGroups];
+#pragma unroll
+  for (int u = 0; u < kMostGroups; ++u) {
+    const int h = h0 + u * kUnits;
+    codes[u] = 0x88888888u;  // zeros
+    par[u] = make_float2(0.f, 0.f);
+    if (u < count && h < a.H && there) {
+      const int64_t at = static_cast<int64_t>(h) << a.page_shift;
+      codes[u] = __ldg(from + at * (D / 8));
+      par[u] = __ldg(params + at);
+    }
   }
-  const int first = static_cast<int>(w % parts) * a.iters, last = min(2 * groups, first + a.iters);
-  for (int g = first; g < last; ++g) {
-    const int kind = g >= groups;
-    const int h = (g - kind * groups) * kUnits + unit;
-    const bool live = h < a.H;
-    if (a.out[kind] == nullptr) continue;
-    float v[kE] = {};
-    if (live && slot >= 0) {
-      const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
-      const int64_t row = (((page * a.H) + h) << a.page_shift) + at;
-      const uint32_t c = __ldg(reinterpret_cast<const uint32_t*>(a.codes[kind] + row * (D / 2)) + l);
-      const float2 p = __ldg(reinterpret_cast<const float2*>(a.params[kind]) + row);
 #pragma unroll
-      for (int e = 0; e < kE; ++e)
-        v[e] = __fadd_rn(__fmul_rn(static_cast<float>(static_cast<int>((c >> (4 * e)) & 15u) - 8), p.x), p.y);
-    }
-    if (a.rotate[kind]) {
-      head_hadamard<D>(v, lane);
+  for (int u = 0; u < kMostGroups; ++u) {
+    if (u >= count) break;
+    const int h = h0 + u * kUnits;
+    // Codes q of channels e and e + 4 as halves: the nibble below the exponent of 1024, less its bias.
+    __half2 q[4];
 #pragma unroll
-      for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(v[e], kRoot);
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t x = ((e < 2 ? codes[u] : codes[u] >> 8) & (e & 1 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
+      const __half2 y = *reinterpret_cast<const __half2*>(&x);
+      q[e] = e & 1 ? __hfma2(y, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hsub2(y, __float2half2_rn(1032.f));
     }
-    if (live) store8(static_cast<Tout*>(a.out[kind]) + t * a.ld[kind] + static_cast<int64_t>(h) * D + l * kE, v);
+    float scale = par[u].x, v[kE];
+    if (rotate) {
+      // H of the integers q (sums of at most 128 x 8: exact in halves); the offset meets channel 0 alone.
+      auto both = [](__half2& x, __half2& y) {
+        const __half2 d = __hsub2(x, y);
+        x = __hadd2(x, y);
+        y = d;
+      };
+      both(q[0], q[1]);
+      both(q[2], q[3]);
+      both(q[0], q[2]);
+      both(q[1], q[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[e] = __hfma2(q[e], __halves2half2(__float2half(1.f), __float2half(-1.f)), __lowhigh2highlow(q[e]));
+#pragma unroll
+      for (int m = 1; m < D / kE; m <<= 1) {
+        const __half2 sign = __float2half2_rn((lane & m) ? -1.f : 1.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = __hfma2(sign, q[e], __shfl_xor_sync(kAll, q[e], m));
+      }
+      scale *= kRoot;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = __half22float2(q[e]);
+      v[e] = rotate ? f.x * scale : fmaf(f.x, scale, par[u].y);
+      v[e + 4] = rotate ? f.y * scale : fmaf(f.y, scale, par[u].y);
+    }
+    if (rotate && l == 0) v[0] = fmaf(par[u].y, D * kRoot, v[0]);
+    if (h < a.H) store8(out + h * D, v);
   }
 }
 
 // Groups of heads per warp: several where there are enough warps to fill the chip without it.
 int groups_per_warp(int64_t T, int groups, int sms) {
   const int64_t per = T * groups / (static_cast<int64_t>(sms) * 64);
-  return static_cast<int>(std::clamp<int64_t>(per, 1, 8));
+  return static_cast<int>(std::clamp<int64_t>(per, 1, kMostGroups));
 }
 
 template <int D, typename Tin, typename Tout>
 int launch_heads(HeadArgs a, int sms, cudaStream_t s) {
   constexpr int kUnits = 32 * kE / D;
-  const int groups = (a.H[0] + kUnits - 1) / kUnits + (a.H[1] + kUnits - 1) / kUnits + (a.H[2] + kUnits - 1) / kUnits;
-  a.iters = groups_per_warp(a.T, groups, sms);
-  const int64_t warps = a.T * ((groups + a.iters - 1) / a.iters), blocks = (warps + kWarps - 1) / kWarps;
+  const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
+  a.iters = groups_per_warp(a.T, gq + 2 * gk, sms);
+  const int64_t parts = (gq + a.iters - 1) / a.iters + 2 * ((gk + a.iters - 1) / a.iters);
+  const int64_t warps = a.T * parts, blocks = (warps + kWarps - 1) / kWarps;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
-  return launch_pdl(heads_kernel<D, Tin, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kWarps * 32), 0, s, a);
+  const dim3 grid(static_cast<unsigned>(blocks)), block(kWarps * 32);
+  return a.H[1] > 0 ? launch_pdl(heads_kernel<D, Tin, Tout, true>, grid, block, 0, s, a)
+                    : launch_pdl(heads_kernel<D, Tin, Tout, false>, grid, block, 0, s, a);
 }
 
 template <int D, typename Tin>
@@ -400,9 +492,9 @@ int run_heads(HeadArgs& a, int dtype, int out_dtype, int head_dim, void* stream)
 template <int D, typename Tout>
 int launch_read(ReadArgs a, int sms, cudaStream_t s) {
   constexpr int kUnits = 32 * kE / D;
-  const int groups = 2 * ((a.H + kUnits - 1) / kUnits);
-  a.iters = groups_per_warp(a.T, groups, sms);
-  const int64_t warps = a.T * ((groups + a.iters - 1) / a.iters), blocks = (warps + kWarps - 1) / kWarps;
+  const int groups = (a.H + kUnits - 1) / kUnits;
+  a.iters = groups_per_warp(a.T, 2 * groups, sms);
+  const int64_t warps = a.T * 2 * ((groups + a.iters - 1) / a.iters), blocks = (warps + kWarps - 1) / kWarps;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
   return launch_pdl(read_kernel<D, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kWarps * 32), 0, s, a);
 }
