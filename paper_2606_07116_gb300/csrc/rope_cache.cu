@@ -326,7 +326,7 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
 
 // A warp takes up to `iters` groups of one kind of heads of one token. kCache: keys and values too.
 template <int D, typename Tin, typename Tout, bool kCache>
-__global__ void __launch_bounds__(kWarps * 32) heads_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 4) heads_kernel(const HeadArgs a) {
   constexpr int kUnits = 32 * kE / D;  // heads per warp
   const int lane = threadIdx.x & 31, unit = lane / (D / kE);
   griddep_wait();

@@ -13,6 +13,7 @@ tensors holding the tiled operand layout of include/offq.h.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 import re
@@ -737,6 +738,14 @@ def paged_attention_workspace(Tq: int, Hq: int, H: int, head_dim: int, B: int, m
     return load_library().offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q)
 
 
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int) -> int:
+    need = paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q)
+    if need < 0:
+        raise LookupError  # not kept; the call itself says what is wrong with its sizes
+    return need
+
+
 def offq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: int, Hq: int, H: int, head_dim: int,
                           ld_q: int, ld_k: int, ld_v: int, cu: torch.Tensor, B: int, scale: float, causal: bool,
                           out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor], stream=None) -> None:
@@ -867,9 +876,12 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
         raise ValueError("out has q's shape and type")
     else:
         ld_out = _heads(out)[3]
-    need = paged_attention_workspace(Tq, Hq, H, hd, B, max_q)
-    if workspace is None and need > 0:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+    if workspace is None:
+        try:
+            need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q)
+        except LookupError:
+            need = 0
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None
     stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
     offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table,
                          ld_table if B > 1 else width, lens, cu_q, B, max_q,
