@@ -268,10 +268,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     uint32_t to_chunk[4];  // of this lane's four words in a tile (kRowsPer is a multiple of 8: the swizzle is the same in all reps)
 #pragma unroll
     for (int k = 0; k < 4; ++k) to_chunk[k] = tile_off(row, 4 * c + k);
-    uint4 kc[kReps], vc[kReps];
-    float2 kp, vp;
+    struct Held {  // a block's codes and parameters in registers
+      uint4 kc[kReps], vc[kReps];
+      float2 kp, vp;
+      uint32_t absent;  // reps whose rows have no page
+    };
     int page[kReps], next_page[kReps];
-    uint32_t absent = 0;  // reps whose rows have no page
     Walk at;              // the block whose pages were found last
     int head = 0, first = 0, len = 0, next_head = 0, next_first = 0, next_len = 0;  // of the block to load, and after it
     auto find_pages = [&]() {  // of block `at`
@@ -299,97 +301,93 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       const int tok = first + kRowsPer * i + row;
       return ((static_cast<int64_t>(page[i]) * a.H + head) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
     };
-    auto load_keys = [&]() {  // and both parameters
-      absent = 0;
-      kp = vp = make_float2(0.f, 0.f);
+    auto load = [&](Held& x) {
+      x.absent = 0;
+      x.kp = x.vp = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kReps; ++i) {
         const int tok = first + kRowsPer * i + row;
-        kc[i] = make_uint4(0u, 0u, 0u, 0u);
+        x.kc[i] = x.vc[i] = make_uint4(0u, 0u, 0u, 0u);
         if (page[i] < 0 || page[i] >= a.pages) {
-          page[i] = -1;
           if ((tok & ~7) < len) {
-            absent |= 1u << i;
+            x.absent |= 1u << i;
             *a.status = OFFQ_ERR_INVALID_ARG;
           }
           continue;
         }
         const int64_t r = slot_of(i);
-        kc[i] = __ldg(reinterpret_cast<const uint4*>(a.k_codes + r * (D / 2)) + c);
+        x.kc[i] = __ldg(reinterpret_cast<const uint4*>(a.k_codes + r * (D / 2)) + c);
+        x.vc[i] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + r * (D / 2)) + c);
         if (i == c && tok < len) {
-          kp = __ldg(reinterpret_cast<const float2*>(a.k_params) + r);
-          vp = __ldg(reinterpret_cast<const float2*>(a.v_params) + r);
+          x.kp = __ldg(reinterpret_cast<const float2*>(a.k_params) + r);
+          x.vp = __ldg(reinterpret_cast<const float2*>(a.v_params) + r);
         }
       }
     };
-    auto load_values = [&]() {
-#pragma unroll
-      for (int i = 0; i < kReps; ++i) {
-        vc[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (page[i] >= 0)
-          vc[i] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + slot_of(i) * (D / 2)) + c);
-      }
-    };
     const float sc = a.scale * kLog2e;
+    Held held[2];
     if (count > 0) {
       at.start(a, ctrl);
       find_pages();
       take_pages();
-      load_keys();
-      load_values();
+      load(held[0]);
       if (count > 1) step();
     }
-    for (int gb = 0; gb < count; ++gb) {
-      const int slot = gb & 1;
-      const bool more = gb + 1 < count;
-      if (more) take_pages();
-      if (gb >= 2 && !wait(&ctrl->k_empty[slot], (gb >> 1) - 1)) break;
-      const uint32_t kt = base + L::kKeys + slot * L::kTileBytes, vt = base + L::kValues + slot * L::kTileBytes;
-      auto widened = [&](uint32_t tile, const uint4& x, int i, auto is_v) {
-        const uint32_t wd[4] = {x.x, x.y, x.z, x.w};
+    auto widened = [&](uint32_t tile, const uint4& x, int i, auto is_v) {
+      const uint32_t wd[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t to = tile + to_chunk[k] + i * kRowsPer * 128;
-          if constexpr (is_v.value) {
-            uint32_t q[4];
-            widen_signed(wd[k], q[0], q[1]);
-            widen_signed(wd[k] >> 8, q[2], q[3]);
-            sts128(to, q[0], q[1], q[2], q[3]);
-          } else {
-            sts128(to, widen<T>(wd[k], 0), widen<T>(wd[k], 1), widen<T>(wd[k], 2), widen<T>(wd[k], 3));
-          }
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t to = tile + to_chunk[k] + i * kRowsPer * 128;
+        if constexpr (is_v.value) {
+          uint32_t q[4];
+          widen_signed(wd[k], q[0], q[1]);
+          widen_signed(wd[k] >> 8, q[2], q[3]);
+          sts128(to, q[0], q[1], q[2], q[3]);
+        } else {
+          sts128(to, widen<T>(wd[k], 0), widen<T>(wd[k], 1), widen<T>(wd[k], 2), widen<T>(wd[k], 3));
         }
-      };
-#pragma unroll
-      for (int i = 0; i < kReps; ++i) widened(kt, kc[i], i, std::false_type{});
-      {
-        float* pk = reinterpret_cast<float*>(smem + L::kParK + slot * 1024) + (par_row >> 1) * 4 + (par_row & 1);
-        float* pv = reinterpret_cast<float*>(smem + L::kParV + slot * 1024) + (par_row >> 1) * 4 + (par_row & 1);
-        pk[0] = kp.x * sc;
-        pk[2] = fmaf(-24.f, kp.x * sc, kp.y * sc);
-        pv[0] = vp.x;
-        pv[2] = vp.y;
       }
-      float top = vp.x;
+    };
+    // Block gb from x; the next one's reads go out first, and have the whole block's time.
+    auto widen_block = [&](int gb, const Held& x, Held& next) {
+      const int slot = gb & 1;
+      if (gb + 1 < count) {
+        take_pages();
+        load(next);
+      }
+      if (gb + 2 < count) step();
+      if (gb >= 2 && !wait(&ctrl->k_empty[slot], (gb >> 1) - 1)) return false;
+      const uint32_t kt = base + L::kKeys + slot * L::kTileBytes, vt = base + L::kValues + slot * L::kTileBytes;
+#pragma unroll
+      for (int i = 0; i < kReps; ++i) widened(kt, x.kc[i], i, std::false_type{});
+      float* pk = reinterpret_cast<float*>(smem + L::kParK + slot * 1024) + (par_row >> 1) * 4 + (par_row & 1);
+      float* pv = reinterpret_cast<float*>(smem + L::kParV + slot * 1024) + (par_row >> 1) * 4 + (par_row & 1);
+      pk[0] = x.kp.x * sc;
+      pk[2] = fmaf(-24.f, x.kp.x * sc, x.kp.y * sc);
+      pv[0] = x.vp.x;
+      pv[2] = x.vp.y;
+      float top = x.vp.x;
 #pragma unroll
       for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, m));
       if (lane == 0) ctrl->smax[slot][w] = top;
       if (lane % (8 * kChunks) == 0) {
 #pragma unroll
-        for (int i = 0; i < kReps; ++i) ctrl->missing[slot][(kRowsPer * i + row) >> 3] = absent >> i & 1u;
+        for (int i = 0; i < kReps; ++i) ctrl->missing[slot][(kRowsPer * i + row) >> 3] = x.absent >> i & 1u;
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctrl->k_full[slot]));
-      if (more) load_keys();
-      if (gb + 2 < count) step();
-      if (gb >= 2 && !wait(&ctrl->v_empty[slot], (gb >> 1) - 1)) break;
+      if (gb >= 2 && !wait(&ctrl->v_empty[slot], (gb >> 1) - 1)) return false;
 #pragma unroll
-      for (int i = 0; i < kReps; ++i) widened(vt, vc[i], i, std::true_type{});
+      for (int i = 0; i < kReps; ++i) widened(vt, x.vc[i], i, std::true_type{});
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctrl->v_full[slot]));
-      if (more) load_values();
+      return true;
+    };
+    for (int gb = 0; gb < count; gb += 2) {
+      if (!widen_block(gb, held[0], held[1])) break;
+      if (gb + 1 < count && !widen_block(gb + 1, held[1], held[0])) break;
     }
   } else if (warp >= 8) {
     fewer_registers<kIssueRegs>();
