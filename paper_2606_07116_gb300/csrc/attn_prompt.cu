@@ -189,24 +189,34 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
       };
       const int total = above(0);
       int level = 0, higher = 0, at_level = 0;  // tiles above it and at it
+      int taken = 0;  // answers so far; negative after a wait that ran out
+      auto take = [&]() {
+        const uint32_t bar = smem_u32(&ctrl->taken);
+        if (lane == 0) {
+          fence_proxy_async_smem();
+          mbar_arrive_expect_tx(bar, 16);
+          take_over(smem_u32(ctrl->answer), bar);
+        }
+        __syncwarp();
+        if (!wait(&ctrl->taken, taken++)) {
+          taken = -1;
+          return -1;
+        }
+        return taken_over(smem_u32(ctrl->answer));
+      };
       bool more = true;
       for (int k = 0; more; ++k) {
         int at = blockIdx.x;
         if (k > 0) {
           // All warps have begun the last item: take over another CTA's.
           if (!wait(&ctrl->item_empty, k - 1)) break;
-          const uint32_t bar = smem_u32(&ctrl->taken);
-          if (lane == 0) {
-            fence_proxy_async_smem();
-            mbar_arrive_expect_tx(bar, 16);
-            take_over(smem_u32(ctrl->answer), bar);
-          }
-          __syncwarp();
-          if (!wait(&ctrl->taken, k - 1)) break;
-          at = taken_over(smem_u32(ctrl->answer));
+          at = take();
         }
+        // The grid is sized by what the lengths could be at most: CTAs past the last item are taken, not started.
+        while (at >= 0 && at / units >= total) at = take();
+        if (taken < 0) break;
         Item found = {0, 0, 0, 0};
-        more = at >= 0 && at / units < total;
+        more = at >= 0;
         if (more) {
           const int rank = static_cast<int>(at / units);
           if (rank < higher || rank >= higher + at_level) {  // another level, with above(lo) > rank >= above(hi)
