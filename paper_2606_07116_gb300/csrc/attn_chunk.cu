@@ -273,52 +273,47 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       float2 kp, vp;
       uint32_t absent;  // reps whose rows have no page
     };
-    int page[kReps], next_page[kReps];
-    Walk at;              // the block whose pages were found last
-    int head = 0, first = 0, len = 0, next_head = 0, next_first = 0, next_len = 0;  // of the block to load, and after it
-    auto find_pages = [&]() {  // of block `at`
-      next_head = at.h;
-      next_first = at.blk * kKt;
-      next_len = at.s.len;
+    struct Pages {  // a block's: head, first token, the sequence's length, the page of this lane's row in each rep
+      int head, first, len, page[kReps];
+    };
+    Pages now, after;  // of the block to load and the one after it
+    Walk at;           // the block whose pages were found last
+    auto find_pages = [&](Pages& x) {  // of block `at`
+      x.head = at.h;
+      x.first = at.blk * kKt;
+      x.len = at.s.len;
 #pragma unroll
       for (int i = 0; i < kReps; ++i) {
-        const int tok = next_first + kRowsPer * i + (row & ~7);
-        next_page[i] = tok < next_len ? __ldg(a.table + static_cast<int64_t>(at.b) * a.ld_table + (tok >> a.page_shift)) : -1;
+        const int tok = x.first + kRowsPer * i + (row & ~7);
+        x.page[i] = tok < x.len ? __ldg(a.table + static_cast<int64_t>(at.b) * a.ld_table + (tok >> a.page_shift)) : -1;
       }
     };
-    auto take_pages = [&]() {
-      head = next_head;
-      first = next_first;
-      len = next_len;
-#pragma unroll
-      for (int i = 0; i < kReps; ++i) page[i] = next_page[i];
-    };
-    auto step = [&]() {
+    auto step = [&](Pages& x) {
       if (++at.blk == at.blocks) at.next_tile(a);
-      find_pages();
+      find_pages(x);
     };
-    auto slot_of = [&](int i) {
-      const int tok = first + kRowsPer * i + row;
-      return ((static_cast<int64_t>(page[i]) * a.H + head) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
+    auto slot_of = [&](const Pages& x, int i) {
+      const int tok = x.first + kRowsPer * i + row;
+      return ((static_cast<int64_t>(x.page[i]) * a.H + x.head) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
     };
     auto load = [&](Held& x) {
       x.absent = 0;
       x.kp = x.vp = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kReps; ++i) {
-        const int tok = first + kRowsPer * i + row;
+        const int tok = now.first + kRowsPer * i + row;
         x.kc[i] = x.vc[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (page[i] < 0 || page[i] >= a.pages) {
-          if ((tok & ~7) < len) {
+        if (now.page[i] < 0 || now.page[i] >= a.pages) {
+          if ((tok & ~7) < now.len) {
             x.absent |= 1u << i;
             *a.status = OFFQ_ERR_INVALID_ARG;
           }
           continue;
         }
-        const int64_t r = slot_of(i);
+        const int64_t r = slot_of(now, i);
         x.kc[i] = __ldg(reinterpret_cast<const uint4*>(a.k_codes + r * (D / 2)) + c);
         x.vc[i] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + r * (D / 2)) + c);
-        if (i == c && tok < len) {
+        if (i == c && tok < now.len) {
           x.kp = __ldg(reinterpret_cast<const float2*>(a.k_params) + r);
           x.vp = __ldg(reinterpret_cast<const float2*>(a.v_params) + r);
         }
@@ -328,10 +323,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     Held held[2];
     if (count > 0) {
       at.start(a, ctrl);
-      find_pages();
-      take_pages();
+      find_pages(now);
+      if (count > 1) step(after);
       load(held[0]);
-      if (count > 1) step();
     }
     auto widened = [&](uint32_t tile, const uint4& x, int i, auto is_v) {
       const uint32_t wd[4] = {x.x, x.y, x.z, x.w};
@@ -352,10 +346,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     auto widen_block = [&](int gb, const Held& x, Held& next) {
       const int slot = gb & 1;
       if (gb + 1 < count) {
-        take_pages();
+        now = after;
         load(next);
       }
-      if (gb + 2 < count) step();
+      if (gb + 2 < count) step(after);
       if (gb >= 2 && !wait(&ctrl->k_empty[slot], (gb >> 1) - 1)) return false;
       const uint32_t kt = base + L::kKeys + slot * L::kTileBytes, vt = base + L::kValues + slot * L::kTileBytes;
 #pragma unroll
@@ -469,37 +463,53 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       while (left > 0 && ok) {
         const int nb = min(w.blocks - w.blk, left), rows = w.s.n * a.G;
         const int row0 = w.p * kPairRows + i * kQt + quad * 32;   // of this warp
-        const bool active = w.p * kPairRows + i * kQt < rows;
+        // A tile without rows takes no part; a warp without rows in a tile that has some only keeps step.
+        const bool active = w.p * kPairRows + i * kQt < rows, live = row0 < rows;
         float m[4], qs[4];
         float l[4], off[4];
         int least = 0;
-        if (active) {
+        if (active && !live && lane == 0) mbar_arrive(smem_u32(&ctrl->q_full[i]));
+        if (live) {
           // This warp's query rows, in the widened channel order, and their sums.
           constexpr int kCh = D / 8, kPer = 32 / kCh;
-#pragma unroll 4
-          for (int it = 0; it < kCh; ++it) {
-            const int r = it * kPer + lane / kCh, ch = lane % kCh, gr = row0 + r;
-            uint4 u = make_uint4(0u, 0u, 0u, 0u);
-            if (gr < rows)
-              u = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) +
-                                                       (static_cast<int64_t>(w.s.first) + gr / a.G) * a.ld_q +
-                                                       static_cast<int64_t>(w.h * a.G + gr % a.G) * D) + ch);
-            sts128(base + i * L::kTileBytes + tile_off(quad * 32 + r, ch), __byte_perm(u.x, u.z, 0x5410),
-                   __byte_perm(u.x, u.z, 0x7632), __byte_perm(u.y, u.w, 0x5410), __byte_perm(u.y, u.w, 0x7632));
-            const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-            float sum = 0.f;
+          const int ch = lane % kCh, r0 = lane / kCh, dt = kPer / a.G, dg = kPer % a.G;
+          int token = (row0 + r0) / a.G, gh = (row0 + r0) % a.G;
+          const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>(w.s.first) * a.ld_q + static_cast<int64_t>(w.h) * a.G * D + ch * 8;
+#pragma unroll 1
+          for (int it0 = 0; it0 < kCh; it0 += 8) {  // eight rows' reads in flight
+            uint4 u[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if constexpr (kHalf) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[k]));
-                sum += f.x + f.y;
-              } else {
-                sum += __uint_as_float(x[k] << 16) + __uint_as_float(x[k] & 0xFFFF0000u);
+            for (int k = 0; k < 8; ++k) {
+              u[k] = make_uint4(0u, 0u, 0u, 0u);
+              if (row0 + (it0 + k) * kPer + r0 < rows)
+                u[k] = __ldg(reinterpret_cast<const uint4*>(src + token * a.ld_q + gh * D));
+              token += dt;
+              gh += dg;
+              if (gh >= a.G) {
+                gh -= a.G;
+                ++token;
               }
             }
 #pragma unroll
-            for (int k = 1; k < kCh; k <<= 1) sum += __shfl_xor_sync(kAllLanes, sum, k);
-            if (ch == 0) sums[r] = sum;
+            for (int k = 0; k < 8; ++k) {
+              const int r = (it0 + k) * kPer + r0;
+              sts128(base + i * L::kTileBytes + tile_off(quad * 32 + r, ch), __byte_perm(u[k].x, u[k].z, 0x5410),
+                     __byte_perm(u[k].x, u[k].z, 0x7632), __byte_perm(u[k].y, u[k].w, 0x5410), __byte_perm(u[k].y, u[k].w, 0x7632));
+              const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+              float sum = 0.f;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if constexpr (kHalf) {
+                  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[e]));
+                  sum += f.x + f.y;
+                } else {
+                  sum += __uint_as_float(x[e] << 16) + __uint_as_float(x[e] & 0xFFFF0000u);
+                }
+              }
+#pragma unroll
+              for (int e = 1; e < kCh; e <<= 1) sum += __shfl_xor_sync(kAllLanes, sum, e);
+              if (ch == 0) sums[r] = sum;
+            }
           }
           fence_proxy_async_smem();
           __syncwarp();
@@ -517,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           ok = wait(&ctrl->k_full[slot], gb >> 1);
           if (ok && active) ok = wait(&ctrl->s_full[i], ns++);
           if (!ok) break;
-          if (active) {
+          if (live) {
             tc_fence_after();
             const float4* pk = reinterpret_cast<const float4*>(smem + L::kParK + slot * 1024) + c;
             const float4* pv = reinterpret_cast<const float4*>(smem + L::kParV + slot * 1024) + c;
@@ -670,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           }
         }
         if (ok && active) ok = wait(&ctrl->s_full[i], ns++);
-        if (ok && active) {
+        if (ok && live) {
           tc_fence_after();
           const bool complete = w.blk == 0 && nb == w.blocks;
           const int which = w.blk == 0 ? 1 : 0;
