@@ -10,8 +10,8 @@
 // in shared memory at the CTA's end, and what crosses CTAs in a second small kernel (at most a first and a
 // last part per CTA: the workspace does not grow with the batch).
 //
-// A warp stages its tokens itself: one lane issues bulk copies (a head's tokens of a page are contiguous) into
-// a ring of its own, and all lanes read fragments for warp-level MMAs of 16 tokens:
+// A warp stages its tokens itself, by asynchronous copies of 16 bytes a lane (a head's tokens of a page are contiguous)
+// into a ring of its own, and all lanes read fragments for warp-level MMAs of 16 tokens:
 //   S^T [tokens x rows]  = codes K [16 x 16 channels] * Q^T [16 channels x 8 rows]
 //   O^T [channels x rows] += codes V^T [16 channels x 16 tokens] * P^T [16 tokens x 8 rows]
 // with the rows on the MMA's 8-wide side, as there are few. Channels may be contracted in any order and tokens
@@ -57,12 +57,10 @@ struct FewLayout {
 // Control block behind the parts.
 template <int D, int NT>
 struct FewCtrl {
-  uint64_t full[FewLayout<D, NT>::kWarps * FewLayout<D, NT>::kStages];
   long long scan[FewLayout<D, NT>::kWarps];
   long long start[FewLayout<D, NT>::kWarps];  // unit offset inside sequence seq
   int seq[FewLayout<D, NT>::kWarps];
   int4 part[2 * FewLayout<D, NT>::kWarps];    // (sequence or -1, head, first stage, last stage) of each part
-  int abort;
 };
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool half) {
@@ -113,10 +111,14 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
+// 16 bytes to shared memory, past the L1; a warp's copies up to commit() are one group.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_but() {  // for all groups but the last N
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 template <int W>
@@ -194,13 +196,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   auto* ctrl = reinterpret_cast<FewCtrl<D, NT>*>(smem + L::kCtrlOff);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   const uint32_t ring = smem_u32(smem) + warp * L::kRing;
-  const uint32_t bars = smem_u32(ctrl->full + warp * L::kStages);
-  if (lane == 0) {
-    for (int i = 0; i < L::kStages; ++i) mbar_init(bars + 8 * i, 1);
-    mbar_fence_init();
-  }
   if (tid < 2 * L::kWarps) ctrl->part[tid] = make_int4(-1, 0, 0, 0);
-  if (tid == 0) ctrl->abort = 0;
   griddep_wait();
   griddep_launch_dependents();
 
@@ -288,33 +284,34 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
       if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
       return static_cast<int64_t>(-1);
     };
-    auto copy = [&](uint32_t stage, uint32_t bar, int at, int tokens, int64_t row) {
-      bulk_load(stage + at * (D / 2), a.k_codes + row * (D / 2), tokens * (D / 2), bar);
-      bulk_load(stage + L::kCodeBytes + at * (D / 2), a.v_codes + row * (D / 2), tokens * (D / 2), bar);
-      bulk_load(stage + 2 * L::kCodeBytes + at * 8, a.k_params + row * 2, tokens * 8, bar);
-      bulk_load(stage + 2 * L::kCodeBytes + kTile * 8 + at * 8, a.v_params + row * 2, tokens * 8, bar);
+    auto copy = [&](uint32_t stage, int half, int64_t row) {  // the codes of 16 tokens
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint32_t at = (i * 32 + lane) * 16;
+        copy16(stage + half * 8 * D + at, a.k_codes + row * (D / 2) + at);
+        copy16(stage + L::kCodeBytes + half * 8 * D + at, a.v_codes + row * (D / 2) + at);
+      }
     };
     auto issue = [&](int slot) {
-      const uint32_t stage = ring + slot * L::kStageBytes, bar = bars + 8 * slot;
+      const uint32_t stage = ring + slot * L::kStageBytes;
       const int tok = pt * kTile, in_page = tok & ((1 << a.page_shift) - 1);
-      missing &= ~(3u << (2 * slot));
+      int64_t r0, r1;  // first rows of the stage's halves, or -1
       if (a.page_shift >= 5) {
         if (turn || in_page == 0) page_row = tok < plen ? find_page(tok) : -1;
         turn = false;
-        if (page_row < 0) missing |= 3u << (2 * slot);
-        if (lane == 0) {
-          mbar_arrive_expect_tx(bar, page_row < 0 ? 0 : kTile * (D + 16));
-          if (page_row >= 0) copy(stage, bar, 0, kTile, page_row + in_page);
-        }
+        r0 = page_row < 0 ? -1 : page_row + in_page;
+        r1 = page_row < 0 ? -1 : r0 + 16;
       } else {  // two pages of 16 tokens
-        const int64_t r0 = tok < plen ? find_page(tok) : -1, r1 = tok + 16 < plen ? find_page(tok + 16) : -1;
-        missing |= ((r0 < 0 ? 1u : 0u) | (r1 < 0 ? 2u : 0u)) << (2 * slot);
-        if (lane == 0) {
-          mbar_arrive_expect_tx(bar, (r0 < 0 ? 0 : 16 * (D + 16)) + (r1 < 0 ? 0 : 16 * (D + 16)));
-          if (r0 >= 0) copy(stage, bar, 0, 16, r0);
-          if (r1 >= 0) copy(stage, bar, 16, 16, r1);
-        }
+        r0 = tok < plen ? find_page(tok) : -1;
+        r1 = tok + 16 < plen ? find_page(tok + 16) : -1;
       }
+      missing &= ~(3u << (2 * slot));
+      missing |= ((r0 < 0 ? 1u : 0u) | (r1 < 0 ? 2u : 0u)) << (2 * slot);
+      if (r0 >= 0) copy(stage, 0, r0);
+      if (r1 >= 0) copy(stage, 1, r1);
+      // Scale and offset pairs: 8 lanes for the keys of each half, 8 for the values.
+      const int64_t r = lane & 8 ? r1 : r0;
+      if (r >= 0) copy16(stage + 2 * L::kCodeBytes + lane * 16, (lane & 16 ? a.v_params : a.k_params) + r * 2 + (lane & 7) * 4);
       if (--ahead > 0 && ++pt == pstages) {
         pt = 0;
         turn = true;
@@ -330,7 +327,11 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         }
       }
     };
-    for (int i = 0; i < L::kStages && ahead > 0; ++i) issue(i);
+#pragma unroll
+    for (int i = 0; i < L::kStages; ++i) {
+      if (ahead > 0) issue(i);
+      commit();
+    }
 
     const int tok_k = (g & ~1) + ((g & 1) ^ ((g >> 1) & 1));              // token of score row g (of 8)
     const int tok_v0 = 2 * c + (c & 1), tok_v1 = 2 * c + 1 - (c & 1);     // tokens of weight rows 2c, 2c + 1
@@ -387,8 +388,8 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             for (int k = 0; k < 4; ++k) o[nt][mt][k] = 0.f;
         }
       }
-      // All lanes go on together or none does.
-      if (!__all_sync(kAllLanes, mbar_wait(bars + 8 * slot, (it / L::kStages) & 1, &ctrl->abort))) break;
+      wait_but<L::kStages - 1>();
+      __syncwarp();
       const uint32_t stage = ring + slot * L::kStageBytes;
       const uint32_t gone = missing >> (2 * slot) & 3u;
 
@@ -526,6 +527,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
       }
       __syncwarp();
       if (ahead > 0) issue(slot);
+      commit();  // with nothing in it too: a stage is as many groups back as the ring is long
 
       ++t;
       if (t < stages && it + 1 < todo) continue;
@@ -577,15 +579,6 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             stages = stages_of(a, s);
           } while (stages == 0);
         }
-      }
-    }
-    if (ctrl->abort) {  // copies in flight land before the CTA ends
-      if (lane == 0) {
-        for (int i = 0; i < L::kStages; ++i) {
-          const int last = (todo - ahead - 1 - i) / L::kStages;  // uses of slot i issued so far, less one
-          if (todo - ahead > i) mbar_wait_teardown(bars + 8 * i, last & 1);
-        }
-        *a.status = OFFQ_ERR_TIMEOUT;
       }
     }
   }
@@ -673,7 +666,6 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int c
   }
   __syncthreads();
   const int last = s_last;
-  if (last >= ctas) return;  // a CTA gave up: the status word says so
   const int rows = p.rows, h = p.id % a.H;
   for (int u = tid; u < rows * (D / 8); u += blockDim.x) {
     const int r = u / (D / 8), d = u % (D / 8) * 8;
