@@ -746,6 +746,16 @@ def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: in
     return need
 
 
+def _workspace(need: int, device: torch.device, stream) -> torch.Tensor:
+    """``need`` bytes whose memory, once let go, is taken again only behind the work of the call's stream."""
+    if stream is None:
+        return torch.empty((need,), dtype=torch.uint8, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device)
+    with torch.cuda.stream(stream):
+        return torch.empty((need,), dtype=torch.uint8, device=device)
+
+
 def offq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: int, Hq: int, H: int, head_dim: int,
                           ld_q: int, ld_k: int, ld_v: int, cu: torch.Tensor, B: int, scale: float, causal: bool,
                           out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor], stream=None) -> None:
@@ -881,7 +891,7 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
             need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q)
         except LookupError:
             need = 0
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None
+        workspace = _workspace(need, q.device, stream) if need > 0 else None
     stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
     offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table,
                          ld_table if B > 1 else width, lens, cu_q, B, max_q,
