@@ -746,13 +746,18 @@ def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: in
     return need
 
 
+def _on(stream, device: torch.device):
+    """Context in which torch takes memory from, and runs behind, the call's stream (None: the current one)."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device)
+    return torch.cuda.stream(stream)
+
+
 def _workspace(need: int, device: torch.device, stream) -> torch.Tensor:
     """``need`` bytes whose memory, once let go, is taken again only behind the work of the call's stream."""
     if stream is None:
         return torch.empty((need,), dtype=torch.uint8, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device)
-    with torch.cuda.stream(stream):
+    with _on(stream, device):
         return torch.empty((need,), dtype=torch.uint8, device=device)
 
 
@@ -879,6 +884,13 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
     ld_table, inner = block_table.stride()
     if block_table.dtype is not torch.int32 or listed != B or (width > 1 and inner != 1):
         raise ValueError("block_table must be int32 [B, width] with contiguous rows")
+    if B > 1 and ld_table != width and (
+            ld_table < width or block_table.storage_offset() + B * ld_table > block_table.untyped_storage().nbytes() // 4):
+        # Rows of one another, or a last row whose ld_table entries pass the end of its memory: the kernels allow
+        # lengths of ld_table pages.
+        with _on(stream, q.device):
+            block_table = block_table.contiguous()
+        ld_table = width
     ld_out = Hq * hd
     if out is None:
         out = torch.empty((Tq, Hq, hd), dtype=q.dtype, device=q.device)

@@ -103,3 +103,21 @@ def test_threads_on_one_stream():
     for t in threads:
         t.join()
     assert wrong == []
+
+
+def test_tables_that_are_views():
+    """Columns from the middle of a wider table, whose last row ends with its memory, and one row for all sequences."""
+    q, cache, table, _, _, _ = _inputs(5, 3, L=400)
+    q = q.contiguous()
+    cu = torch.arange(4, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([400, 77, 399], dtype=torch.int32, device="cuda")
+    want = Q.paged_attention(q, cache, table.repeat(3, 1), lens, cu, 1)
+    wide = torch.full((3, table.shape[1] + 9), -1, dtype=torch.int32, device="cuda")
+    wide[:, 9:] = table
+    for view in (wide[:, 9:], table.expand(3, -1)):
+        assert torch.equal(Q.paged_attention(q, cache, view, lens, cu, 1), want)
+        assert torch.equal(Q.paged_attention(q, cache, view, lens, cu, 1, stream=torch.cuda.current_stream()), want)
+        assert Q.offq_get_device_status() == Q.OFFQ_OK
+        # A length that the view's pages do not hold is an error, not a read of what lies behind them.
+        Q.paged_attention(q, cache, view, lens + 16, cu, 1)
+        assert Q.offq_get_device_status() == Q.OFFQ_ERR_INVALID_ARG
