@@ -22,6 +22,11 @@
 //
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 finds the CTA's work, warps
 // 12-15 widen.
+//
+// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 592 us, 815 TFLOP/s; 16 sequences of
+// 8 tokens over 500 to 6000 122 us. What bounds it: with softmax, widening and reads left out the products take 341 us, since S has
+// both operands in shared memory, which delivers them at 77 % of the tensor rate; reads add about 80, widening 50, the
+// softmax 130. 16 softmax warps of 16 rows were slower (671 against 640), as were maxima taken before the weights (901).
 #include <algorithm>
 #include <cstddef>
 

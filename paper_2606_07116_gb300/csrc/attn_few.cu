@@ -24,6 +24,12 @@
 // O summed with P' = p s_v as halves, p = 2^(z - m). The reference m follows the largest z_j + log2(s_v), so that P'
 // fits a half whatever the values' size; it moves only when some P' passes 2^8 (or p 2^32). Scores are taken relative
 // to it as they are made; a stage that must move it, or has tokens that some row does not see, does its softmax again.
+//
+// Copies of 16 bytes a lane rather than one lane's bulk copies: those cost more instructions than they save (4 streams of 65536
+// tokens 233 against 212 us; pages of 16 tokens, 64 streams of 1 to 8191, 96 against 84). 16 warps of 8 rows (128 registers, two
+// stages each) or 8 of 16 rows (250, four stages): more warps spill (12 of 16 rows: 50 us where 8 take 36).
+// Measured: 4 x 65536 tokens, 32 heads of 128: 212 us, 5.7 TB/s, integer pipe and issue slots at 60 %. 64 streams of 1 to 8191,
+// 64 heads on 8: 84 us, 4.0 TB/s, 17 us of them whatever the lengths. 16 x 4 tokens over 500 to 6000: 36 us.
 #include <algorithm>
 #include <type_traits>
 

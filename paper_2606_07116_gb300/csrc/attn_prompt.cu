@@ -19,6 +19,11 @@
 //
 // Rows past a sequence's end are the next sequence's. As queries they are not written, as keys their
 // scores are replaced, and as values they are zeroed in shared memory (0 times infinity is not 0).
+//
+// Measured (causal): one prompt of 8192, 32 heads on 8 of 128, bf16: 388 us, 1416 TFLOP/s, tensor pipe 58 % on a prompt of 4096;
+// S with both operands in shared memory runs at 77 % of the tensor rate at best. 24 prompts of 5 to 2000, 16 heads on 4 of
+// 64, f16: 125 us, 680 TFLOP/s: 1.33 us a block of 128 keys and about 2 us an item, latency and not any one pipe (exponentials
+// 28 %). Without taking over items 151 us; with two threads a row 148.
 #include <algorithm>
 
 #include "attn_tc.cuh"
