@@ -130,130 +130,197 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[kE]) {
   }
 }
 
+// A lane's channels of a head on its way in: 8 l + e in the low half of v[e], D / 2 + 8 l + e in the high half. Two
+// operations at once, each rounded as a single one is.
+using Pairs = uint64_t[kE];
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t shfl_xor2(uint64_t v, int m) {
+  float x, y;
+  unpack2(v, x, y);
+  return pack2(__shfl_xor_sync(kAll, x, m), __shfl_xor_sync(kAll, y, m));
+}
+__device__ __forceinline__ void pairs_of(const float (&lo)[kE], const float (&hi)[kE], Pairs& v) {
+#pragma unroll
+  for (int e = 0; e < kE; ++e) v[e] = pack2(lo[e], hi[e]);
+}
+
 // Sum of a head's channels, neighbours first, in every lane of the head.
 template <int D>
-__device__ __forceinline__ float head_sum(const float (&v)[kE]) {
-  float s = __fadd_rn(__fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3])),
-                      __fadd_rn(__fadd_rn(v[4], v[5]), __fadd_rn(v[6], v[7])));
+__device__ __forceinline__ float head_sum(const Pairs& v) {
+  uint64_t s = add2(add2(add2(v[0], v[1]), add2(v[2], v[3])), add2(add2(v[4], v[5]), add2(v[6], v[7])));
 #pragma unroll
-  for (int m = 1; m < D / kE; m <<= 1) s = __fadd_rn(s, __shfl_xor_sync(kAll, s, m));
-  return s;
+  for (int m = 1; m < D / (2 * kE); m <<= 1) s = add2(s, shfl_xor2(s, m));
+  float x, y;
+  unpack2(s, x, y);
+  return __fadd_rn(x, y);
 }
 
 template <int D>
-__device__ __forceinline__ float head_absmax(const float (&v)[kE]) {
+__device__ __forceinline__ float head_absmax(const Pairs& v) {
   float s = 0.f;
 #pragma unroll
-  for (int e = 0; e < kE; ++e) s = fmaxf(s, fabsf(v[e]));
+  for (int e = 0; e < kE; ++e) {
+    float x, y;
+    unpack2(v[e], x, y);
+    asm("max.f32 %0, %0, %1, %2;" : "+f"(s) : "f"(fabsf(x)), "f"(fabsf(y)));
+  }
 #pragma unroll
-  for (int m = 1; m < D / kE; m <<= 1) s = fmaxf(s, __shfl_xor_sync(kAll, s, m));
+  for (int m = 1; m < D / (2 * kE); m <<= 1) s = fmaxf(s, __shfl_xor_sync(kAll, s, m));
   return s;
 }
 
-// x H_D, not normalised. Channels e and e + 4 of a lane go through packed additions together.
+// x H_D, not normalised.
 template <int D>
-__device__ __forceinline__ void head_hadamard(float (&v)[kE], int lane) {
-  butterfly2(v[0], v[4], v[1], v[5]);
-  butterfly2(v[2], v[6], v[3], v[7]);
-  butterfly2(v[0], v[4], v[2], v[6]);
-  butterfly2(v[1], v[5], v[3], v[7]);
+__device__ __forceinline__ void head_hadamard(Pairs& v, int lane) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float x = v[e], y = v[e + 4];
-    v[e] = __fadd_rn(x, y);
-    v[e + 4] = __fsub_rn(x, y);
+  for (int d = 1; d < kE; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+      if ((e & d) == 0) {
+        const uint64_t x = v[e], y = v[e + d];
+        v[e] = add2(x, y);
+        v[e + d] = sub2(x, y);
+      }
+#pragma unroll
+  for (int m = 1; m < D / (2 * kE); m <<= 1) {
+    const float sign = (lane & m) ? -1.f : 1.f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) v[e] = fma2v(pack2(sign, sign), v[e], shfl_xor2(v[e], m));  // the product with +-1 is exact
   }
 #pragma unroll
-  for (int m = 1; m < D / kE; m <<= 1) {
-    const float sign = (lane & m) ? -1.f : 1.f;
-    const uint64_t sign2 = pack2(sign, sign);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint64_t o = pack2(__shfl_xor_sync(kAll, v[e], m), __shfl_xor_sync(kAll, v[e + 4], m));
-      unpack2(fma2v(sign2, pack2(v[e], v[e + 4]), o), v[e], v[e + 4]);  // o + v or o - v: the product with +-1 is exact
-    }
+  for (int e = 0; e < kE; ++e) {
+    float x, y;
+    unpack2(v[e], x, y);
+    v[e] = pack2(__fadd_rn(x, y), __fsub_rn(x, y));
   }
 }
 
-// Cosines and sines of this lane's channels. Pairs of two lanes: x c + y s with the sine's sign taken in, 1 and 0
-// past the rotated channels; neighbouring pairs: the first four of each.
+// Cosines and sines of this lane's channels. Neighbouring pairs: four of the low channels, four of the high ones.
+// Pairs half the rotated channels apart: those of the low channels, x c + y s with the sine's sign taken in; the high channels'
+// are the same with the other sign where all channels rotate, and else are read when they are needed. 1 and 0
+// past the rotated channels.
 struct Angles {
   float c[kE], s[kE];
 };
 
-template <int D>
-__device__ __forceinline__ void load_angles(const HeadArgs& a, const float* row, int d0, Angles& t) {
-  const int half = a.rot / 2;
+// Of the 8 channels from d0 on, in pairs rot / 2 apart.
+__device__ __forceinline__ void half_angles(const float* row, int rot, int d0, Angles& t) {
+  const int half = rot / 2;
+  if (d0 >= rot) {
 #pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    t.c[e] = 1.f;
-    t.s[e] = 0.f;
-  }
-  if (d0 >= a.rot) return;
-  if (a.interleaved) {
-    const float4 c = __ldg(reinterpret_cast<const float4*>(row + d0 / 2));
-    const float4 s = __ldg(reinterpret_cast<const float4*>(row + half + d0 / 2));
-    t.c[0] = c.x; t.c[1] = c.y; t.c[2] = c.z; t.c[3] = c.w;
-    t.s[0] = s.x; t.s[1] = s.y; t.s[2] = s.z; t.s[3] = s.w;
-  } else {
-    const int f = d0 < half ? d0 : d0 - half;
-    load8(row + f, t.c);
-    load8(row + half + f, t.s);
-    if (d0 < half) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e) t.s[e] = -t.s[e];
+    for (int e = 0; e < kE; ++e) {
+      t.c[e] = 1.f;
+      t.s[e] = 0.f;
     }
+    return;
+  }
+  const int f = d0 < half ? d0 : d0 - half;
+  load8(row + f, t.c);
+  load8(row + half + f, t.s);
+  if (d0 < half) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) t.s[e] = -t.s[e];
   }
 }
 
-// `partner`: the lane of the other half of this lane's pairs (rot_dim is a multiple of 16: same element).
 template <int D>
-__device__ __forceinline__ void rotary(bool interleaved, const Angles& t, int partner, float (&v)[kE]) {
-  if (interleaved) {
+__device__ __forceinline__ void load_angles(const HeadArgs& a, const float* row, int l, Angles& t) {
+  if (!a.interleaved) return half_angles(row, a.rot, l * kE, t);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int d0 = i * (D / 2) + l * kE;
+    float4 c = make_float4(1.f, 1.f, 1.f, 1.f), s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (d0 < a.rot) {
+      c = __ldg(reinterpret_cast<const float4*>(row + d0 / 2));
+      s = __ldg(reinterpret_cast<const float4*>(row + a.rot / 2 + d0 / 2));
+    }
+    t.c[4 * i] = c.x; t.c[4 * i + 1] = c.y; t.c[4 * i + 2] = c.z; t.c[4 * i + 3] = c.w;
+    t.s[4 * i] = s.x; t.s[4 * i + 1] = s.y; t.s[4 * i + 2] = s.z; t.s[4 * i + 3] = s.w;
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void rotary(const HeadArgs& a, const float* row, const Angles& t, int lane, Pairs& v) {
+  constexpr int kLanes = D / (2 * kE);
+  if (a.interleaved) {
 #pragma unroll
     for (int m = 0; m < kE / 2; ++m) {
-      const float x = v[2 * m], y = v[2 * m + 1];
-      v[2 * m] = __fsub_rn(__fmul_rn(x, t.c[m]), __fmul_rn(y, t.s[m]));
-      v[2 * m + 1] = __fadd_rn(__fmul_rn(y, t.c[m]), __fmul_rn(x, t.s[m]));
+      const uint64_t x = v[2 * m], y = v[2 * m + 1], c = pack2(t.c[m], t.c[4 + m]), s = pack2(t.s[m], t.s[4 + m]);
+      v[2 * m] = sub2(mul2v(x, c), mul2v(y, s));
+      v[2 * m + 1] = add2(mul2v(y, c), mul2v(x, s));
     }
-  } else {
+  } else if (a.rot == D) {  // both channels of a pair are this lane's
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
-      const float o = __shfl_sync(kAll, v[e], partner);
-      v[e] = __fadd_rn(__fmul_rn(v[e], t.c[e]), __fmul_rn(o, t.s[e]));
+      float x, y;
+      unpack2(v[e], x, y);
+      v[e] = add2(mul2v(v[e], pack2(t.c[e], t.c[e])), mul2v(pack2(y, x), pack2(t.s[e], -t.s[e])));
+    }
+  } else {  // rot is a multiple of 16: a pair's other channel is the same element of another eight
+    const int l = lane % kLanes, n = a.rot / (2 * kE), base = lane - l;
+    auto other = [&](int o) { return o < n ? o + n : o < 2 * n ? o - n : o; };
+    const int p0 = other(l), p1 = other(l + kLanes);
+    Angles u;
+    half_angles(row, a.rot, D / 2 + l * kE, u);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      float x, y;
+      unpack2(v[e], x, y);
+      const float a0 = __shfl_sync(kAll, x, base + p0 % kLanes), b0 = __shfl_sync(kAll, y, base + p0 % kLanes);
+      const float a1 = __shfl_sync(kAll, x, base + p1 % kLanes), b1 = __shfl_sync(kAll, y, base + p1 % kLanes);
+      const uint64_t o = pack2(p0 < kLanes ? a0 : b0, p1 < kLanes ? a1 : b1);
+      v[e] = add2(mul2v(v[e], pack2(t.c[e], u.c[e])), mul2v(o, pack2(t.s[e], u.s[e])));
     }
   }
 }
 
 // Codes of a head y (before H3 where `rotate`) into its slot.
 template <int D>
-__device__ __forceinline__ void quantize_head(float (&v)[kE], bool rotate, bool offset, bool live, int lane,
-                                              uint8_t* codes, float* params) {
+__device__ __forceinline__ void quantize_head(Pairs& v, bool rotate, bool offset, bool live, int lane, uint8_t* codes,
+                                              float* params) {
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;  // 1 / sqrt(D) in fp32
-  const int l = lane % (D / kE);
+  constexpr int kLanes = D / (2 * kE);
+  const int l = lane % kLanes;
   float o = 0.f;
   if (rotate) {
     if (offset) {
-      o = __fmul_rn(__shfl_sync(kAll, v[0], lane - l), kRoot);
-      if (l == 0) v[0] = 0.f;  // the first row of H_D is all ones: without x_0 the mean is 0
+      float x, y;
+      unpack2(v[0], x, y);
+      o = __fmul_rn(__shfl_sync(kAll, x, lane - l), kRoot);
+      if (l == 0) v[0] = pack2(0.f, y);  // the first row of H_D is all ones: without x_0 the mean is 0
     }
     head_hadamard<D>(v, lane);
   } else if (offset) {
     o = __fmul_rn(head_sum<D>(v), 1.0f / D);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) v[e] = __fsub_rn(v[e], o);
+    for (int e = 0; e < kE; ++e) v[e] = sub2(v[e], pack2(o, o));
   }
   const float top = head_absmax<D>(v);
   const float inv = top > 0.f ? __fdiv_rn(7.0f, top) : 0.f;
   // |r inv| <= 7 (1 + 2^-22), so rounding alone keeps the codes in -7 .. 7. Adding 1.5 * 2^23 + 8 rounds to the nearest
   // even integer (the spacing there is 1) and leaves u = q + 8 in the low bits; eight are packed by shifted sums, and
   // what the upper bits add up to is taken off at the end.
-  uint32_t w = 0;
+  uint32_t w0 = 0, w1 = 0;
 #pragma unroll
-  for (int e = kE - 1; e >= 0; --e) w = (w << 4) + __float_as_uint(__fadd_rn(__fmul_rn(v[e], inv), 12582920.0f));
-  w -= 0x4B400000u * 0x11111111u;
+  for (int e = kE - 1; e >= 0; --e) {
+    float x, y;
+    unpack2(add2(mul2v(v[e], pack2(inv, inv)), pack2(12582920.0f, 12582920.0f)), x, y);
+    w0 = (w0 << 4) + __float_as_uint(x);
+    w1 = (w1 << 4) + __float_as_uint(y);
+  }
   if (!live) return;
-  reinterpret_cast<uint32_t*>(codes)[l] = w;
+  reinterpret_cast<uint32_t*>(codes)[l] = w0 - 0x4B400000u * 0x11111111u;
+  reinterpret_cast<uint32_t*>(codes)[l + kLanes] = w1 - 0x4B400000u * 0x11111111u;
   if (l == 0) {
     const float s = rotate ? __fmul_rn(__fmul_rn(top, kRoot), 1.0f / 7.0f) : __fmul_rn(top, 1.0f / 7.0f);
     *reinterpret_cast<float2*>(params) = make_float2(s, o);
@@ -263,19 +330,19 @@ __device__ __forceinline__ void quantize_head(float (&v)[kE], bool rotate, bool 
 // `groups` groups of heads of token t, from head h0 on (this lane's first head). KIND 0: queries, 1: keys, 2: values.
 template <int D, typename Tin, typename Tout, int KIND>
 __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, int groups, int lane) {
-  constexpr int kLanes = D / kE, kUnits = 32 / kLanes;
+  constexpr int kLanes = D / (2 * kE), kUnits = 32 / kLanes;
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
   const int l = lane % kLanes, heads = a.H[KIND];
   const Tin* x = static_cast<const Tin*>(a.x[KIND]) + t * a.ld[KIND] + l * kE;
   bool ok = true;
   Angles ang;
-  int partner = lane;
+  const float* row = nullptr;
   if (KIND < 2 && a.rot != 0) {
     const int64_t p = __ldg(a.pos + t);
     ok = p >= 0 && p < a.max_pos;
     if (!ok && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-    load_angles<D>(a, a.table + (ok ? p : 0) * a.rot, l * kE, ang);
-    if (l * kE < a.rot) partner = lane + (l * kE < a.rot / 2 ? a.rot / 2 / kE : -(a.rot / 2 / kE));
+    row = a.table + (ok ? p : 0) * a.rot;
+    load_angles<D>(a, row, l, ang);
   }
   uint8_t* codes = nullptr;
   float* params = nullptr;
@@ -284,46 +351,62 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
     if (slot >= a.slots_in_cache && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
     ok = ok && slot >= 0 && slot < a.slots_in_cache;
     const int64_t page = slot >> a.page_shift, at = slot & ((1 << a.page_shift) - 1);
-    const int64_t row = ok ? ((page * heads) << a.page_shift) + at : 0;
-    codes = a.codes[KIND - 1] + row * (D / 2);
-    params = a.params[KIND - 1] + row * 2;
+    const int64_t first = ok ? ((page * heads) << a.page_shift) + at : 0;
+    codes = a.codes[KIND - 1] + first * (D / 2);
+    params = a.params[KIND - 1] + first * 2;
   }
   const float* norm = KIND < 2 ? a.norm[KIND == 1] : nullptr;
   for (int base = 0; base < groups; base += kAhead) {
-    Raw8<Tin> raw[kAhead];
+    Raw8<Tin> raw[kAhead][2];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (base + u < groups) read8(x + min(h0 + (base + u) * kUnits, heads - 1) * D, raw[u]);
+      if (base + u < groups) {
+        const Tin* from = x + min(h0 + (base + u) * kUnits, heads - 1) * D;
+        read8(from, raw[u][0]);
+        read8(from + D / 2, raw[u][1]);
+      }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (base + u >= groups) break;
       const int h = h0 + (base + u) * kUnits;
       const bool live = ok && h < heads;
-      float v[kE];
-      widen8(raw[u], v);
+      float lo[kE], hi[kE];
+      Pairs v;
+      widen8(raw[u][0], lo);
+      widen8(raw[u][1], hi);
+      pairs_of(lo, hi, v);
       if (KIND < 2) {
         if (norm != nullptr) {
-          float sq[kE], wt[kE];
-          load8(norm + min(h, heads - 1) * D + l * kE, wt);
+          Pairs wt;
 #pragma unroll
-          for (int e = 0; e < kE; ++e) sq[e] = __fmul_rn(v[e], v[e]);
-          const float mean = __fmul_rn(head_sum<D>(sq), 1.0f / D);
+          for (int e = 0; e < kE; ++e) wt[e] = mul2v(v[e], v[e]);
+          const float mean = __fmul_rn(head_sum<D>(wt), 1.0f / D);
           const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(mean, a.eps)));
+          const float* weights = norm + min(h, heads - 1) * D + l * kE;
+          load8(weights, lo);
+          load8(weights + D / 2, hi);
+          pairs_of(lo, hi, wt);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(__fmul_rn(v[e], inv), wt[e]);
+          for (int e = 0; e < kE; ++e) v[e] = mul2v(mul2v(v[e], pack2(inv, inv)), wt[e]);
         }
-        if (a.rot != 0) rotary<D>(a.interleaved != 0, ang, partner, v);
+        if (a.rot != 0) rotary<D>(a, row, ang, lane, v);
       }
       if constexpr (KIND == 0) {
         if (a.rotate[0]) {
           head_hadamard<D>(v, lane);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[e] = __fmul_rn(v[e], kRoot);
+          for (int e = 0; e < kE; ++e) v[e] = mul2v(v[e], pack2(kRoot, kRoot));
         }
-        if (live) store8(static_cast<Tout*>(a.out) + t * a.ld_out + h * D + l * kE, v);
+        if (live) {
+          Tout* to = static_cast<Tout*>(a.out) + t * a.ld_out + h * D + l * kE;
+#pragma unroll
+          for (int e = 0; e < kE; ++e) unpack2(v[e], lo[e], hi[e]);
+          store8(to, lo);
+          store8(to + D / 2, hi);
+        }
       } else {
-        const int64_t row = static_cast<int64_t>(live ? h : 0) << a.page_shift;
-        quantize_head<D>(v, a.rotate[KIND] != 0, a.offset != 0, live, lane, codes + row * (D / 2), params + row * 2);
+        const int64_t at = static_cast<int64_t>(live ? h : 0) << a.page_shift;
+        quantize_head<D>(v, a.rotate[KIND] != 0, a.offset != 0, live, lane, codes + at * (D / 2), params + at * 2);
       }
     }
   }
@@ -331,9 +414,9 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
 
 // A warp takes up to `iters` groups of one kind of heads of one token. kCache: keys and values too.
 template <int D, typename Tin, typename Tout, bool kCache>
-__global__ void __launch_bounds__(kWarps * 32, 4) heads_kernel(const HeadArgs a) {
-  constexpr int kUnits = 32 * kE / D;  // heads per warp
-  const int lane = threadIdx.x & 31, unit = lane / (D / kE);
+__global__ void __launch_bounds__(kWarps * 32, 3) heads_kernel(const HeadArgs a) {
+  constexpr int kUnits = 64 * kE / D;  // heads per warp
+  const int lane = threadIdx.x & 31, unit = lane / (D / (2 * kE));
   griddep_wait();
   griddep_launch_dependents();
   const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
@@ -456,7 +539,7 @@ int groups_per_warp(int64_t T, int groups, int sms) {
 
 template <int D, typename Tin, typename Tout>
 int launch_heads(HeadArgs a, int sms, cudaStream_t s) {
-  constexpr int kUnits = 32 * kE / D;
+  constexpr int kUnits = 64 * kE / D;
   const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
   a.iters = groups_per_warp(a.T, gq + 2 * gk, sms);
   const int64_t parts = (gq + a.iters - 1) / a.iters + 2 * ((gk + a.iters - 1) / a.iters);
