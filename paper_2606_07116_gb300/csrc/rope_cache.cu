@@ -38,8 +38,7 @@ namespace {
 using namespace offq;
 
 constexpr int kE = 8;        // channels per lane
-constexpr int kWarps = 8;    // warps per CTA
-constexpr int kAhead = 2;    // groups of heads read ahead
+constexpr int kReadWarps = 8;  // warps per CTA of the reading kernel; the others' CTAs are one warp
 constexpr int kMostGroups = 8;  // of a warp
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
@@ -328,7 +327,7 @@ __device__ __forceinline__ void quantize_head(Pairs& v, bool rotate, bool offset
 }
 
 // `groups` groups of heads of token t, from head h0 on (this lane's first head). KIND 0: queries, 1: keys, 2: values.
-template <int D, typename Tin, typename Tout, int KIND>
+template <int D, typename Tin, typename Tout, int KIND, int kAhead>
 __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, int groups, int lane) {
   constexpr int kLanes = D / (2 * kE), kUnits = 32 / kLanes;
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
@@ -414,26 +413,27 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
 
 // A warp takes up to `iters` groups of one kind of heads of one token. kCache: keys and values too.
 template <int D, typename Tin, typename Tout, bool kCache>
-__global__ void __launch_bounds__(kWarps * 32, 3) heads_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(32, kCache ? 28 : 24) heads_kernel(const HeadArgs a) {
   constexpr int kUnits = 64 * kE / D;  // heads per warp
-  const int lane = threadIdx.x & 31, unit = lane / (D / (2 * kE));
+  constexpr int kAhead = kCache ? 1 : 2;  // groups of heads read ahead
+  const int lane = threadIdx.x, unit = lane / (D / (2 * kE));
   griddep_wait();
   griddep_launch_dependents();
   const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
   const int pq = (gq + a.iters - 1) / a.iters, pk = (gk + a.iters - 1) / a.iters, parts = pq + 2 * pk;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t w = blockIdx.x;
   const int64_t t = w / parts;
   if (t >= a.T) return;
   const int part = static_cast<int>(w % parts);
   const int first = (part < pq ? part : (part - pq) % max(pk, 1)) * a.iters;
   const int h0 = first * kUnits + unit;
   if (part < pq) {
-    run_heads<D, Tin, Tout, 0>(a, t, h0, min(a.iters, gq - first), lane);
+    run_heads<D, Tin, Tout, 0, kAhead>(a, t, h0, min(a.iters, gq - first), lane);
   } else if constexpr (kCache) {
     if (part < pq + pk)
-      run_heads<D, Tin, Tout, 1>(a, t, h0, min(a.iters, gk - first), lane);
+      run_heads<D, Tin, Tout, 1, kAhead>(a, t, h0, min(a.iters, gk - first), lane);
     else
-      run_heads<D, Tin, Tout, 2>(a, t, h0, min(a.iters, gk - first), lane);
+      run_heads<D, Tin, Tout, 2, kAhead>(a, t, h0, min(a.iters, gk - first), lane);
   }
 }
 
@@ -452,14 +452,14 @@ struct ReadArgs {
 
 // Values s (u - 8) + o of cached heads, keys taken back by H3 (symmetric and orthonormal: its own inverse).
 template <int D, typename Tout>
-__global__ void __launch_bounds__(kWarps * 32) read_kernel(const ReadArgs a) {
+__global__ void __launch_bounds__(kReadWarps * 32) read_kernel(const ReadArgs a) {
   constexpr int kLanes = D / kE, kUnits = 32 / kLanes;
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
   const int lane = threadIdx.x & 31, l = lane % kLanes, unit = lane / kLanes;
   griddep_wait();
   griddep_launch_dependents();
   const int groups = (a.H + kUnits - 1) / kUnits, per = (groups + a.iters - 1) / a.iters;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int64_t w = static_cast<int64_t>(blockIdx.x) * kReadWarps + (threadIdx.x >> 5);
   const int64_t t = w / (2 * per);
   if (t >= a.T) return;
   const int part = static_cast<int>(w % (2 * per)), kind = part >= per;
@@ -543,9 +543,9 @@ int launch_heads(HeadArgs a, int sms, cudaStream_t s) {
   const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
   a.iters = groups_per_warp(a.T, gq + 2 * gk, sms);
   const int64_t parts = (gq + a.iters - 1) / a.iters + 2 * ((gk + a.iters - 1) / a.iters);
-  const int64_t warps = a.T * parts, blocks = (warps + kWarps - 1) / kWarps;
+  const int64_t blocks = a.T * parts;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(blocks)), block(kWarps * 32);
+  const dim3 grid(static_cast<unsigned>(blocks)), block(32);
   return a.H[1] > 0 ? launch_pdl(heads_kernel<D, Tin, Tout, true>, grid, block, 0, s, a)
                     : launch_pdl(heads_kernel<D, Tin, Tout, false>, grid, block, 0, s, a);
 }
@@ -582,9 +582,9 @@ int launch_read(ReadArgs a, int sms, cudaStream_t s) {
   constexpr int kUnits = 32 * kE / D;
   const int groups = (a.H + kUnits - 1) / kUnits;
   a.iters = groups_per_warp(a.T, 2 * groups, sms);
-  const int64_t warps = a.T * 2 * ((groups + a.iters - 1) / a.iters), blocks = (warps + kWarps - 1) / kWarps;
+  const int64_t warps = a.T * 2 * ((groups + a.iters - 1) / a.iters), blocks = (warps + kReadWarps - 1) / kReadWarps;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
-  return launch_pdl(read_kernel<D, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kWarps * 32), 0, s, a);
+  return launch_pdl(read_kernel<D, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kReadWarps * 32), 0, s, a);
 }
 
 bool dtype_ok(int d) { return elem_bytes(d) != 0; }
