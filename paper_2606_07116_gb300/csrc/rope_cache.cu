@@ -38,8 +38,9 @@ namespace {
 using namespace offq;
 
 constexpr int kE = 8;        // channels per lane
-constexpr int kReadWarps = 8;  // warps per CTA of the reading kernel; the others' CTAs are one warp
-constexpr int kMostGroups = 8;  // of a warp
+constexpr int kReadWarps = 4;  // warps per CTA of the reading kernel; the others' CTAs are one warp
+constexpr int kMostGroups = 8;   // of a warp
+constexpr int kReadGroups = 4;   // of a warp that reads the cache: all are read at once
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 struct HeadArgs {
@@ -453,7 +454,7 @@ struct ReadArgs {
 // Values s (u - 8) + o of cached heads, keys taken back by H3 (symmetric and orthonormal: its own inverse).
 template <int D, typename Tout>
 __global__ void __launch_bounds__(kReadWarps * 32) read_kernel(const ReadArgs a) {
-  constexpr int kLanes = D / kE, kUnits = 32 / kLanes;
+  constexpr int kLanes = D / (2 * kE), kUnits = 32 / kLanes;
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;
   const int lane = threadIdx.x & 31, l = lane % kLanes, unit = lane / kLanes;
   griddep_wait();
@@ -473,32 +474,35 @@ __global__ void __launch_bounds__(kReadWarps * 32) read_kernel(const ReadArgs a)
   const uint32_t* from = reinterpret_cast<const uint32_t*>((kind ? a.codes[1] : a.codes[0]) + row * (D / 2)) + l;
   const float2* params = reinterpret_cast<const float2*>(kind ? a.params[1] : a.params[0]) + row;
   out += t * (kind ? a.ld[1] : a.ld[0]) + l * kE;
-  uint32_t codes[kMostGroups];
-  float2 par[kMostGroups];
+  uint32_t codes[kReadGroups][2];  // channels 8 l .. 8 l + 7 and those D / 2 further on
+  float2 par[kReadGroups];
 #pragma unroll
-  for (int u = 0; u < kMostGroups; ++u) {
+  for (int u = 0; u < kReadGroups; ++u) {
     const int h = h0 + u * kUnits;
-    codes[u] = 0x88888888u;  // zeros
+    codes[u][0] = codes[u][1] = 0x88888888u;  // zeros
     par[u] = make_float2(0.f, 0.f);
     if (u < count && h < a.H && there) {
       const int64_t at = static_cast<int64_t>(h) << a.page_shift;
-      codes[u] = __ldg(from + at * (D / 8));
+      codes[u][0] = __ldg(from + at * (D / 8));
+      codes[u][1] = __ldg(from + at * (D / 8) + kLanes);
       par[u] = __ldg(params + at);
     }
   }
 #pragma unroll
-  for (int u = 0; u < kMostGroups; ++u) {
+  for (int u = 0; u < kReadGroups; ++u) {
     if (u >= count) break;
     const int h = h0 + u * kUnits;
     // Codes q of channels e and e + 4 as halves: the nibble below the exponent of 1024, less its bias.
-    __half2 q[4];
+    __half2 q[2][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t x = ((e < 2 ? codes[u] : codes[u] >> 8) & (e & 1 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
-      const __half2 y = *reinterpret_cast<const __half2*>(&x);
-      q[e] = e & 1 ? __hfma2(y, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hsub2(y, __float2half2_rn(1032.f));
-    }
-    float scale = par[u].x, v[kE];
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t w = codes[u][i], x = ((e < 2 ? w : w >> 8) & (e & 1 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
+        const __half2 y = *reinterpret_cast<const __half2*>(&x);
+        q[i][e] = e & 1 ? __hfma2(y, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hsub2(y, __float2half2_rn(1032.f));
+      }
+    float scale = par[u].x, v[2][kE];
     if (rotate) {
       // H of the integers q (sums of at most 128 x 8: exact in halves); the offset meets channel 0 alone.
       auto both = [](__half2& x, __half2& y) {
@@ -506,42 +510,56 @@ __global__ void __launch_bounds__(kReadWarps * 32) read_kernel(const ReadArgs a)
         x = __hadd2(x, y);
         y = d;
       };
-      both(q[0], q[1]);
-      both(q[2], q[3]);
-      both(q[0], q[2]);
-      both(q[1], q[3]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q[e] = __hfma2(q[e], __halves2half2(__float2half(1.f), __float2half(-1.f)), __lowhigh2highlow(q[e]));
+      for (int i = 0; i < 2; ++i) {
+        both(q[i][0], q[i][1]);
+        both(q[i][2], q[i][3]);
+        both(q[i][0], q[i][2]);
+        both(q[i][1], q[i][3]);
 #pragma unroll
-      for (int m = 1; m < D / kE; m <<= 1) {
+        for (int e = 0; e < 4; ++e)
+          q[i][e] = __hfma2(q[i][e], __halves2half2(__float2half(1.f), __float2half(-1.f)), __lowhigh2highlow(q[i][e]));
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) both(q[0][e], q[1][e]);
+#pragma unroll
+      for (int m = 1; m < kLanes; m <<= 1) {
         const __half2 sign = __float2half2_rn((lane & m) ? -1.f : 1.f);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = __hfma2(sign, q[e], __shfl_xor_sync(kAll, q[e], m));
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) q[i][e] = __hfma2(sign, q[i][e], __shfl_xor_sync(kAll, q[i][e], m));
       }
       scale *= kRoot;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = __half22float2(q[e]);
-      v[e] = rotate ? f.x * scale : fmaf(f.x, scale, par[u].y);
-      v[e + 4] = rotate ? f.y * scale : fmaf(f.y, scale, par[u].y);
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __half22float2(q[i][e]);
+        v[i][e] = rotate ? f.x * scale : fmaf(f.x, scale, par[u].y);
+        v[i][e + 4] = rotate ? f.y * scale : fmaf(f.y, scale, par[u].y);
+      }
     }
-    if (rotate && l == 0) v[0] = fmaf(par[u].y, D * kRoot, v[0]);
-    if (h < a.H) store8(out + h * D, v);
+    if (rotate && l == 0) v[0][0] = fmaf(par[u].y, D * kRoot, v[0][0]);
+    if (h < a.H) {
+      store8(out + h * D, v[0]);
+      store8(out + h * D + D / 2, v[1]);
+    }
   }
 }
 
 // Groups of heads per warp: several where there are enough warps to fill the chip without it.
-int groups_per_warp(int64_t T, int groups, int sms) {
+int groups_per_warp(int64_t T, int groups, int sms, int most) {
   const int64_t per = T * groups / (static_cast<int64_t>(sms) * 64);
-  return static_cast<int>(std::clamp<int64_t>(per, 1, kMostGroups));
+  return static_cast<int>(std::clamp<int64_t>(per, 1, most));
 }
 
 template <int D, typename Tin, typename Tout>
 int launch_heads(HeadArgs a, int sms, cudaStream_t s) {
   constexpr int kUnits = 64 * kE / D;
   const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
-  a.iters = groups_per_warp(a.T, gq + 2 * gk, sms);
+  a.iters = groups_per_warp(a.T, gq + 2 * gk, sms, kMostGroups);
   const int64_t parts = (gq + a.iters - 1) / a.iters + 2 * ((gk + a.iters - 1) / a.iters);
   const int64_t blocks = a.T * parts;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
@@ -579,9 +597,9 @@ int run_heads(HeadArgs& a, int dtype, int out_dtype, int head_dim, void* stream)
 
 template <int D, typename Tout>
 int launch_read(ReadArgs a, int sms, cudaStream_t s) {
-  constexpr int kUnits = 32 * kE / D;
+  constexpr int kUnits = 64 * kE / D;
   const int groups = (a.H + kUnits - 1) / kUnits;
-  a.iters = groups_per_warp(a.T, 2 * groups, sms);
+  a.iters = groups_per_warp(a.T, 2 * groups, sms, kReadGroups);
   const int64_t warps = a.T * 2 * ((groups + a.iters - 1) / a.iters), blocks = (warps + kReadWarps - 1) / kReadWarps;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
   return launch_pdl(read_kernel<D, Tout>, dim3(static_cast<unsigned>(blocks)), dim3(kReadWarps * 32), 0, s, a);
