@@ -12,17 +12,19 @@
 // Every operation above is rounded on its own (no contraction), so the codes are a function of the
 // formula and not of the compiler.
 //
-// A lane owns 8 neighbouring channels (one 16-byte load of a 16-bit type), so a head of 128 takes
-// half a warp and a head of 64 a quarter; sums, maxima and the outer butterflies are xor shuffles.
+// A lane owns 16 channels, 8 neighbours (one 16-byte load of a 16-bit type) in each half of a head, so a head of 128 takes
+// a fourth of a warp. The last butterfly and, where the whole head rotates, both channels of a rotary pair are in the
+// lane, and all arithmetic goes two channels at a time; sums, maxima and three butterflies are xor shuffles. With 8 channels
+// a lane 4097 tokens of 96 heads took 58 us to write (217 instructions a pair of heads) and take 41 now (120).
 // A warp stays with one token and takes several groups of heads, with the token's cosines and sines
-// in registers: they would otherwise be read again for each head, four times the data's own bytes. The reads of
-// two groups (eight of the cache's) are issued before the first is worked on: one 16-byte read a lane in flight
-// does not cover the memory's latency.
+// in registers: they would otherwise be read again for each head, four times the data's own bytes. Without a cache the
+// reads of two groups are issued before the first is worked on (8191 tokens of 72 heads: 51 us, with one 56); with one the
+// registers serve more warps instead (59 us with the reading back, with two 65). CTAs of one warp leave no registers idle and
+// end one by one: with eight warps a CTA the same took 57 and 69 us.
 //
-// Measured: 8191 tokens x 72 heads of 128 (f16, rotary on 64 channels) 60 us, 5.0 TB/s, bound by the memory (of
-// 2 to 5 CTAs per SM four are fastest: 68, 59, 70 us with 3, 4, 5). With the cache's codes the instructions bound it: 4097
-// tokens x 32 query, 32 key and 32 value heads of 128 58 us, 64 % of the issue slots, 217 a pair of heads. Reading back
-// 16384 tokens x 8 heads of 128 takes 26 us, 3.3 TB/s, 76 % of the issue slots.
+// Measured: 8191 tokens x 72 heads of 128 (f16, rotary on 64 channels) 51 us, 5.9 TB/s, 88 % of the copy bandwidth. 4097
+// tokens x 32 query, 32 key and 32 value heads of 128 written in 41 us, 3.8 TB/s: reads' latency and issue slots (55 %). 16384
+// tokens x 8 heads of 128 read back in 22 us, 3.9 TB/s, 77 % of the issue slots: widening, butterflies in packed halves.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -37,9 +39,9 @@ namespace {
 
 using namespace offq;
 
-constexpr int kE = 8;        // channels per lane
-constexpr int kReadWarps = 4;  // warps per CTA of the reading kernel; the others' CTAs are one warp
-constexpr int kMostGroups = 8;   // of a warp
+constexpr int kE = 8;            // a lane's channels in each half of a head
+constexpr int kReadWarps = 4;    // warps per CTA of the reading kernel (one, two or eight are 2 to 30 % slower)
+constexpr int kMostGroups = 8;   // groups of heads of a warp
 constexpr int kReadGroups = 4;   // of a warp that reads the cache: all are read at once
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
