@@ -68,6 +68,7 @@ struct HeadArgs {
   int64_t slots_in_cache;
   int page_shift;
   int iters;         // groups of heads per warp
+  float zero;        // -0 (mul2)
   int* status;
 };
 
@@ -146,6 +147,10 @@ __device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
   asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// a b, as a multiply-add of a -0 that the compiler does not know: a packed product that meets a packed sum would become one
+// multiply-add with one rounding, in spite of the .rn of both.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b, float zero) { return fma2v(a, b, pack2(zero, zero)); }
+
 __device__ __forceinline__ uint64_t shfl_xor2(uint64_t v, int m) {
   float x, y;
   unpack2(v, x, y);
@@ -258,15 +263,15 @@ __device__ __forceinline__ void rotary(const HeadArgs& a, const float* row, cons
 #pragma unroll
     for (int m = 0; m < kE / 2; ++m) {
       const uint64_t x = v[2 * m], y = v[2 * m + 1], c = pack2(t.c[m], t.c[4 + m]), s = pack2(t.s[m], t.s[4 + m]);
-      v[2 * m] = sub2(mul2v(x, c), mul2v(y, s));
-      v[2 * m + 1] = add2(mul2v(y, c), mul2v(x, s));
+      v[2 * m] = sub2(mul2(x, c, a.zero), mul2(y, s, a.zero));
+      v[2 * m + 1] = add2(mul2(y, c, a.zero), mul2(x, s, a.zero));
     }
   } else if (a.rot == D) {  // both channels of a pair are this lane's
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       float x, y;
       unpack2(v[e], x, y);
-      v[e] = add2(mul2v(v[e], pack2(t.c[e], t.c[e])), mul2v(pack2(y, x), pack2(t.s[e], -t.s[e])));
+      v[e] = add2(mul2(v[e], pack2(t.c[e], t.c[e]), a.zero), mul2(pack2(y, x), pack2(t.s[e], -t.s[e]), a.zero));
     }
   } else {  // rot is a multiple of 16: a pair's other channel is the same element of another eight
     const int l = lane % kLanes, n = a.rot / (2 * kE), base = lane - l;
@@ -281,15 +286,15 @@ __device__ __forceinline__ void rotary(const HeadArgs& a, const float* row, cons
       const float a0 = __shfl_sync(kAll, x, base + p0 % kLanes), b0 = __shfl_sync(kAll, y, base + p0 % kLanes);
       const float a1 = __shfl_sync(kAll, x, base + p1 % kLanes), b1 = __shfl_sync(kAll, y, base + p1 % kLanes);
       const uint64_t o = pack2(p0 < kLanes ? a0 : b0, p1 < kLanes ? a1 : b1);
-      v[e] = add2(mul2v(v[e], pack2(t.c[e], u.c[e])), mul2v(o, pack2(t.s[e], u.s[e])));
+      v[e] = add2(mul2(v[e], pack2(t.c[e], u.c[e]), a.zero), mul2(o, pack2(t.s[e], u.s[e]), a.zero));
     }
   }
 }
 
 // Codes of a head y (before H3 where `rotate`) into its slot.
 template <int D>
-__device__ __forceinline__ void quantize_head(Pairs& v, bool rotate, bool offset, bool live, int lane, uint8_t* codes,
-                                              float* params) {
+__device__ __forceinline__ void quantize_head(Pairs& v, bool rotate, bool offset, bool live, int lane, float zero,
+                                              uint8_t* codes, float* params) {
   constexpr float kRoot = D == 128 ? 0.08838834764831844055f : 0.125f;  // 1 / sqrt(D) in fp32
   constexpr int kLanes = D / (2 * kE);
   const int l = lane % kLanes;
@@ -316,7 +321,7 @@ __device__ __forceinline__ void quantize_head(Pairs& v, bool rotate, bool offset
 #pragma unroll
   for (int e = kE - 1; e >= 0; --e) {
     float x, y;
-    unpack2(add2(mul2v(v[e], pack2(inv, inv)), pack2(12582920.0f, 12582920.0f)), x, y);
+    unpack2(add2(mul2(v[e], pack2(inv, inv), zero), pack2(12582920.0f, 12582920.0f)), x, y);
     w0 = (w0 << 4) + __float_as_uint(x);
     w1 = (w1 << 4) + __float_as_uint(y);
   }
@@ -381,7 +386,7 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
         if (norm != nullptr) {
           Pairs wt;
 #pragma unroll
-          for (int e = 0; e < kE; ++e) wt[e] = mul2v(v[e], v[e]);
+          for (int e = 0; e < kE; ++e) wt[e] = mul2(v[e], v[e], a.zero);
           const float mean = __fmul_rn(head_sum<D>(wt), 1.0f / D);
           const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(mean, a.eps)));
           const float* weights = norm + min(h, heads - 1) * D + l * kE;
@@ -389,7 +394,7 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
           load8(weights + D / 2, hi);
           pairs_of(lo, hi, wt);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[e] = mul2v(mul2v(v[e], pack2(inv, inv)), wt[e]);
+          for (int e = 0; e < kE; ++e) v[e] = mul2(mul2(v[e], pack2(inv, inv), a.zero), wt[e], a.zero);
         }
         if (a.rot != 0) rotary<D>(a, row, ang, lane, v);
       }
@@ -397,7 +402,7 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
         if (a.rotate[0]) {
           head_hadamard<D>(v, lane);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) v[e] = mul2v(v[e], pack2(kRoot, kRoot));
+          for (int e = 0; e < kE; ++e) v[e] = mul2(v[e], pack2(kRoot, kRoot), a.zero);
         }
         if (live) {
           Tout* to = static_cast<Tout*>(a.out) + t * a.ld_out + h * D + l * kE;
@@ -408,7 +413,7 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
         }
       } else {
         const int64_t at = static_cast<int64_t>(live ? h : 0) << a.page_shift;
-        quantize_head<D>(v, a.rotate[KIND] != 0, a.offset != 0, live, lane, codes + at * (D / 2), params + at * 2);
+        quantize_head<D>(v, a.rotate[KIND] != 0, a.offset != 0, live, lane, a.zero, codes + at * (D / 2), params + at * 2);
       }
     }
   }
@@ -562,6 +567,7 @@ int launch_heads(HeadArgs a, int sms, cudaStream_t s) {
   constexpr int kUnits = 64 * kE / D;
   const int gq = (a.H[0] + kUnits - 1) / kUnits, gk = (a.H[1] + kUnits - 1) / kUnits;
   a.iters = groups_per_warp(a.T, gq + 2 * gk, sms, kMostGroups);
+  a.zero = -0.0f;
   const int64_t parts = (gq + a.iters - 1) / a.iters + 2 * ((gk + a.iters - 1) / a.iters);
   const int64_t blocks = a.T * parts;
   if (blocks > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;

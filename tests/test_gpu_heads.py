@@ -87,6 +87,45 @@ def test_rope_heads(T, H, D, rot, interleaved, norm, rotate, dt, odt):
     assert Q.offq_get_device_status() == Q.OFFQ_OK
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,rot", [(D, rot) for D in (64, 128) for rot in range(16, D + 1, 16)])
+def test_every_rotary_size(D, rot, interleaved):
+    test_rope_heads(9, 6, D, rot, interleaved, True, True, "bf16", "f32")
+    test_rope_heads(2, 5, D, rot, interleaved, False, False, "f16", "f32")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_products_are_rounded_one_by_one(interleaved, D):
+    """x c - y s and y c + x s: the bits of three fp32 operations each, for whole and partly rotated heads."""
+    for rot in (D, D // 2, D - 16):
+        x, _ = _x(50, 6, D, "f32", rot)
+        (pos, table), _ = _rotary(50, rot, 7)
+        y = Q.rope_heads(x, pos, table, interleaved=interleaved)
+        c, s = (t[:, None].cpu() for t in table[pos.long()].split(rot // 2, 1))
+        a, b = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+        x, ref = x.cpu(), x.cpu().clone()
+        ref[..., a] = x[..., a] * c - x[..., b] * s
+        ref[..., b] = x[..., b] * c + x[..., a] * s
+        assert torch.equal(y.cpu(), ref)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_codes_are_those_of_single_operations(D):
+    """u = rne(fl(x * fl(7 / max|x|))) + 8 to the bit, with as many near ties as 100000 heads have."""
+    T, H, page = 12500, 8, 256
+    x, _ = _x(T, H, D, "f32", D)
+    cache = Q.kv4_cache(-(-T // page), H, D, page)
+    slots = torch.arange(T, device="cuda")
+    Q.kv4_paged_write(cache, x, x, slots, rotate=False, offset=False)
+    p = x * (7.0 / x.abs().amax(-1, keepdim=True))
+    u = (torch.round(p) + 8).to(torch.uint8)
+    want = u[..., 0::2] | u[..., 1::2] << 4
+    for codes in (cache.k_codes, cache.v_codes):
+        got = codes.permute(0, 2, 1, 3).reshape(-1, H, D // 2)[:T]
+        assert torch.equal(got, want)
+
+
 def test_rope_heads_in_place_and_strided():
     T, H, D = 37, 6, 128
     x, x64 = _x(T, H + 3, D, "bf16", 5)
