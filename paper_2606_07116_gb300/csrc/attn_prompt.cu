@@ -58,6 +58,9 @@ struct PromptCtrl {
   uint64_t q_full[2], q_empty[2], tail, done;
   uint64_t full[8], empty[8];
   uint64_t s_full[2], p_ready[2][2];  // weights of 64 keys at a time
+  // An item's outputs. Not a further phase of s_full: the next item's scores follow them without an answer from the
+  // softmax, and a warp that came after both would wait for a third.
+  uint64_t o_full[2];
   uint64_t item_full, item_empty, taken;
   alignas(16) uint32_t answer[4];
   alignas(16) Item item;
@@ -122,6 +125,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
       mbar_init(smem_u32(&ctrl->q_full[i]), 1);
       mbar_init(smem_u32(&ctrl->q_empty[i]), 1);
       mbar_init(smem_u32(&ctrl->s_full[i]), 1);
+      mbar_init(smem_u32(&ctrl->o_full[i]), 1);
       mbar_init(smem_u32(&ctrl->p_ready[i][0]), 4);
       mbar_init(smem_u32(&ctrl->p_ready[i][1]), 4);
     }
@@ -373,7 +377,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
                 scores(i, ks);
                 if (j + 2 == blocks[i]) mma_commit(smem_u32(&ctrl->q_empty[i]));
               } else {
-                mma_commit(smem_u32(&ctrl->s_full[i]));  // the last phase says that O is complete
+                mma_commit(smem_u32(&ctrl->o_full[i]));
               }
             }
             __syncwarp();
@@ -400,7 +404,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
     const float sc = a.scale * kLog2e;
-    int ns = 0;
+    int ns = 0, no = 0;
     bool ok = true;
     for (int k = 0; ok && next_item(k); ++k) {
       const int my_blocks = i ? blocks[1] : blocks[0], my_row0 = i ? row0[1] : row0[0], my_head = i ? head[1] : head[0];
@@ -469,7 +473,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
         unpack2(add2_rn(add2_rn(part[0], part[1]), add2_rn(part[2], part[3])), x, y);
         sum += x + y;
       }
-      if (ok) ok = wait(&ctrl->s_full[i], ns++);
+      if (ok) ok = wait(&ctrl->o_full[i], no++);
       if (ok) {
         tc_fence_after();
         const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;

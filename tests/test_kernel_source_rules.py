@@ -110,3 +110,20 @@ def test_the_host_keeps_no_plain_mutable_statics():
                             or "std::call_once(once" in text and "std::once_flag once;" in text[m.end():m.end() + 60])
             assert synchronised, (name, decl)
     assert sum(source(n).count("cudaDevAttrMultiProcessorCount") for n in os.listdir(B.CSRC)) == 1
+
+
+def test_one_barrier_says_one_thing_to_the_prompt_softmax():
+    """A waiter that is late by two phases of a barrier takes them for none. The issuing warp may run from an item's last
+    products into the next item's scores without hearing from the softmax, so the outputs and the scores of a tile have a
+    barrier each: the next phase of either takes weights that only a softmax past the last one hands on."""
+    text = source("attn_prompt.cu")
+    body = block(text, text.index("prompt_kernel(const AttnArgs a"))
+    scores = block(body, body.index("auto scores = [&]"))
+    assert re.findall(r"mma_commit\(smem_u32\(&ctrl->(\w+)\[i\]\)\)", scores) == ["s_full"]
+    rest = body.replace(scores, "")
+    assert "mma_commit(smem_u32(&ctrl->s_full" not in rest
+    assert rest.count("mma_commit(smem_u32(&ctrl->o_full[i]))") == 1
+    softmax = rest[rest.index("more_registers<kSoftmaxRegs>()"):]
+    waits = re.findall(r"wait\(&ctrl->(\w+)\[i\], (\w+)\+\+\)", softmax)
+    assert waits == [("s_full", "ns"), ("o_full", "no")]
+    assert "mbar_init(smem_u32(&ctrl->o_full[i]), 1)" in body
