@@ -211,7 +211,9 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
           taken = -1;
           return -1;
         }
-        return taken_over(smem_u32(ctrl->answer));
+        int at = 0;  // read by the lane that asks and fences: the next answer is written over this one
+        if (lane == 0) at = taken_over(smem_u32(ctrl->answer));
+        return __shfl_sync(kAllLanes, at, 0);
       };
       bool more = true;
       for (int k = 0; more; ++k) {

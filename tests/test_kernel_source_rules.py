@@ -127,3 +127,14 @@ def test_one_barrier_says_one_thing_to_the_prompt_softmax():
     waits = re.findall(r"wait\(&ctrl->(\w+)\[i\], (\w+)\+\+\)", softmax)
     assert waits == [("s_full", "ns"), ("o_full", "no")]
     assert "mbar_init(smem_u32(&ctrl->o_full[i]), 1)" in body
+
+
+def test_one_lane_reads_the_answers_about_items():
+    """The next answer is written by the asynchronous proxy over the last one, after a fence by the lane that asks for it:
+    that lane alone reads them, and the warp takes what it read by a shuffle."""
+    text = source("attn_prompt.cu")
+    take = block(text, text.index("auto take = [&]()"))
+    assert len(re.findall(r"\btaken_over\(", text.replace("int taken_over(uint32_t answer)", ""))) == 1
+    assert re.search(r"if \(lane == 0\) at = taken_over\(smem_u32\(ctrl->answer\)\);\s*return __shfl_sync\(kAllLanes, at, 0\);", take)
+    assert re.search(r"if \(lane == 0\) \{\s*fence_proxy_async_smem\(\);\s*mbar_arrive_expect_tx\(bar, 16\);\s*take_over\(", take)
+    assert text.count("ctrl->answer") == 2
