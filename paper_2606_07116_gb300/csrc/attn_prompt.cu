@@ -207,10 +207,13 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
           take_over(smem_u32(ctrl->answer), bar);
         }
         __syncwarp();
-        if (!wait(&ctrl->taken, taken++)) {
+        if (!wait(&ctrl->taken, taken)) {
+          if (lane == 0) mbar_wait_teardown(bar, taken & 1);  // the answer lands before the CTA ends
+          __syncwarp();
           taken = -1;
           return -1;
         }
+        ++taken;
         int at = 0;  // read by the lane that asks and fences: the next answer is written over this one
         if (lane == 0) at = taken_over(smem_u32(ctrl->answer));
         return __shfl_sync(kAllLanes, at, 0);

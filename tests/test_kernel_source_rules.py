@@ -138,3 +138,13 @@ def test_one_lane_reads_the_answers_about_items():
     assert re.search(r"if \(lane == 0\) at = taken_over\(smem_u32\(ctrl->answer\)\);\s*return __shfl_sync\(kAllLanes, at, 0\);", take)
     assert re.search(r"if \(lane == 0\) \{\s*fence_proxy_async_smem\(\);\s*mbar_arrive_expect_tx\(bar, 16\);\s*take_over\(", take)
     assert text.count("ctrl->answer") == 2
+
+
+def test_a_request_in_flight_is_waited_for_before_the_cta_ends():
+    """An answer that lands after its CTA has ended would be written into another CTA's shared memory: where the wait for
+    it is given up (some other wait of the CTA ran out), the request's own barrier is waited for without the abort flag."""
+    text = source("attn_prompt.cu")
+    take = block(text, text.index("auto take = [&]()"))
+    given_up = block(take, take.index("if (!wait(&ctrl->taken"))
+    assert "mbar_wait_teardown(bar, taken & 1)" in given_up
+    assert given_up.index("mbar_wait_teardown") < given_up.index("taken = -1") < given_up.index("return -1")
