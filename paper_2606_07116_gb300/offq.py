@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 import math
 import os
 import re
@@ -171,6 +172,29 @@ def _stream(stream):
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
+
+
+def _on(stream):
+    """Context in which torch takes memory from, and runs behind, a stream given as such or as its handle."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
+
+
+def _on_its_stream(helper):
+    """With a stream given, what the helper allocates and copies is that stream's too: memory let go on the current
+    stream may still be in use there, and a copy made there would not be ordered with the call. What it returns is
+    memory of the call's stream, as under torch.cuda.stream."""
+    at = list(inspect.signature(helper).parameters).index("stream")
+
+    @functools.wraps(helper)
+    def call(*args, **kwargs):
+        stream = args[at] if len(args) > at else kwargs.get("stream")
+        if stream is None:
+            return helper(*args, **kwargs)
+        with _on(stream):
+            return helper(*args, **kwargs)
+    return call
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -746,21 +770,6 @@ def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: in
     return need
 
 
-def _on(stream, device: torch.device):
-    """Context in which torch takes memory from, and runs behind, the call's stream (None: the current one)."""
-    if stream is not None and not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device)
-    return torch.cuda.stream(stream)
-
-
-def _workspace(need: int, device: torch.device, stream) -> torch.Tensor:
-    """``need`` bytes whose memory, once let go, is taken again only behind the work of the call's stream."""
-    if stream is None:
-        return torch.empty((need,), dtype=torch.uint8, device=device)
-    with _on(stream, device):
-        return torch.empty((need,), dtype=torch.uint8, device=device)
-
-
 def offq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: int, Hq: int, H: int, head_dim: int,
                           ld_q: int, ld_k: int, ld_v: int, cu: torch.Tensor, B: int, scale: float, causal: bool,
                           out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor], stream=None) -> None:
@@ -807,6 +816,7 @@ def _cache_shape(cache: KV4Cache, H: Optional[int], hd: Optional[int]):
     return pages, heads, page_size, 2 * half
 
 
+@_on_its_stream
 def rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
                norm: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, rotate: bool = False,
                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -826,6 +836,7 @@ def rope_heads(x: torch.Tensor, positions: Optional[torch.Tensor] = None, table:
     return out
 
 
+@_on_its_stream
 def kv4_paged_write(cache: KV4Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
                     positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
                     q: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
@@ -855,6 +866,7 @@ def kv4_paged_write(cache: KV4Cache, k: torch.Tensor, v: torch.Tensor, slots: to
     return q_out
 
 
+@_on_its_stream
 def kv4_paged_read(cache: KV4Cache, slots: torch.Tensor, rotate: bool = True, rotate_v: bool = False,
                    out_dtype: torch.dtype = torch.bfloat16, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Keys (H3 undone with rotate) and values [T, H, hd] of the tokens in slots [T] (int64)."""
@@ -868,6 +880,7 @@ def kv4_paged_read(cache: KV4Cache, slots: torch.Tensor, rotate: bool = True, ro
     return k, v
 
 
+@_on_its_stream
 def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, lens: torch.Tensor,
                     cu_q: torch.Tensor, max_q: int, scale: Optional[float] = None, lse: bool = False,
                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
@@ -888,8 +901,7 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
             ld_table < width or block_table.storage_offset() + B * ld_table > block_table.untyped_storage().nbytes() // 4):
         # Rows of one another, or a last row whose ld_table entries pass the end of its memory: the kernels allow
         # lengths of ld_table pages.
-        with _on(stream, q.device):
-            block_table = block_table.contiguous()
+        block_table = block_table.contiguous()
         ld_table = width
     ld_out = Hq * hd
     if out is None:
@@ -903,7 +915,7 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
             need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q)
         except LookupError:
             need = 0
-        workspace = _workspace(need, q.device, stream) if need > 0 else None
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None
     stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
     offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table,
                          ld_table if B > 1 else width, lens, cu_q, B, max_q,
@@ -912,6 +924,7 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
     return (out, stats) if lse else out
 
 
+@_on_its_stream
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, scale: Optional[float] = None,
                      causal: bool = True, lse: bool = False, out: Optional[torch.Tensor] = None, stream=None):
     """Attention inside packed sequences: rows cu[b] .. cu[b + 1] - 1 of q [T, Hq, hd] and k, v [T, H, hd] are sequence

@@ -1,0 +1,79 @@
+"""With stream= given, a helper takes the memory of what it returns, and makes its copies, on that stream: memory of the
+current stream may still be used by work queued there, and a copy made there is not ordered with the call. Run without a
+GPU: the library and the streams are stand-ins that record where an allocation or a copy was made."""
+
+import contextlib
+import inspect
+
+import pytest
+import torch
+
+from paper_2606_07116_gb300 import offq as Q
+
+STREAM = 0x5EED
+
+
+class _Library:
+    def __getattr__(self, name):
+        return lambda *args: 64 if name.endswith("_workspace") or name.endswith("_bytes") else Q.OFFQ_OK
+
+
+@pytest.fixture
+def record(monkeypatch):
+    """Allocations and copies, each with the streams that were entered around it."""
+    entered, made = [], []
+
+    @contextlib.contextmanager
+    def on(stream, *_):
+        entered.append(stream)
+        yield
+        entered.pop()
+
+    empty, contiguous = torch.empty, torch.Tensor.contiguous
+    monkeypatch.setattr(Q, "_on", on)
+    monkeypatch.setattr(Q, "load_library", _Library)
+    monkeypatch.setattr(Q, "_ptr", lambda t: 0)
+    monkeypatch.setattr(Q, "_stream", lambda s: s)
+    monkeypatch.setattr(Q.torch, "empty", lambda *a, **k: (made.append(("empty", list(entered))), empty(*a, **k))[1])
+    monkeypatch.setattr(torch.Tensor, "contiguous", lambda t: t if t.is_contiguous() else
+                        (made.append(("copy", list(entered))), contiguous(t))[1])
+    Q._workspace_bytes.cache_clear()
+    yield made
+    Q._workspace_bytes.cache_clear()
+
+
+def _attention_calls():
+    x = torch.zeros((3, 2, 128), dtype=torch.bfloat16)
+    cache = Q.kv4_cache(2, 2, 128, 16, device="cpu")
+    slots, i32 = torch.zeros(3, dtype=torch.int64), torch.zeros(4, dtype=torch.int32)
+    table = torch.zeros((3, 9), dtype=torch.int32)
+    return {
+        "rope_heads": (x,),
+        "kv4_paged_write": (cache, x, x, slots, None, None, x),
+        "kv4_paged_read": (cache, slots),
+        "paged_attention": (x, cache, table[:, 7:], i32[:3], i32, 1, None, True),
+        "prompt_attention": (x, x, x, i32, None, True, True),
+    }
+
+
+@pytest.mark.parametrize("name", list(_attention_calls()))
+def test_attention_helpers_allocate_on_the_calls_stream(record, name):
+    args = _attention_calls()[name]
+    record.clear()
+    getattr(Q, name)(*args, stream=STREAM)
+    assert record and all(entered == [STREAM] for _, entered in record), record
+    record.clear()
+    getattr(Q, name)(*args)
+    assert record and all(entered in ([], [None]) for _, entered in record)
+
+
+@pytest.mark.parametrize("name", list(_attention_calls()))
+def test_a_stream_given_by_position(record, name):
+    """As the last of the positional arguments."""
+    f = getattr(Q, name)
+    bound = inspect.signature(f).bind(*_attention_calls()[name])
+    bound.apply_defaults()
+    bound.arguments["stream"] = STREAM
+    record.clear()
+    f(*bound.args)
+    assert record and all(entered == [STREAM] for _, entered in record), record
