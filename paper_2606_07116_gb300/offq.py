@@ -355,6 +355,7 @@ def padded_rows(R: int) -> int:
 # Allocating helpers (torch allocates; the entry points above compute).
 # ---------------------------------------------------------------------------
 
+@_on_its_stream
 def quantize_act(x: torch.Tensor, g: int, rotate: bool = True, offset: bool = True,
                  stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     T, K = x.shape
@@ -366,6 +367,7 @@ def quantize_act(x: torch.Tensor, g: int, rotate: bool = True, offset: bool = Tr
     return codes, scale, off
 
 
+@_on_its_stream
 def kv4_quantize(kv: torch.Tensor, rotate: bool = True, offset: bool = True,
                  stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     T, H, hd = kv.shape
@@ -379,6 +381,7 @@ def kv4_quantize(kv: torch.Tensor, rotate: bool = True, offset: bool = True,
     return codes, scale, off
 
 
+@_on_its_stream
 def prepare_weight(w: torch.Tensor, g: int, rotate: bool = True,
                    stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     N, K = w.shape
@@ -390,6 +393,7 @@ def prepare_weight(w: torch.Tensor, g: int, rotate: bool = True,
     return codes, scale, rowsum
 
 
+@_on_its_stream
 def w4a4_linear(a_codes: torch.Tensor, a_scale: torch.Tensor, a_offset: Optional[torch.Tensor],
                 w_codes: torch.Tensor, w_scale: torch.Tensor, w_offsum: torch.Tensor, g: int,
                 out_dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
@@ -407,6 +411,7 @@ def w4a4_linear(a_codes: torch.Tensor, a_scale: torch.Tensor, a_offset: Optional
 GROUP = 128  # activation group size of the per-group path (the paper's evaluated setting)
 
 
+@_on_its_stream
 def quantize_act_group(x: torch.Tensor, g: int, group: int = GROUP, rotate: bool = True,
                        stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Per-group asymmetric codes, scales and zero-points of token rows x [T, K]."""
@@ -419,6 +424,7 @@ def quantize_act_group(x: torch.Tensor, g: int, group: int = GROUP, rotate: bool
     return codes, scale, zero
 
 
+@_on_its_stream
 def weight_group_sums(w_codes: torch.Tensor, N: int, K: int, group: int = GROUP, stream=None) -> torch.Tensor:
     """Integer row sums of the weight codes per activation group, [K/group, N] float32."""
     sums = torch.empty((K // group, N), dtype=torch.float32, device=w_codes.device)
@@ -426,6 +432,7 @@ def weight_group_sums(w_codes: torch.Tensor, N: int, K: int, group: int = GROUP,
     return sums
 
 
+@_on_its_stream
 def w4a4_linear_group(a_codes: torch.Tensor, a_scale: torch.Tensor, a_zero: torch.Tensor,
                       w_codes: torch.Tensor, w_scale: torch.Tensor, w_groupsum: torch.Tensor,
                       group: int = GROUP, out_dtype: torch.dtype = torch.bfloat16,
@@ -440,6 +447,7 @@ def w4a4_linear_group(a_codes: torch.Tensor, a_scale: torch.Tensor, a_zero: torc
     return out
 
 
+@_on_its_stream
 def kv4_quantize_rotated(kv: torch.Tensor, rot: torch.Tensor, offset: bool = True,
                          stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Key-cache codes, scales and offsets of kv [T, H, hd] under per-head rotations rot [H, hd, hd]."""
@@ -454,6 +462,7 @@ def kv4_quantize_rotated(kv: torch.Tensor, rot: torch.Tensor, offset: bool = Tru
     return codes, scale, off
 
 
+@_on_its_stream
 def rotate_heads(x: torch.Tensor, rot: torch.Tensor, out_dtype: torch.dtype = torch.float32,
                  stream=None) -> torch.Tensor:
     """x [T, H, hd] rotated per head by rot [H, hd, hd] (y = x rot[h])."""
@@ -468,6 +477,7 @@ def rotate_heads(x: torch.Tensor, rot: torch.Tensor, out_dtype: torch.dtype = to
 KEY_ROTATION_BYTES = 98304  # OFFQ_KEY_ROTATION_BYTES: one head's prepared rotation
 
 
+@_on_its_stream
 def prepare_key_rotation(rot: torch.Tensor, stream=None) -> torch.Tensor:
     """rot [H, hd, hd] float32 -> the prepared image [H, KEY_ROTATION_BYTES] (uint8)."""
     H, hd, _ = rot.shape
@@ -476,6 +486,7 @@ def prepare_key_rotation(rot: torch.Tensor, stream=None) -> torch.Tensor:
     return prep
 
 
+@_on_its_stream
 def kv4_quantize_prepared(kv: torch.Tensor, prepared: torch.Tensor, offset: bool = True,
                           stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """kv4_quantize_rotated for bf16 kv [T, H, hd] with M given as prepare_key_rotation's image."""
@@ -490,6 +501,7 @@ def kv4_quantize_prepared(kv: torch.Tensor, prepared: torch.Tensor, offset: bool
     return codes, scale, off
 
 
+@_on_its_stream
 def rotate_heads_prepared(x: torch.Tensor, prepared: torch.Tensor, out_dtype: torch.dtype = torch.float32,
                           stream=None) -> torch.Tensor:
     """rotate_heads for bf16 x [T, H, hd] with M given as prepare_key_rotation's image."""
@@ -515,6 +527,7 @@ def prepare_key_reflection(v: torch.Tensor, perm: torch.Tensor, device=None) -> 
     return img.to(device) if device is not None else img
 
 
+@_on_its_stream
 def kv4_quantize_reflected(kv: torch.Tensor, prepared: torch.Tensor, offset: bool = True,
                            stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Key-cache codes, scales and offsets of bf16 kv [T, H, hd] under the structured M = U3 P3 H3."""
@@ -529,6 +542,7 @@ def kv4_quantize_reflected(kv: torch.Tensor, prepared: torch.Tensor, offset: boo
     return codes, scale, off
 
 
+@_on_its_stream
 def rotate_heads_reflected(x: torch.Tensor, prepared: torch.Tensor, out_dtype: torch.dtype = torch.float32,
                            stream=None) -> torch.Tensor:
     """bf16 x [T, H, hd] rotated per head by the structured M = U3 P3 H3."""
@@ -544,6 +558,7 @@ def rotate_heads_reflected(x: torch.Tensor, prepared: torch.Tensor, out_dtype: t
 # Offline transform builder
 # ---------------------------------------------------------------------------
 
+@_on_its_stream
 def top1_tokens(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [S, L, D] (contiguous tokens): per sequence the token of largest L-inf norm."""
     S, L, D = x.shape
@@ -556,6 +571,7 @@ def top1_tokens(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tenso
     return index, rows
 
 
+@_on_its_stream
 def top1_direction(X: torch.Tensor, iters: int = 100, v0: Optional[torch.Tensor] = None,
                    stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Leading eigenvector of X^T X / N by power iteration (and X v)."""
@@ -570,6 +586,7 @@ def top1_direction(X: torch.Tensor, iters: int = 100, v0: Optional[torch.Tensor]
     return v, proj
 
 
+@_on_its_stream
 def reflect_rows(A: torch.Tensor, v: torch.Tensor, stream=None) -> torch.Tensor:
     R, D = A.shape
     out = torch.empty((R, D), dtype=torch.float32, device=A.device)
@@ -578,6 +595,7 @@ def reflect_rows(A: torch.Tensor, v: torch.Tensor, stream=None) -> torch.Tensor:
     return out
 
 
+@_on_its_stream
 def column_absmax(A: torch.Tensor, stream=None) -> torch.Tensor:
     R, D = A.shape
     mag = torch.empty((D,), dtype=torch.float32, device=A.device)
@@ -595,6 +613,7 @@ def sorted_grouping(mag: torch.Tensor, G: int) -> torch.Tensor:
     return perm
 
 
+@_on_its_stream
 def fuse_rotation(W: torch.Tensor, v: torch.Tensor, perm: torch.Tensor, g: int, stream=None) -> torch.Tensor:
     N, D = W.shape
     out = torch.empty((N, D), dtype=torch.float32, device=W.device)

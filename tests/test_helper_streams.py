@@ -77,3 +77,48 @@ def test_a_stream_given_by_position(record, name):
     record.clear()
     f(*bound.args)
     assert record and all(entered == [STREAM] for _, entered in record), record
+
+
+def _linear_calls():
+    """The helpers of the linears, the KV quantizers and the transform builder, with inputs that are copied where a
+    helper takes such."""
+    codes, f = torch.zeros((32, 64), dtype=torch.uint8), torch.zeros(2, dtype=torch.float32)
+    x, kv = torch.zeros((2, 256)), torch.zeros((2, 1, 64))
+    rot = torch.zeros((1, 64, 64)).transpose(1, 2)
+    cols = torch.zeros((64, 4)).t()
+    perm = torch.zeros(64, dtype=torch.int64)
+    return {
+        "quantize_act": (x, 128),
+        "kv4_quantize": (kv,),
+        "prepare_weight": (torch.zeros((128, 64)).t(), 128),
+        "w4a4_linear": (codes, f, f, codes, f, f, 128),
+        "quantize_act_group": (x, 128),
+        "weight_group_sums": (codes, 32, 128),
+        "w4a4_linear_group": (codes, f, f, codes, f, f),
+        "kv4_quantize_rotated": (kv, rot),
+        "rotate_heads": (kv, rot),
+        "prepare_key_rotation": (rot,),
+        "kv4_quantize_prepared": (kv, rot),
+        "rotate_heads_prepared": (kv, rot),
+        "kv4_quantize_reflected": (kv, rot),
+        "rotate_heads_reflected": (kv, rot),
+        "top1_tokens": (torch.zeros((2, 3, 64)),),
+        "top1_direction": (cols,),
+        "reflect_rows": (cols, perm.float()),
+        "column_absmax": (cols,),
+        "fuse_rotation": (cols, perm.float(), perm, 64),
+    }
+
+
+@pytest.mark.parametrize("name", list(_linear_calls()))
+def test_other_helpers_allocate_on_the_calls_stream(record, name):
+    args = _linear_calls()[name]
+    record.clear()
+    getattr(Q, name)(*args, stream=STREAM)
+    assert record and all(entered == [STREAM] for _, entered in record), record
+
+
+def test_no_helper_is_left_out():
+    helpers = {n for n, f in vars(Q).items() if inspect.isfunction(f) and f.__module__ == Q.__name__
+               and not n.startswith(("_", "offq_")) and "stream" in inspect.signature(f).parameters}
+    assert helpers == set(_linear_calls()) | set(_attention_calls())
