@@ -577,30 +577,31 @@ def top1_direction(X: torch.Tensor, iters: int = 100, v0: Optional[torch.Tensor]
     """Leading eigenvector of X^T X / N by power iteration (and X v)."""
     N, D = X.shape
     X = X.contiguous()
-    if v0 is None:
-        v0 = torch.ones((D,), dtype=torch.float32, device=X.device)
+    v0 = torch.ones((D,), dtype=torch.float32, device=X.device) if v0 is None else v0.contiguous()
     v = torch.empty((D,), dtype=torch.float32, device=X.device)
     proj = torch.empty((N,), dtype=torch.float32, device=X.device)
     _check("offq_top1_direction", load_library().offq_top1_direction(
-        _ptr(X), N, D, iters, _ptr(v0.contiguous()), _ptr(v), _ptr(proj), _stream(stream)))
+        _ptr(X), N, D, iters, _ptr(v0), _ptr(v), _ptr(proj), _stream(stream)))
     return v, proj
 
 
 @_on_its_stream
 def reflect_rows(A: torch.Tensor, v: torch.Tensor, stream=None) -> torch.Tensor:
     R, D = A.shape
+    A = A.contiguous()
     out = torch.empty((R, D), dtype=torch.float32, device=A.device)
     _check("offq_reflect_rows", load_library().offq_reflect_rows(
-        _ptr(A.contiguous()), R, D, _ptr(v), _ptr(out), _stream(stream)))
+        _ptr(A), R, D, _ptr(v), _ptr(out), _stream(stream)))
     return out
 
 
 @_on_its_stream
 def column_absmax(A: torch.Tensor, stream=None) -> torch.Tensor:
     R, D = A.shape
+    A = A.contiguous()
     mag = torch.empty((D,), dtype=torch.float32, device=A.device)
     _check("offq_column_absmax", load_library().offq_column_absmax(
-        _ptr(A.contiguous()), R, D, _ptr(mag), _stream(stream)))
+        _ptr(A), R, D, _ptr(mag), _stream(stream)))
     return mag
 
 
@@ -616,10 +617,10 @@ def sorted_grouping(mag: torch.Tensor, G: int) -> torch.Tensor:
 @_on_its_stream
 def fuse_rotation(W: torch.Tensor, v: torch.Tensor, perm: torch.Tensor, g: int, stream=None) -> torch.Tensor:
     N, D = W.shape
+    W, perm = W.contiguous(), perm.to(W.device, torch.int32).contiguous()
     out = torch.empty((N, D), dtype=torch.float32, device=W.device)
     _check("offq_fuse_rotation", load_library().offq_fuse_rotation(
-        _ptr(W.contiguous()), N, D, _ptr(v), _ptr(perm.to(W.device, torch.int32).contiguous()), g, _ptr(out),
-        _stream(stream)))
+        _ptr(W), N, D, _ptr(v), _ptr(perm), g, _ptr(out), _stream(stream)))
     return out
 
 

@@ -4,6 +4,7 @@ GPU: the library and the streams are stand-ins that record where an allocation o
 
 import contextlib
 import inspect
+import weakref
 
 import pytest
 import torch
@@ -122,3 +123,26 @@ def test_no_helper_is_left_out():
     helpers = {n for n, f in vars(Q).items() if inspect.isfunction(f) and f.__module__ == Q.__name__
                and not n.startswith(("_", "offq_")) and "stream" in inspect.signature(f).parameters}
     assert helpers == set(_linear_calls()) | set(_attention_calls())
+
+
+@pytest.mark.parametrize("name", list(_linear_calls()) + list(_attention_calls()))
+def test_copies_live_until_the_call(monkeypatch, name):
+    """A copy that only its address was taken of goes back to the allocator before the launch: another copy of the same
+    call, or another thread, may be given its memory."""
+    args = {**_linear_calls(), **_attention_calls()}[name]
+    taken = []
+
+    class Library:
+        def __getattr__(self, function):
+            def call(*_):
+                if function.endswith(("_workspace", "_bytes")):
+                    return 64
+                assert all(ref() is not None for ref in taken), function
+                return Q.OFFQ_OK
+            return call
+
+    monkeypatch.setattr(Q, "load_library", Library)
+    monkeypatch.setattr(Q, "_ptr", lambda t: taken.append(weakref.ref(t)) if t is not None else None)
+    monkeypatch.setattr(Q, "_stream", lambda s: s)
+    getattr(Q, name)(*args)
+    assert taken
