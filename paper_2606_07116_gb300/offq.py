@@ -905,7 +905,8 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
                     cu_q: torch.Tensor, max_q: int, scale: Optional[float] = None, lse: bool = False,
                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """New tokens' queries q [Tq, Hq, hd] over the pages block_table [B, width] (int32) of lens [B] cached tokens;
-    sequence b's queries are rows cu_q[b] .. cu_q[b + 1] - 1 and its last tokens. Returns out, or (out, lse [Tq, Hq])."""
+    sequence b's queries are rows cu_q[b] .. cu_q[b + 1] - 1 and its last tokens. A length may not pass the columns of
+    block_table (a part of a wider table is copied). Returns out, or (out, lse [Tq, Hq])."""
     Tq, Hq, hd, ld_q = _heads(q)
     pages, H, page_size, _ = _cache_shape(cache, None, hd)
     B = lens.shape[0]
@@ -917,12 +918,10 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
     ld_table, inner = block_table.stride()
     if block_table.dtype is not torch.int32 or listed != B or (width > 1 and inner != 1):
         raise ValueError("block_table must be int32 [B, width] with contiguous rows")
-    if B > 1 and ld_table != width and (
-            ld_table < width or block_table.storage_offset() + B * ld_table > block_table.untyped_storage().nbytes() // 4):
-        # Rows of one another, or a last row whose ld_table entries pass the end of its memory: the kernels allow
-        # lengths of ld_table pages.
+    if B > 1 and ld_table != width:
+        # The library's ld_table is the pages a sequence can hold as well as the way to the next row: columns that were
+        # not given would count as pages.
         block_table = block_table.contiguous()
-        ld_table = width
     ld_out = Hq * hd
     if out is None:
         out = torch.empty((Tq, Hq, hd), dtype=q.dtype, device=q.device)
@@ -938,7 +937,7 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
         workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None
     stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
     offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table,
-                         ld_table if B > 1 else width, lens, cu_q, B, max_q,
+                         width, lens, cu_q, B, max_q,
                          scale if scale is not None else hd ** -0.5, out, ld_out, stats, workspace,
                          workspace.nbytes if workspace is not None else 0, stream)
     return (out, stats) if lse else out
