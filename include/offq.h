@@ -682,7 +682,8 @@ int offq_kv4_paged_read(const uint8_t* k_codes, const float* k_params, const uin
  *             OFFQ_BF16 or OFFQ_F16 (OFFQ_F32: OFFQ_ERR_UNSUPPORTED), 16-byte
  *             aligned, ld_q a multiple of 8; in the keys' rotated basis.
  *   Tq        query rows in all sequences; Hq a multiple of H, Hq / H <= 64.
- *   block_table  device, [B][ld_table] int32: the pages of a sequence, in order.
+ *   block_table  device, [B][ld_table] int32: the pages of a sequence, in order
+ *             (NULL where ld_table is 0: no sequence holds a token).
  *             Entries past its length are not read; one outside [0, pages) counts
  *             as a page of nothing that is seen, and is recorded in the device
  *             status word, as is a length past ld_table * page_size (cut there).

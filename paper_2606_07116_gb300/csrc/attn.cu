@@ -59,7 +59,7 @@ extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_
   if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || pages > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
   if (Tq == 0 || B == 0 || max_q == 0) return OFFQ_OK;
   if (q == nullptr || k_codes == nullptr || k_params == nullptr || v_codes == nullptr || v_params == nullptr ||
-      block_table == nullptr || lens == nullptr || cu_q == nullptr || out == nullptr)
+      (block_table == nullptr && ld_table > 0) || lens == nullptr || cu_q == nullptr || out == nullptr)
     return OFFQ_ERR_INVALID_ARG;
   if (!row_ok(q, ld_q) || !row_ok(out, ld_out) || !aligned(k_codes, 16) || !aligned(k_params, 16) ||
       !aligned(v_codes, 16) || !aligned(v_params, 16) || !aligned(block_table, 4) || !aligned(lens, 4) ||

@@ -41,3 +41,17 @@ def test_columns_of_a_wider_table(n, rows, columns):
     got = Q.paged_attention(q, cache, view, lens, cu, n)
     assert Q.offq_get_device_status() == Q.OFFQ_ERR_INVALID_ARG
     assert torch.equal(got[n:], want[n:])  # the other sequences are unharmed
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_table_without_columns(n):
+    """Sequences that hold nothing yet: zeros and -inf; a length that has no page is reported."""
+    q, cache, wide, cu = _inputs(n)
+    for table in (wide[:3, :0], torch.empty((3, 0), dtype=torch.int32, device="cuda")):
+        lens = torch.zeros(3, dtype=torch.int32, device="cuda")
+        out, lse = Q.paged_attention(q, cache, table, lens, cu, n, lse=True)
+        assert torch.all(out == 0) and torch.all(lse == float("-inf"))
+        assert Q.offq_get_device_status() == Q.OFFQ_OK
+        lens[1] = 1
+        Q.paged_attention(q, cache, table, lens, cu, n)
+        assert Q.offq_get_device_status() == Q.OFFQ_ERR_INVALID_ARG
