@@ -644,6 +644,8 @@ int offq_rope_heads(const void* x, int dtype, int64_t T, int32_t H, int32_t head
  *   slots     device, [T] int64. A negative slot writes no key or value; one
  *             past the cache records OFFQ_ERR_INVALID_ARG in the device status
  *             word and writes none. Two tokens of a call may not share a slot.
+ *   positions as in offq_rope_heads: one outside the table leaves the token's
+ *             query and slot (its value too) as they are.
  *   flags     OR of OFFQ_ROTATE (queries and keys), OFFQ_OFFSET,
  *             OFFQ_INTERLEAVED, OFFQ_ROTATE_V.
  */

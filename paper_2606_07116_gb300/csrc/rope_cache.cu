@@ -344,12 +344,14 @@ __device__ __forceinline__ void run_heads(const HeadArgs& a, int64_t t, int h0, 
   bool ok = true;
   Angles ang;
   const float* row = nullptr;
-  if (KIND < 2 && a.rot != 0) {
+  if (a.rot != 0) {  // of a value too: a slot does not get a new value beside an old key
     const int64_t p = __ldg(a.pos + t);
     ok = p >= 0 && p < a.max_pos;
     if (!ok && lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-    row = a.table + (ok ? p : 0) * a.rot;
-    load_angles<D>(a, row, l, ang);
+    if constexpr (KIND < 2) {
+      row = a.table + (ok ? p : 0) * a.rot;
+      load_angles<D>(a, row, l, ang);
+    }
   }
   uint8_t* codes = nullptr;
   float* params = nullptr;
