@@ -14,10 +14,10 @@
 //   * out = (O + sum p o_v) / sum p: the values' offsets add the same to every channel.
 //   * Work is the list of (row pair tile, block) steps; the CTAs take equal shares of it, and what crosses CTAs
 //     is joined by a second kernel from at most two parts per CTA.
-// P' is a half, and the values q are: the reference m of the exponentials carries the largest value scale of the block,
-// so that P' stays in range whatever the values' size is. 32 keys at a time are weighed against the reference they meet;
-// only where a row's 32 weights sum to more than 2^kMostLog2 the maxima are taken, what was summed and stored so far is rescaled and
-// the 32 are weighed again. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
+// P' is a half, and the values q are: the reference m of a row's exponentials is the largest z + log2(s_v) of the keys that it
+// sees (or up to kMostLog2 below it), so that the largest P' is 1 to 2^kMostLog2 whatever the values' size is. 32 keys at a time are
+// weighed against the reference they meet; only where a row's weights times the block's largest s_v could pass 2^kMostLog2 the maxima
+// are taken, and only where one does, what was summed and stored so far is rescaled and the 32 are weighed again. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
 // memory leave (four reloads in a row cost more than the products of a block).
 //
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 finds the CTA's work, warps
@@ -40,6 +40,7 @@ constexpr int kThreads = 512;
 constexpr int kPairRows = 2 * kQt;
 // A weight times its value's scale, as a half, reaches 2^14 before a row's reference is moved (and is 1 at most after it).
 constexpr float kMostLog2 = 14.f;
+constexpr float kLeastLog2 = -24.f;  // of a value's scale in a reference: smaller ones count as this
 // Registers: 128 a thread at launch, 2 x 144 + 96 + 128 = 4 x 128.
 constexpr int kSoftmaxRegs = 144, kIssueRegs = 96, kWidenRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kWidenRegs <= 4 * 128, "register shares");
@@ -539,9 +540,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             const int key0 = (w.blk + j) * kKt;
             const uint4 gone = *reinterpret_cast<const uint4*>(ctrl->missing[slot]);
             const float4 sm = *reinterpret_cast<const float4*>(ctrl->smax[slot]);
-            // log2 of the block's largest value scale, rounded up: weights times scales stay below 2^kMostLog2.
+            // log2 of the block's largest value scale, rounded up: weights up to 2^(kMostLog2 - lift) stay below 2^kMostLog2 with it.
             const float big = fmaxf(fmaxf(sm.x, sm.y), fmaxf(sm.z, sm.w));
-            const float lift = static_cast<float>(min(64, max(-24, static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
+            const float lift = static_cast<float>(min(64, max(static_cast<int>(kLeastLog2), static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
             const float most = ex2(kMostLog2 - lift);
             const bool masked = key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u;
             int sees[4] = {0, 0, 0, 0};
@@ -610,27 +611,42 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                 row_sum[x] = y0 + y1;
                 fits &= row_sum[x] <= most;
               }
-              if (__any_sync(kAllLanes, !fits)) {  // some row's reference moves
+              // Where some row's may not: the largest z + log2 of the value's scale among the keys it sees. A large scale that is
+              // not seen or hardly weighs moves no reference.
+              if (__any_sync(kAllLanes, !fits)) {
                 float keep[4];
+                bool move = false;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  float top = -INFINITY;
+                for (int x = 0; x < 4; ++x) keep[x] = -INFINITY;
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) {
-                    const float4 f = lds128f(pkq + k * 4);
+                for (int k = 0; k < 4; ++k) {
+                  const float4 f = lds128f(pkq + k * 4), v = lds128f(pvq + k * 4);
+                  const float v0 = fmaxf(__log2f(v.x), kLeastLog2), v1 = fmaxf(__log2f(v.y), kLeastLog2);
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
                     const uint32_t* e = &s[x >> 1][4 * k + 2 * (x & 1)];
                     const float z0 = fmaf(__uint_as_float(e[0]), f.x, f.z * qs[x]), z1 = fmaf(__uint_as_float(e[1]), f.y, f.w * qs[x]);
-                    top = fmaxf(top, fmaxf(z0, z1));  // hidden keys are NaN and do not count
+                    keep[x] = fmaxf(keep[x], fmaxf(z0 + v0, z1 + v1));  // hidden keys are NaN and do not count
                   }
-                  top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, 1));
-                  top = fmaxf(top, __shfl_xor_sync(kAllLanes, top, 2));
-                  top = fmaxf(top + lift, m[x]);
-                  keep[x] = m[x] == -INFINITY ? 0.f : ex2(m[x] - top);
-                  m[x] = top;
-                  l[x] *= keep[x];
-                  off[x] *= keep[x];
                 }
-                if (j > 0) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  keep[x] = fmaxf(keep[x], __shfl_xor_sync(kAllLanes, keep[x], 1));
+                  keep[x] = fmaxf(keep[x], __shfl_xor_sync(kAllLanes, keep[x], 2));
+                  move |= keep[x] > m[x] + kMostLog2;
+                }
+                move = __any_sync(kAllLanes, move);
+                if (move) {
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
+                    const float top = fmaxf(keep[x], m[x]);
+                    keep[x] = m[x] == -INFINITY ? 0.f : ex2(m[x] - top);
+                    m[x] = top;
+                    l[x] *= keep[x];
+                    off[x] *= keep[x];
+                  }
+                }
+                if (move && j > 0) {
 #pragma unroll 1
                   for (int u = 0; u < D / 32; ++u) {
                     uint32_t o0[16], o1[16];
@@ -646,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                 }
                 tmem_st_wait();
 #pragma unroll 1
-                for (int u = 0; u < 2 * q; ++u) {  // this block's weights so far
+                for (int u = 0; u < (move ? 2 * q : 0); ++u) {  // this block's weights so far
                   const uint32_t at = s_tm + 16 * (u >> 1) + (static_cast<uint32_t>(16 * (u & 1)) << 16);
                   uint32_t r[8];
                   tmem_ld_pairs(at, r);
