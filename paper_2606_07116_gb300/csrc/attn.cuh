@@ -14,6 +14,9 @@ namespace offq {
 constexpr uint32_t kAllLanes = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+// Paged: what a value's scale adds to the reference of a row's exponentials is its log2, this at least (zero has none). An
+// exponential is then 2^(64 + kMostLog2) at most, and its sums over any context stay far from an overflow.
+constexpr float kLeastLog2 = -64.f;
 
 struct AttnArgs {
   const void* q;

@@ -40,7 +40,6 @@ constexpr int kThreads = 512;
 constexpr int kPairRows = 2 * kQt;
 // A weight times its value's scale, as a half, reaches 2^14 before a row's reference is moved (and is 1 at most after it).
 constexpr float kMostLog2 = 14.f;
-constexpr float kLeastLog2 = -24.f;  // of a value's scale in a reference: smaller ones count as this
 // Registers: 128 a thread at launch, 2 x 144 + 96 + 128 = 4 x 128.
 constexpr int kSoftmaxRegs = 144, kIssueRegs = 96, kWidenRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kWidenRegs <= 4 * 128, "register shares");
@@ -542,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             const float4 sm = *reinterpret_cast<const float4*>(ctrl->smax[slot]);
             // log2 of the block's largest value scale, rounded up: weights up to 2^(kMostLog2 - lift) stay below 2^kMostLog2 with it.
             const float big = fmaxf(fmaxf(sm.x, sm.y), fmaxf(sm.z, sm.w));
-            const float lift = static_cast<float>(min(64, max(static_cast<int>(kLeastLog2), static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
+            const float lift = static_cast<float>(min(128, max(static_cast<int>(kLeastLog2), static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
             const float most = ex2(kMostLog2 - lift);
             const bool masked = key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u;
             int sees[4] = {0, 0, 0, 0};

@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
           for (int i = 0; i < 2; ++i) {  // what nobody sees may hold anything
             none[half][i] = t * kTile + half * 16 + tok_k + 8 * i >= s.len || (gone >> half & 1u);
             if (none[half][i]) sv[half][i] = ov[half][i] = 0.f;
-            lift[half][i] = fmaxf(__log2f(sv[half][i]), -24.f);
+            lift[half][i] = fmaxf(__log2f(sv[half][i]), kLeastLog2);
           }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {

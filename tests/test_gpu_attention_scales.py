@@ -120,3 +120,9 @@ def test_scales_of_zero(n, Hq, D, dt):
     """Values that are their offset alone: all of them, a first block of them, every other one."""
     for i, some in enumerate((np.ones(L, bool), np.arange(L) < 140, np.arange(L) % 2 == 0)):
         _run(np.where(some, 0.0, 0.5), n, Hq, D, dt, seed=6 + i)
+
+
+@pytest.mark.parametrize("n,Hq,D", [(n, Hq, D) for n, Hq, D, dt in FORMS if dt == "bf16"])
+@pytest.mark.parametrize("lo,hi", [(-45, -45), (-60, -60), (-55, -30), (70, 70), (60, 100), (-60, 100)])
+def test_tiny_and_huge_scales(n, Hq, D, lo, hi):
+    _run(2.0 ** np.random.default_rng(9).uniform(lo, hi, L), n, Hq, D, "bf16", seed=9)
