@@ -688,7 +688,8 @@ int offq_kv4_paged_read(const uint8_t* k_codes, const float* k_params, const uin
  *             (NULL where ld_table is 0: no sequence holds a token).
  *             Entries past its length are not read; one outside [0, pages) counts
  *             as a page of nothing that is seen, and is recorded in the device
- *             status word, as is a length past ld_table * page_size (cut there).
+ *             status word, as is a length past ld_table * page_size or
+ *             2^31 - 256 (cut there).
  *   lens      device, [B] int32.   cu_q  device, [B + 1] int32, cu_q[0] = 0,
  *             non-decreasing, cu_q[B] <= Tq.
  *   max_q     most queries of one sequence. A sequence with more is recorded in

@@ -48,6 +48,9 @@ struct AttnArgs {
   int* status;
 };
 
+// Most tokens of a sequence: the number of a token past its end by up to two blocks of 128 is an int.
+constexpr int kMostTokens = 0x7FFFFF00;
+
 // A sequence of the paged call: its first query row, queries and cached tokens. One whose entries are out of
 // range (negative or too long counts) has no queries; `bad` says so.
 struct PagedSeq {
@@ -57,7 +60,7 @@ struct PagedSeq {
 
 __device__ __forceinline__ PagedSeq paged_seq(const AttnArgs& a, int b) {
   const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1), l = __ldg(a.lens + b);
-  const int64_t most = min(a.ld_table << a.page_shift, static_cast<int64_t>(0x7FFFFFC0));
+  const int64_t most = min(a.ld_table << a.page_shift, static_cast<int64_t>(kMostTokens));
   PagedSeq s;
   s.first = c0;
   s.n = c1 - c0;

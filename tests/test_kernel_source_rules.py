@@ -148,3 +148,14 @@ def test_a_request_in_flight_is_waited_for_before_the_cta_ends():
     given_up = block(take, take.index("if (!wait(&ctrl->taken"))
     assert "mbar_wait_teardown(bar, taken & 1)" in given_up
     assert given_up.index("mbar_wait_teardown") < given_up.index("taken = -1") < given_up.index("return -1")
+
+
+def test_token_numbers_of_the_longest_context_fit_an_int():
+    """Lengths are cut at kMostTokens so that a token's number plus a stage or a block of tokens stays an int."""
+    most = int(re.search(r"constexpr int kMostTokens = (0x[0-9A-Fa-f]+);", source("attn.cuh")).group(1), 16)
+    largest = 0
+    for name in ("attn_few.cu", "attn_chunk.cu", "attn_tc.cuh"):
+        for m in re.finditer(r"constexpr int (?:kTile|kKt) = (\d+);", source(name)):
+            largest = max(largest, int(m.group(1)))
+    assert largest == 128 and most + 2 * largest <= 2 ** 31
+    assert "kMostTokens" in block(source("attn.cuh"), source("attn.cuh").index("PagedSeq paged_seq("))
