@@ -672,6 +672,7 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int c
   }
   __syncthreads();
   const int last = s_last;
+  if (last >= ctas) return;  // not this call's parts (a workspace that another call writes): none is read past them
   const int rows = p.rows, h = p.id % a.H;
   for (int u = tid; u < rows * (D / 8); u += blockDim.x) {
     const int r = u / (D / 8), d = u % (D / 8) * 8;

@@ -159,3 +159,11 @@ def test_token_numbers_of_the_longest_context_fit_an_int():
             largest = max(largest, int(m.group(1)))
     assert largest == 128 and most + 2 * largest <= 2 ** 31
     assert "kMostTokens" in block(source("attn.cuh"), source("attn.cuh").index("PagedSeq paged_seq("))
+
+
+def test_joining_kernels_read_the_parts_of_the_call_alone():
+    """A part whose last one is not among the CTAs' (a CTA gave up, or a workspace that two streams write) is left: the
+    loops over parts end at the last CTA's."""
+    for name, kernel in (("attn_few.cu", "join_parts_kernel(const"), ("attn_chunk.cu", "join_chunks_kernel(const")):
+        body = block(source(name), source(name).index(kernel))
+        assert body.index("if (last >= ctas) return;") < body.index("<= last")
