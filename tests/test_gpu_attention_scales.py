@@ -35,11 +35,44 @@ def _lib():
     Q.load_library()
 
 
+def check_paged(out, lse, q, keys, values, scale, dt, rounds):
+    """The rows of one sequence, its last tokens, against the oracle. keys, values: as A.cached gives them; rounds: how
+    often a weight is rounded."""
+    _, unit, least = DT[dt]
+    (k, kq, ks, ko), (v, vq, vs, vo) = keys, values
+    n, Hq, D = q.shape
+    tokens, G = k.shape[0], Hq // k.shape[1]
+    sees = np.array([tokens - n + i + 1 for i in range(n)])
+    ref, ref_lse, w = A.attention(q, k, v, scale, sees)
+    if n == 0:
+        return
+    empty = np.isinf(ref_lse)
+    assert np.array_equal(empty, np.isinf(lse)) and np.all(lse[empty] < 0) and np.all(out[empty] == 0)
+    if tokens == 0:
+        return
+    k_mag = (np.abs(kq) + 24) * ks[..., None] + np.abs(ko)[..., None]
+    for h in range(Hq):
+        g = h // G
+        mags = np.where(np.arange(tokens) < sees[:, None], np.abs(q[:, h]) @ k_mag[:, g].T * scale, 0).max(-1)
+        dz = (2 * D + 8) * U32 * mags + 4 * U32 * (mags + 128)
+        coded = w[:, h] @ (np.abs(vq[:, g]) * vs[:, g, None])
+        spread = coded + w[:, h] @ np.broadcast_to(np.abs(vo[:, g, None]), vq[:, g].shape)
+        top = (w[:, h] * vs[:, g]).max(-1)
+        tol = (2 * (dz + 2.0 ** -18 + 2 * tokens * U32)[:, None] * spread + rounds * 2.0 ** -11 * coded
+               + (rounds * 7 * tokens * 2.0 ** -25 * top)[:, None] + unit * np.abs(ref[:, h]) + least)
+        assert np.all(np.isfinite(out[:, h]))
+        worst = np.max(np.abs(out[:, h] - ref[:, h]) / (tol + 1e-300))
+        assert worst <= 1, (h, worst)
+        seen = ~empty[:, h]
+        assert np.all(np.abs(lse[seen, h] - ref_lse[seen, h]) <=
+                      (dz + 2.0 ** -18 + 2 * tokens * U32)[seen] + 2 * U32 * np.abs(ref_lse[seen, h]))
+
+
 def _run(scales, n, Hq, D, dt, unlikely=(), seed=0):
     """n new tokens at the end of L cached ones whose values have these scales (and offsets of a fifth of them, or 0.2
     where the scale is 0); the keys at `unlikely` have scores far below the others'."""
     rng = np.random.default_rng(seed)
-    kind, unit, least = DT[dt]
+    kind = DT[dt][0]
     pages = -(-L // PAGE)
     codes = [rng.integers(0, 256, (pages, H, PAGE, D // 2), dtype=np.uint8) for _ in range(2)]
     for c in codes:  # nibbles 1..15, as the quantizer leaves them
@@ -60,26 +93,8 @@ def _run(scales, n, Hq, D, dt, unlikely=(), seed=0):
                                  torch.tensor([0, n], **i32), n, lse=True)
     assert Q.offq_get_device_status() == Q.OFFQ_OK
     out, lse, q = out.cpu().double().numpy(), lse.cpu().double().numpy(), q.double().numpy()
-    k, kq, ks, ko = A.cached(codes[0], pairs[0], at // PAGE, at % PAGE)
-    v, vq, vs, vo = A.cached(codes[1], pairs[1], at // PAGE, at % PAGE)
-    scale, G = D ** -0.5, Hq // H
-    sees = np.array([L - n + i + 1 for i in range(n)])
-    ref, ref_lse, w = A.attention(q, k, v, scale, sees)
-    k_mag = (np.abs(kq) + 24) * ks[..., None] + np.abs(ko)[..., None]
-    rounds = 1 if n * G <= 16 else 4
-    for h in range(Hq):
-        g = h // G
-        mags = np.where(at < sees[:, None], np.abs(q[:, h]) @ k_mag[:, g].T * scale, 0).max(-1)
-        dz = (2 * D + 8) * U32 * mags + 4 * U32 * (mags + 128)
-        spread = w[:, h] @ (np.abs(vq[:, g]) * vs[:, g, None] + np.abs(vo[:, g, None]))
-        coded = w[:, h] @ (np.abs(vq[:, g]) * vs[:, g, None])
-        top = (w[:, h] * vs[:, g]).max(-1)
-        tol = (2 * (dz + 2.0 ** -18 + 2 * L * U32)[:, None] * spread + rounds * 2.0 ** -11 * coded
-               + (rounds * 7 * L * 2.0 ** -25 * top)[:, None] + unit * np.abs(ref[:, h]) + least)
-        assert np.all(np.isfinite(out[:, h]))
-        worst = np.max(np.abs(out[:, h] - ref[:, h]) / tol)
-        assert worst <= 1, (h, worst)
-        assert np.all(np.abs(lse[:, h] - ref_lse[:, h]) <= dz + 2.0 ** -18 + 2 * L * U32 + 2 * U32 * np.abs(ref_lse[:, h]))
+    held = [A.cached(c, p, at // PAGE, at % PAGE) for c, p in zip(codes, pairs)]
+    check_paged(out, lse, q, *held, D ** -0.5, dt, 1 if n * Hq // H <= 16 else 4)
 
 
 FORMS = [(1, 2, 128, "bf16"), (1, 16, 64, "bf16"), (4, 8, 128, "bf16"), (7, 4, 64, "f16"),       # few rows
