@@ -13,7 +13,7 @@ namespace {
 using namespace offq;
 
 // What both calls ask of their queries, heads and outputs.
-int check_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int64_t ld_q,
+int check_attention(int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int64_t ld_q,
                     int32_t B, float scale, int64_t ld_out) {
   if (elem_bytes(dtype) == 0 || Tq < 0 || Hq < 1 || H < 1 || Hq % H != 0 || head_dim < 1 || B < 0)
     return OFFQ_ERR_INVALID_ARG;
@@ -40,7 +40,7 @@ bool row_ok(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0; }
 
 extern "C" int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
                                                   int32_t max_q) {
-  if (check_attention(nullptr, OFFQ_BF16, Tq, Hq, H, head_dim, int64_t{1} << 40, B, 1.f, int64_t{1} << 40) != OFFQ_OK ||
+  if (check_attention(OFFQ_BF16, Tq, Hq, H, head_dim, int64_t{1} << 40, B, 1.f, int64_t{1} << 40) != OFFQ_OK ||
       max_q < 0)
     return -1;
   if (Tq == 0 || B == 0 || max_q == 0) return 0;
@@ -54,7 +54,7 @@ extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_
                                     const int32_t* cu_q, int32_t B, int32_t max_q, float scale, void* out,
                                     int64_t ld_out, float* lse, void* workspace, int64_t workspace_bytes,
                                     void* stream) {
-  if (const int rc = check_attention(q, dtype, Tq, Hq, H, head_dim, ld_q, B, scale, ld_out); rc != OFFQ_OK) return rc;
+  if (const int rc = check_attention(dtype, Tq, Hq, H, head_dim, ld_q, B, scale, ld_out); rc != OFFQ_OK) return rc;
   if (pages < 1 || page_size < 1 || ld_table < 0 || max_q < 0 || workspace_bytes < 0) return OFFQ_ERR_INVALID_ARG;
   if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || pages > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
   if (Tq == 0 || B == 0 || max_q == 0) return OFFQ_OK;
@@ -84,7 +84,6 @@ extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_
   a.cu = cu_q;
   a.B = B;
   a.max_q = max_q;
-  a.causal = 1;
   a.scale = scale;
   a.out = out;
   a.ld_out = ld_out;
@@ -105,7 +104,7 @@ extern "C" int offq_prompt_attention(const void* q, const void* k, const void* v
                                      int32_t H, int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v,
                                      const int32_t* cu, int32_t B, float scale, int32_t causal, void* out,
                                      int64_t ld_out, float* lse, void* stream) {
-  if (const int rc = check_attention(q, dtype, T, Hq, H, head_dim, ld_q, B, scale, ld_out); rc != OFFQ_OK) return rc;
+  if (const int rc = check_attention(dtype, T, Hq, H, head_dim, ld_q, B, scale, ld_out); rc != OFFQ_OK) return rc;
   const int64_t width = static_cast<int64_t>(H) * head_dim;
   if (ld_k < width || ld_v < width) return OFFQ_ERR_INVALID_ARG;
   if (T == 0 || B == 0) return OFFQ_OK;

@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "offq.h"
 #include "offq_device.cuh"
 #include "offq_host.h"
@@ -39,7 +41,7 @@ struct AttnArgs {
   int B;
   int max_q;
   int few_rows;   // sequences with at most this many rows n * G take the few-row form
-  int causal;
+  int causal;     // prompts
   float scale;
   void* out;
   int64_t ld_out;
@@ -77,6 +79,36 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Nibbles n (0..3) of both 16-bit halves of w as two 16-bit floats 16 + u of type T: the bits land below the exponent
+// of 16.0 (mantissa weight 1 is bit 3 in bf16, bit 6 in f16).
+template <typename T>
+__device__ __forceinline__ uint32_t widen(uint32_t w, int n) {
+  constexpr bool kHalf = std::is_same<T, __half>::value;
+  constexpr int kAt = kHalf ? 6 : 3;
+  constexpr uint32_t kMask = (0xFu << kAt) * 0x10001u, kMagic = kHalf ? 0x4C004C00u : 0x41804180u;
+  const int sh = kAt - 4 * n;
+  const uint32_t x = sh >= 0 ? w << sh : w >> -sh;
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "n"(kMask), "n"(kMagic));  // (x & mask) | magic
+  return r;
+}
+
+// Nibbles 0 and 1 of both halves of w as signed codes q in f16 (2 and 3 of w shifted right by 8).
+__device__ __forceinline__ void widen_signed(uint32_t w, uint32_t& even, uint32_t& odd) {
+  uint32_t x, y;
+  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x) : "r"(w));  // 1024 + u
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(y) : "r"(w));  // 1024 + 16 u
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(even) : "r"(x), "r"(0x64086408u));                        // - 1032
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(odd) : "r"(y), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
+}
+
+// The log of a row's sum l of exponentials 2^(z - m), row r of (sequence starting at query row `first`, key head h).
+__device__ __forceinline__ void write_lse(const AttnArgs& a, int first, int h, int r, float m, float l) {
+  if (a.lse == nullptr) return;
+  a.lse[(static_cast<int64_t>(first) + r / a.G) * a.Hq + h * a.G + r % a.G] =
+      l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // The few-row form of offq_paged_attention (csrc/attn_few.cu): rows n * G of a sequence that it takes, its

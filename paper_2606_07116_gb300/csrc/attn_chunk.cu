@@ -117,27 +117,6 @@ struct Walk {
   }
 };
 
-// Nibbles n of both halves of w as 16 + u in T (see the few-row kernel).
-template <typename T>
-__device__ __forceinline__ uint32_t widen(uint32_t w, int n) {
-  constexpr bool kHalf = std::is_same<T, __half>::value;
-  constexpr int kAt = kHalf ? 6 : 3;
-  constexpr uint32_t kMask = (0xFu << kAt) * 0x10001u, kMagic = kHalf ? 0x4C004C00u : 0x41804180u;
-  const int sh = kAt - 4 * n;
-  const uint32_t x = sh >= 0 ? w << sh : w >> -sh;
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "n"(kMask), "n"(kMagic));
-  return r;
-}
-// Nibbles 0 and 1 of both halves of w as signed codes q in f16 (2 and 3 of w shifted right by 8).
-__device__ __forceinline__ void widen_signed(uint32_t w, uint32_t& even, uint32_t& odd) {
-  uint32_t x, y;
-  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x) : "r"(w));  // 1024 + u
-  asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(y) : "r"(w));  // 1024 + 16 u
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(even) : "r"(x), "r"(0x64086408u));                        // - 1032
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(odd) : "r"(y), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
-}
-
 // Byte offset of 16-byte chunk ch (8 channels) of row r in a swizzled tile.
 __device__ __forceinline__ uint32_t tile_off(int r, int ch) {
   return (ch >> 3) * kAtom + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
@@ -167,12 +146,6 @@ __device__ __forceinline__ void write_pair(T* row, int k, int lane, float x, flo
   const uint32_t v1 = __shfl_sync(kAllLanes, u, (lane & ~3) | ((2 * c + 1) & 3));
   if (row != nullptr) *reinterpret_cast<uint32_t*>(row + 8 * k + 2 * c) = __byte_perm(v0, v1, c < 2 ? 0x5410 : 0x7632);
 }
-__device__ __forceinline__ void write_lse(const AttnArgs& a, const PagedSeq& s, int h, int row, float m, float l) {
-  if (a.lse == nullptr) return;
-  a.lse[(static_cast<int64_t>(s.first) + row / a.G) * a.Hq + h * a.G + row % a.G] =
-      l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
-}
-
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   using L = ChunkLayout<D>;
@@ -668,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
 #pragma unroll
                   for (int e = 0; e < 8; ++e) {
                     const float k = u & 1 ? keep[2 + (e & 1)] : keep[e & 1];
-                    r[e] = scale_16<__half>(r[e], k);
+                    r[e] = scale_halves(r[e], k);
                   }
                   tmem_st_pairs(at, r);
                 }
@@ -722,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                 part[i * kQt + quad * 32 + r] = m[x];
                 part[kPairRows + i * kQt + quad * 32 + r] = l[x];
               } else if (row0 + r < rows) {
-                write_lse(a, w.s, w.h, row0 + r, m[x], l[x]);
+                write_lse(a, w.s.first, w.h, row0 + r, m[x], l[x]);
               }
             }
           }
@@ -834,7 +807,7 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
 #pragma unroll
       for (int k = 0; k < kReps; ++k)
         write_pair<T>(to, q * kReps + k, lane, (ii ? acc[hh][k].z : acc[hh][k].x) * inv, (ii ? acc[hh][k].w : acc[hh][k].y) * inv);
-      if (q == 0 && c == 0 && r < rows) write_lse(a, s, p.h, r, top[x], sum[x]);
+      if (q == 0 && c == 0 && r < rows) write_lse(a, s.first, p.h, r, top[x], sum[x]);
     }
 }
 

@@ -80,28 +80,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Nibbles n (0..3) of both 16-bit halves of w as two 16-bit floats 16 + u: the bits land below the exponent
-// of 16.0 (mantissa weight 1 is bit 3 in bf16, bit 6 in f16).
-template <bool HALF>
-__device__ __forceinline__ uint32_t widen(uint32_t w, int n) {
-  constexpr int kAt = HALF ? 6 : 3;
-  constexpr uint32_t kMask = (0xFu << kAt) * 0x10001u, kMagic = HALF ? 0x4C004C00u : 0x41804180u;
-  const int sh = kAt - 4 * n;
-  const uint32_t x = sh >= 0 ? w << sh : w >> -sh;
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "n"(kMask), "n"(kMagic));  // (x & mask) | magic
-  return r;
-}
-
-// Nibbles 0 and 1 of both halves of w as signed codes q in f16 (2 and 3 of w shifted right by 8).
-__device__ __forceinline__ void widen_signed(uint32_t w, uint32_t& even, uint32_t& odd) {
-  uint32_t x, y;
-  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x) : "r"(w));  // 1024 + u
-  asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(y) : "r"(w));  // 1024 + 16 u
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(even) : "r"(x), "r"(0x64086408u));                        // - 1032
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(odd) : "r"(y), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
-}
-
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -182,12 +160,6 @@ __device__ __forceinline__ void write_out8(const AttnArgs& a, int first, int h, 
   }
   *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + static_cast<int64_t>(h * a.G + r % a.G) * D + d) =
       make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-__device__ __forceinline__ void write_lse(const AttnArgs& a, int first, int h, int r, float m, float l) {
-  if (a.lse == nullptr) return;
-  a.lse[(static_cast<int64_t>(first) + r / a.G) * a.Hq + h * a.G + r % a.G] =
-      l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 template <int D, int NT, typename T>
@@ -410,8 +382,8 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         for (int i = 0; i < kKw; ++i) {
 #pragma unroll
           for (int n = 0; n < 4; n += 2) {
-            const uint32_t f[4] = {widen<kHalf>(k0.w[i], n), widen<kHalf>(k1.w[i], n), widen<kHalf>(k0.w[i], n + 1),
-                                   widen<kHalf>(k1.w[i], n + 1)};
+            const uint32_t f[4] = {widen<T>(k0.w[i], n), widen<T>(k1.w[i], n), widen<T>(k0.w[i], n + 1),
+                                   widen<T>(k1.w[i], n + 1)};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma16816(acc[half][nt], f, qf[nt][4 * i + n], qf[nt][4 * i + n + 1], kHalf);
           }

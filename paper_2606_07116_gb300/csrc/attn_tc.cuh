@@ -148,15 +148,10 @@ __device__ __forceinline__ uint32_t pack_16(float a, float b) {
   }
 }
 
-// A pair of weights times k.
-template <typename T>
-__device__ __forceinline__ uint32_t scale_16(uint32_t w, float k) {
-  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-    return pack_16<T>(__uint_as_float(w << 16) * k, __uint_as_float(w & 0xFFFF0000u) * k);
-  } else {
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    return pack_16<T>(v.x * k, v.y * k);
-  }
+// A pair of halves times k.
+__device__ __forceinline__ uint32_t scale_halves(uint32_t w, float k) {
+  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return pack_16<__half>(v.x * k, v.y * k);
 }
 
 __device__ __forceinline__ uint64_t add2_rn(uint64_t a, uint64_t b) {
