@@ -678,12 +678,19 @@ int offq_kv4_paged_read(const uint8_t* k_codes, const float* k_params, const uin
  *   lse_i = log sum_j e^z_j,
  * k_j and v_j the cached values s (u - 8) + o. A query that sees nothing
  * (len - n + i < 0) gets out 0 and lse -inf. The codes enter the products
- * exactly; softmax statistics and sums are fp32.
+ * exactly; softmax statistics and sums are fp32. What a key adds, its weight
+ * times the scale of its value, is rounded to a half (2^-11 of itself; a row of
+ * more than 16 queries and heads per key head may round it again, up to four
+ * times), in a range that follows the largest of the keys that the row sees:
+ * less than 2^-25 of that one adds its offset alone. Scales below 2^-64 count
+ * as 2^-64 there.
  *
  *   q         device, element (t, h, d) at q[t*ld_q + h*head_dim + d], dtype
  *             OFFQ_BF16 or OFFQ_F16 (OFFQ_F32: OFFQ_ERR_UNSUPPORTED), 16-byte
  *             aligned, ld_q a multiple of 8; in the keys' rotated basis.
- *   Tq        query rows in all sequences; Hq a multiple of H, Hq / H <= 64.
+ *   Tq        query rows in all sequences (up to 2^24); Hq a multiple of H, up to
+ *             4096, Hq / H <= 64; B up to 65535; 0 < scale <= 1e30. Rows of q
+ *             outside cu_q[0] .. cu_q[B] are left out, their rows of out as they are.
  *   block_table  device, [B][ld_table] int32: the pages of a sequence, in order
  *             (NULL where ld_table is 0: no sequence holds a token).
  *             Entries past its length are not read; one outside [0, pages) counts
@@ -716,7 +723,9 @@ int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_
  * offq_paged_attention; k and v [T][H][head_dim] with ld_k, ld_v (multiples of 8)
  * of the same type. cu: device, [B + 1] int32, non-decreasing, cu[B] <= T; rows
  * outside cu[0] .. cu[B] are left as they are. What one sequence holds (infinities
- * or NaN too) does not reach another's outputs.
+ * or NaN too) does not reach another's outputs. Scores, statistics and sums are
+ * fp32; the weights are rounded to the inputs' type for their product with v.
+ * Limits as in offq_paged_attention.
  */
 int offq_prompt_attention(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq, int32_t H,
                           int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v, const int32_t* cu, int32_t B,

@@ -14,16 +14,17 @@
 //   * out = (O + sum p o_v) / sum p: the values' offsets add the same to every channel.
 //   * Work is the list of (row pair tile, block) steps; the CTAs take equal shares of it, and what crosses CTAs
 //     is joined by a second kernel from at most two parts per CTA.
-// P' is a half, and the values q are: the reference m of a row's exponentials is the largest z + log2(s_v) of the keys that it
-// sees (or up to kMostLog2 below it), so that the largest P' is 1 to 2^kMostLog2 whatever the values' size is. 32 keys at a time are
-// weighed against the reference they meet; only where a row's weights times the block's largest s_v could pass 2^kMostLog2 the maxima
-// are taken, and only where one does, what was summed and stored so far is rescaled and the 32 are weighed again. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
+// P' is a half, and the values q are: the reference m of a row's exponentials is the largest z + log2(s_v) of the keys that
+// it sees (or up to kMostLog2 below it), so that the largest P' is 1 to 2^kMostLog2 whatever the values' size is. 32 keys at a
+// time are weighed against the reference they meet; only where a row's weights times the block's largest s_v could pass
+// 2^kMostLog2 the maxima are taken and the 32 are weighed again, and only where one does pass it, what was summed and stored so
+// far is rescaled before that. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
 // memory leave (four reloads in a row cost more than the products of a block).
 //
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 finds the CTA's work, warps
 // 12-15 widen.
 //
-// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 592 us, 815 TFLOP/s; 16 sequences of
+// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 599 us, 805 TFLOP/s; 16 sequences of
 // 8 tokens over 500 to 6000 122 us. What bounds it: with softmax, widening and reads left out the products take 341 us, since S has
 // both operands in shared memory, which delivers them at 77 % of the tensor rate; reads add about 80, widening 50, the
 // softmax 130. 16 softmax warps of 16 rows were slower (671 against 640), as were maxima taken before the weights (901).
