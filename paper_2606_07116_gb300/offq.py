@@ -804,7 +804,7 @@ def _heads(x: torch.Tensor) -> Tuple[int, int, int, int]:
     ld, between, inner = x.stride()
     if inner != 1 or (H > 1 and between != hd):
         raise ValueError("heads of a token must be contiguous")
-    return T, H, hd, ld if T > 1 else max(ld, H * hd)
+    return T, H, hd, ld if T > 1 else H * hd
 
 
 def _like(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple) -> None:
