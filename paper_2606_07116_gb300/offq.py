@@ -177,7 +177,9 @@ def _stream(stream):
 def _on(stream):
     """Context in which torch takes memory from, and runs behind, a stream given as such or as its handle."""
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream))
+        handle = int(stream)
+        # 0, 1 and 2 are the runtime's names for the default stream and the per-thread one, which is ordered with it.
+        stream = torch.cuda.ExternalStream(handle) if handle > 2 else torch.cuda.default_stream()
     return torch.cuda.stream(stream)
 
 

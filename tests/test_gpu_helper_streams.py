@@ -53,3 +53,16 @@ def test_outputs_are_not_memory_that_the_current_stream_still_uses(name, handle)
     assert not at & {g.data_ptr() for g in got}
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+@pytest.mark.parametrize("handle", [0, 1, 2])
+def test_the_runtimes_own_handles(handle):
+    """The default stream as 0 and as the runtime's legacy handle, and the per-thread default stream, which is ordered
+    with it."""
+    x = torch.randn((96, 4096), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    for call in list(_calls().values()) + [lambda **s: Q.quantize_act(x, 1024, **s)]:
+        want = call()
+        with torch.cuda.stream(torch.cuda.Stream()):   # not the current stream
+            got = call(stream=handle)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g.view(torch.uint8), w.view(torch.uint8)) for g, w in zip(got, want))

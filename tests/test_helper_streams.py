@@ -146,3 +146,11 @@ def test_copies_live_until_the_call(monkeypatch, name):
     monkeypatch.setattr(Q, "_stream", lambda s: s)
     getattr(Q, name)(*args)
     assert taken
+
+
+def test_the_runtimes_own_handles_stand_for_the_default_stream(monkeypatch):
+    """torch packs a stream's kind into its number, so the small handles 1 and 2 would be streams of its pools."""
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda: "default")
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: handle)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: s)
+    assert [Q._on(h) for h in (0, 1, 2, STREAM)] == ["default"] * 3 + [STREAM]
