@@ -43,6 +43,10 @@
  *   offq_kv4_paged_read    cached tokens back as values
  *   offq_paged_attention   new tokens (one or many per sequence) over the pages
  *   offq_prompt_attention  packed prompts on 16-bit keys and values
+ *   offq_paged_attention_window, offq_prompt_attention_window
+ *                          both over a sliding window and a few first tokens
+ *   offq_paged_attention_prefix
+ *                          for batches whose sequences share long prefixes
  *
  * Conventions shared by every call
  *   - Pointers named as device buffers are device pointers allocated and owned
@@ -712,7 +716,55 @@ int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32
                          const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q, float scale, void* out,
                          int64_t ld_out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
-/* Bytes of offq_paged_attention's workspace on the current device (-1 on sizes
+/*
+ * offq_paged_attention_window -- offq_paged_attention for layers with a sliding
+ * window: the query at position p = len - n + i of its sequence sees the tokens
+ * j <= p with j > p - window or j < sinks. Tokens that no query of the sequence
+ * sees are not read, and may have been given back: the slots may hold anything,
+ * and entries of block_table whose pages hold nothing else are not looked at.
+ * The same rows, workspace, roundings and errors.
+ *   window    newest tokens up to the query itself, 1 at least.
+ *   sinks     first tokens of the sequence that stay visible, 0 at least.
+ */
+int offq_paged_attention_window(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
+                                int64_t ld_q, const uint8_t* k_codes, const float* k_params, const uint8_t* v_codes,
+                                const float* v_params, int64_t pages, int32_t page_size, const int32_t* block_table,
+                                int64_t ld_table, const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q,
+                                float scale, int32_t window, int32_t sinks, void* out, int64_t ld_out, float* lse,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * offq_paged_attention_prefix -- offq_paged_attention for batches whose sequences
+ * stand behind shared prefixes: prefix g is the first prefix_lens[g] tokens of the
+ * pages prefix_table[g], the sequences cu_prefix[g] .. cu_prefix[g + 1] - 1 share it,
+ * and their block_table and lens list the tokens after it. Query i of a sequence sees
+ * all of its prefix and tokens 0 .. len - n + i of its own (none where that is
+ * negative). Each prefix is read once for all queries of its sequences, whose rows in
+ * q follow each other. Every part of a row is summed as in offq_paged_attention, and
+ * both are joined in fp32.
+ *   prefix_table  device, [P][ld_prefix] int32, as block_table (the pages may be
+ *             in other rows too).   prefix_lens  device, [P] int32.
+ *   cu_prefix device, [P + 1] int32, non-decreasing, cu_prefix[P] <= B. Sequences
+ *             outside cu_prefix[0] .. cu_prefix[P] have no prefix, nor have those
+ *             of a prefix whose entries, or whose queries' count (over B * max_q or
+ *             Tq), are out of range; such a prefix, as one longer than
+ *             ld_prefix * page_size or 2^31 - 2^25 (cut there), is recorded in the
+ *             device status word.
+ *   P         prefixes, up to 65535 (0: offq_paged_attention).
+ *   workspace offq_paged_attention_prefix_workspace(...) bytes: 8 head_dim + 16
+ *             for each query and head on top of offq_paged_attention's.
+ */
+int offq_paged_attention_prefix(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
+                                int64_t ld_q, const uint8_t* k_codes, const float* k_params, const uint8_t* v_codes,
+                                const float* v_params, int64_t pages, int32_t page_size, const int32_t* block_table,
+                                int64_t ld_table, const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q,
+                                const int32_t* prefix_table, int64_t ld_prefix, const int32_t* prefix_lens,
+                                const int32_t* cu_prefix, int32_t P, float scale, void* out, int64_t ld_out, float* lse,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
+                                              int32_t max_q, int32_t P);
+
+/* Bytes of offq_paged_attention's workspace (and of the call's with a window) on the current device (-1 on sizes
  * it refuses). */
 int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B, int32_t max_q);
 
@@ -730,6 +782,18 @@ int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_
 int offq_prompt_attention(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq, int32_t H,
                           int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v, const int32_t* cu, int32_t B,
                           float scale, int32_t causal, void* out, int64_t ld_out, float* lse, void* stream);
+
+/*
+ * offq_prompt_attention_window -- offq_prompt_attention (causal) for layers with a
+ * sliding window: query i sees the keys j <= i with j > i - window or j < sinks.
+ * What stands between the sinks and the window of all queries of a tile (128 or
+ * 256 of a head) costs nothing.
+ *   window, sinks  as in offq_paged_attention_window.
+ */
+int offq_prompt_attention_window(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq, int32_t H,
+                                 int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v, const int32_t* cu, int32_t B,
+                                 float scale, int32_t window, int32_t sinks, void* out, int64_t ld_out, float* lse,
+                                 void* stream);
 
 /* Bytes of a tiled MXFP4 shift buffer for R rows of K channels (-1 unless K is
  * a positive multiple of 128 and R >= 0): ceil(R/32) * 32 * K / 32. */

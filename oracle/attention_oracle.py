@@ -82,3 +82,27 @@ def attention(q, k, v, scale, sees):
             w[i, h, :m] = e / e.sum()
             out[i, h] = w[i, h, :m] @ v[:m, h * H // Hq]
     return out, lse, w
+
+
+def attention_masked(q, k, v, scale, seen):
+    """The same where query i sees the keys of seen [n, L] (bool)."""
+    n, Hq, D = q.shape
+    L, H = k.shape[0], k.shape[1]
+    out, lse, w = np.zeros((n, Hq, D)), np.full((n, Hq), -np.inf), np.zeros((n, Hq, L))
+    some = seen.any(1)
+    if not some.any():
+        return out, lse, w
+    for h in range(Hq):
+        z = np.where(seen[some], q[some, h] @ k[:, h * H // Hq].T * scale, -np.inf)
+        top = z.max(1, keepdims=True)
+        e = np.exp(z - top)
+        lse[some, h] = top[:, 0] + np.log(e.sum(1))
+        w[some, h] = e / e.sum(1, keepdims=True)
+        out[some, h] = w[some, h] @ v[:, h * H // Hq]
+    return out, lse, w
+
+
+def in_window(at, n, L, window, sinks):
+    """[n, L]: which tokens queries at positions at .. at + n - 1 see under a sliding window with sinks."""
+    p, j = at + np.arange(n)[:, None], np.arange(L)[None]
+    return (j <= p) & ((j > p - window) | (j < sinks))

@@ -1,6 +1,7 @@
 // Attention's entry points: packed prompts on 16-bit keys and values (offq_prompt_attention,
 // csrc/attn_prompt.cu) and new tokens over the paged 4-bit cache (offq_paged_attention: csrc/attn_few.cu
-// for few rows per sequence and key head, csrc/attn_chunk.cu for many).
+// for few rows per sequence and key head, csrc/attn_chunk.cu for many); either over a window and sinks, and the latter
+// behind prefixes that sequences share (csrc/attn_prefix.cu joins what the forms found).
 //
 // out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j - m_i),  lse_i = m_i + log sum_j p_ij
 // over the keys j that query i sees, m_i any number near their largest score.
@@ -34,6 +35,14 @@ int64_t workspace_bytes_for(int head_dim, int64_t most_rows) {
   return most_rows > kFewRows ? std::max(few, chunk) : few;
 }
 
+// Behind shared prefixes: the most rows that a prefix may have, and the bytes of all rows' two sums and statistics.
+int64_t shared_rows(int64_t Tq, int32_t B, int32_t max_q, int32_t G) {
+  return std::min(Tq, static_cast<int64_t>(B) * max_q) * G;
+}
+int64_t sums_bytes(int64_t Tq, int32_t Hq, int32_t head_dim) {
+  return 2 * Tq * Hq * (static_cast<int64_t>(sizeof(float)) * head_dim + static_cast<int64_t>(sizeof(float2)));
+}
+
 bool row_ok(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0; }
 
 }  // namespace
@@ -47,37 +56,81 @@ extern "C" int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_
   return workspace_bytes_for(head_dim, static_cast<int64_t>(max_q) * (Hq / H));
 }
 
-extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
-                                    int64_t ld_q, const uint8_t* k_codes, const float* k_params,
-                                    const uint8_t* v_codes, const float* v_params, int64_t pages, int32_t page_size,
-                                    const int32_t* block_table, int64_t ld_table, const int32_t* lens,
-                                    const int32_t* cu_q, int32_t B, int32_t max_q, float scale, void* out,
-                                    int64_t ld_out, float* lse, void* workspace, int64_t workspace_bytes,
-                                    void* stream) {
-  if (const int rc = check_attention(dtype, Tq, Hq, H, head_dim, ld_q, B, scale, ld_out); rc != OFFQ_OK) return rc;
-  if (pages < 1 || page_size < 1 || ld_table < 0 || max_q < 0 || workspace_bytes < 0) return OFFQ_ERR_INVALID_ARG;
-  if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || pages > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
-  if (Tq == 0 || B == 0 || max_q == 0) return OFFQ_OK;
-  if (q == nullptr || k_codes == nullptr || k_params == nullptr || v_codes == nullptr || v_params == nullptr ||
-      (block_table == nullptr && ld_table > 0) || lens == nullptr || cu_q == nullptr || out == nullptr)
+extern "C" int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
+                                                         int32_t max_q, int32_t P) {
+  if (P < 0 || P > 65535) return -1;
+  const int64_t parts = offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q);
+  if (parts <= 0 || P == 0) return parts;
+  const int64_t most = workspace_bytes_for(head_dim, shared_rows(Tq, B, max_q, Hq / H));
+  return most < 0 ? -1 : most + sums_bytes(Tq, Hq, head_dim);
+}
+
+namespace {
+
+// The paged calls' own arguments: checks and launches. `mode` says which of them was made.
+int paged_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, int32_t page_size, int64_t workspace_bytes,
+               void* stream) {
+  if (const int rc = check_attention(dtype, a.Tq, a.Hq, a.H, head_dim, a.ld_q, a.B, a.scale, a.ld_out); rc != OFFQ_OK)
+    return rc;
+  if (a.pages < 1 || page_size < 1 || a.ld_table < 0 || a.max_q < 0 || workspace_bytes < 0) return OFFQ_ERR_INVALID_ARG;
+  if (mode == kWindowed && (a.window < 1 || a.sinks < 0)) return OFFQ_ERR_INVALID_ARG;
+  if (mode == kShared && (a.P < 0 || a.ld_prefix < 0)) return OFFQ_ERR_INVALID_ARG;
+  if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || a.pages > (int64_t{1} << 31)) return OFFQ_ERR_UNSUPPORTED;
+  if (mode == kShared && a.P > 65535) return OFFQ_ERR_UNSUPPORTED;
+  if (a.Tq == 0 || a.B == 0 || a.max_q == 0) return OFFQ_OK;
+  if (a.q == nullptr || a.k_codes == nullptr || a.k_params == nullptr || a.v_codes == nullptr || a.v_params == nullptr ||
+      (a.table == nullptr && a.ld_table > 0) || a.lens == nullptr || a.cu == nullptr || a.out == nullptr)
     return OFFQ_ERR_INVALID_ARG;
-  if (!row_ok(q, ld_q) || !row_ok(out, ld_out) || !aligned(k_codes, 16) || !aligned(k_params, 16) ||
-      !aligned(v_codes, 16) || !aligned(v_params, 16) || !aligned(block_table, 4) || !aligned(lens, 4) ||
-      !aligned(cu_q, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
+  if (mode == kShared && a.P == 0) mode = kCausal;
+  if (mode == kShared && ((a.prefix_table == nullptr && a.ld_prefix > 0) || a.prefix_lens == nullptr || a.cu_prefix == nullptr))
+    return OFFQ_ERR_INVALID_ARG;
+  if (!row_ok(a.q, a.ld_q) || !row_ok(a.out, a.ld_out) || !aligned(a.k_codes, 16) || !aligned(a.k_params, 16) ||
+      !aligned(a.v_codes, 16) || !aligned(a.v_params, 16) || !aligned(a.table, 4) || !aligned(a.lens, 4) ||
+      !aligned(a.cu, 4) || !aligned(a.lse, 4) || !aligned(a.workspace, 16))
     return OFFQ_ERR_MISALIGNED;
+  if (mode == kShared && (!aligned(a.prefix_table, 4) || !aligned(a.prefix_lens, 4) || !aligned(a.cu_prefix, 4)))
+    return OFFQ_ERR_MISALIGNED;
+  a.G = a.Hq / a.H;
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  a.window = std::min(a.window, kMostTokens);
+  a.sinks = std::min(a.sinks, kMostTokens);
+  a.status = device_status_ptr();
+  const int64_t own_rows = static_cast<int64_t>(a.max_q) * a.G;
+  const int64_t most_rows = mode == kShared ? shared_rows(a.Tq, a.B, a.max_q, a.G) : own_rows;
+  const int64_t parts = workspace_bytes_for(head_dim, most_rows);
+  if (a.status == nullptr || parts < 0) return OFFQ_ERR_CUDA;
+  const int64_t need = mode == kShared ? parts + sums_bytes(a.Tq, a.Hq, head_dim) : parts;
+  if (a.workspace == nullptr || workspace_bytes < need) return OFFQ_ERR_INVALID_ARG;
+  a.few_rows = kFewRows;
+  if (mode == kShared) {
+    a.sums = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + parts);
+    a.stats = reinterpret_cast<float2*>(a.sums + 2 * a.Tq * a.Hq * head_dim);
+    // Sequences of up to 8 rows each keep the few-row form of 8 rows: its 16 warps read faster than the 8 of 16 rows.
+    // The queries of a prefix that has 9 to 16 rows take the many-row form then.
+    if (own_rows <= 8) a.few_rows = 8;
+  }
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (const int rc = paged_few(a, mode, dtype, head_dim, s); rc != OFFQ_OK) return rc;
+  if (most_rows > a.few_rows)
+    if (const int rc = paged_chunk(a, mode, dtype, head_dim, s); rc != OFFQ_OK) return rc;
+  return mode == kShared ? join_shared(a, dtype, head_dim, s) : OFFQ_OK;
+}
+
+AttnArgs paged_args(const void* q, int64_t Tq, int32_t Hq, int32_t H, int64_t ld_q, const uint8_t* k_codes,
+                    const float* k_params, const uint8_t* v_codes, const float* v_params, int64_t pages,
+                    const int32_t* block_table, int64_t ld_table, const int32_t* lens, const int32_t* cu_q, int32_t B,
+                    int32_t max_q, float scale, void* out, int64_t ld_out, float* lse, void* workspace) {
   AttnArgs a = {};
   a.q = q;
   a.ld_q = ld_q;
   a.Tq = Tq;
   a.Hq = Hq;
   a.H = H;
-  a.G = Hq / H;
   a.k_codes = k_codes;
   a.v_codes = v_codes;
   a.k_params = k_params;
   a.v_params = v_params;
   a.pages = pages;
-  a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
   a.table = block_table;
   a.ld_table = ld_table;
   a.lens = lens;
@@ -88,49 +141,113 @@ extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_
   a.out = out;
   a.ld_out = ld_out;
   a.lse = lse;
-  a.status = device_status_ptr();
-  const int64_t most_rows = static_cast<int64_t>(max_q) * a.G;
-  const int64_t need = workspace_bytes_for(head_dim, most_rows);
-  if (a.status == nullptr || need < 0) return OFFQ_ERR_CUDA;
-  if (workspace == nullptr || workspace_bytes < need) return OFFQ_ERR_INVALID_ARG;
   a.workspace = workspace;
-  a.few_rows = kFewRows;
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (const int rc = paged_few(a, dtype, head_dim, s); rc != OFFQ_OK) return rc;
-  return most_rows > kFewRows ? paged_chunk(a, dtype, head_dim, s) : OFFQ_OK;
+  return a;
 }
 
-extern "C" int offq_prompt_attention(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq,
-                                     int32_t H, int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v,
-                                     const int32_t* cu, int32_t B, float scale, int32_t causal, void* out,
-                                     int64_t ld_out, float* lse, void* stream) {
-  if (const int rc = check_attention(dtype, T, Hq, H, head_dim, ld_q, B, scale, ld_out); rc != OFFQ_OK) return rc;
-  const int64_t width = static_cast<int64_t>(H) * head_dim;
-  if (ld_k < width || ld_v < width) return OFFQ_ERR_INVALID_ARG;
-  if (T == 0 || B == 0) return OFFQ_OK;
-  if (q == nullptr || k == nullptr || v == nullptr || cu == nullptr || out == nullptr) return OFFQ_ERR_INVALID_ARG;
-  if (!row_ok(q, ld_q) || !row_ok(k, ld_k) || !row_ok(v, ld_v) || !row_ok(out, ld_out) || !aligned(cu, 4) ||
-      !aligned(lse, 4))
+int prompt_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, void* stream) {
+  if (const int rc = check_attention(dtype, a.Tq, a.Hq, a.H, head_dim, a.ld_q, a.B, a.scale, a.ld_out); rc != OFFQ_OK)
+    return rc;
+  const int64_t width = static_cast<int64_t>(a.H) * head_dim;
+  if (a.ld_k < width || a.ld_v < width) return OFFQ_ERR_INVALID_ARG;
+  if (mode == kWindowed && (a.window < 1 || a.sinks < 0)) return OFFQ_ERR_INVALID_ARG;
+  if (a.Tq == 0 || a.B == 0) return OFFQ_OK;
+  if (a.q == nullptr || a.k == nullptr || a.v == nullptr || a.cu == nullptr || a.out == nullptr) return OFFQ_ERR_INVALID_ARG;
+  if (!row_ok(a.q, a.ld_q) || !row_ok(a.k, a.ld_k) || !row_ok(a.v, a.ld_v) || !row_ok(a.out, a.ld_out) ||
+      !aligned(a.cu, 4) || !aligned(a.lse, 4))
     return OFFQ_ERR_MISALIGNED;
+  a.G = a.Hq / a.H;
+  a.window = std::min(a.window, kMostTokens);
+  a.sinks = std::min(a.sinks, kMostTokens);
+  a.status = device_status_ptr();
+  if (a.status == nullptr) return OFFQ_ERR_CUDA;
+  return prompt_tc(a, mode, dtype, head_dim, static_cast<cudaStream_t>(stream));
+}
+
+AttnArgs prompt_args(const void* q, const void* k, const void* v, int64_t T, int32_t Hq, int32_t H, int64_t ld_q,
+                     int64_t ld_k, int64_t ld_v, const int32_t* cu, int32_t B, float scale, void* out, int64_t ld_out,
+                     float* lse) {
   AttnArgs a = {};
   a.q = q;
   a.ld_q = ld_q;
   a.Tq = T;
   a.Hq = Hq;
   a.H = H;
-  a.G = Hq / H;
   a.k = k;
   a.v = v;
   a.ld_k = ld_k;
   a.ld_v = ld_v;
   a.cu = cu;
   a.B = B;
-  a.causal = causal != 0;
   a.scale = scale;
   a.out = out;
   a.ld_out = ld_out;
   a.lse = lse;
-  a.status = device_status_ptr();
-  if (a.status == nullptr) return OFFQ_ERR_CUDA;
-  return prompt_tc(a, dtype, head_dim, static_cast<cudaStream_t>(stream));
+  return a;
+}
+
+}  // namespace
+
+extern "C" int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
+                                    int64_t ld_q, const uint8_t* k_codes, const float* k_params,
+                                    const uint8_t* v_codes, const float* v_params, int64_t pages, int32_t page_size,
+                                    const int32_t* block_table, int64_t ld_table, const int32_t* lens,
+                                    const int32_t* cu_q, int32_t B, int32_t max_q, float scale, void* out,
+                                    int64_t ld_out, float* lse, void* workspace, int64_t workspace_bytes,
+                                    void* stream) {
+  AttnArgs a = paged_args(q, Tq, Hq, H, ld_q, k_codes, k_params, v_codes, v_params, pages, block_table, ld_table, lens, cu_q,
+                          B, max_q, scale, out, ld_out, lse, workspace);
+  return paged_call(a, kCausal, dtype, head_dim, page_size, workspace_bytes, stream);
+}
+
+extern "C" int offq_paged_attention_window(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
+                                           int64_t ld_q, const uint8_t* k_codes, const float* k_params,
+                                           const uint8_t* v_codes, const float* v_params, int64_t pages,
+                                           int32_t page_size, const int32_t* block_table, int64_t ld_table,
+                                           const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q,
+                                           float scale, int32_t window, int32_t sinks, void* out, int64_t ld_out,
+                                           float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  AttnArgs a = paged_args(q, Tq, Hq, H, ld_q, k_codes, k_params, v_codes, v_params, pages, block_table, ld_table, lens, cu_q,
+                          B, max_q, scale, out, ld_out, lse, workspace);
+  a.window = window;
+  a.sinks = sinks;
+  return paged_call(a, kWindowed, dtype, head_dim, page_size, workspace_bytes, stream);
+}
+
+extern "C" int offq_paged_attention_prefix(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
+                                           int64_t ld_q, const uint8_t* k_codes, const float* k_params,
+                                           const uint8_t* v_codes, const float* v_params, int64_t pages,
+                                           int32_t page_size, const int32_t* block_table, int64_t ld_table,
+                                           const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q,
+                                           const int32_t* prefix_table, int64_t ld_prefix, const int32_t* prefix_lens,
+                                           const int32_t* cu_prefix, int32_t P, float scale, void* out, int64_t ld_out,
+                                           float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  AttnArgs a = paged_args(q, Tq, Hq, H, ld_q, k_codes, k_params, v_codes, v_params, pages, block_table, ld_table, lens, cu_q,
+                          B, max_q, scale, out, ld_out, lse, workspace);
+  a.prefix_table = prefix_table;
+  a.ld_prefix = ld_prefix;
+  a.prefix_lens = prefix_lens;
+  a.cu_prefix = cu_prefix;
+  a.P = P;
+  return paged_call(a, kShared, dtype, head_dim, page_size, workspace_bytes, stream);
+}
+
+extern "C" int offq_prompt_attention(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq,
+                                     int32_t H, int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                                     const int32_t* cu, int32_t B, float scale, int32_t causal, void* out,
+                                     int64_t ld_out, float* lse, void* stream) {
+  AttnArgs a = prompt_args(q, k, v, T, Hq, H, ld_q, ld_k, ld_v, cu, B, scale, out, ld_out, lse);
+  a.causal = causal != 0;
+  return prompt_call(a, kCausal, dtype, head_dim, stream);
+}
+
+extern "C" int offq_prompt_attention_window(const void* q, const void* k, const void* v, int dtype, int64_t T, int32_t Hq,
+                                            int32_t H, int32_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                                            const int32_t* cu, int32_t B, float scale, int32_t window, int32_t sinks,
+                                            void* out, int64_t ld_out, float* lse, void* stream) {
+  AttnArgs a = prompt_args(q, k, v, T, Hq, H, ld_q, ld_k, ld_v, cu, B, scale, out, ld_out, lse);
+  a.causal = 1;
+  a.window = window;
+  a.sinks = sinks;
+  return prompt_call(a, kWindowed, dtype, head_dim, stream);
 }

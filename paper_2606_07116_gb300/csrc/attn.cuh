@@ -42,6 +42,14 @@ struct AttnArgs {
   int max_q;
   int few_rows;   // sequences with at most this many rows n * G take the few-row form
   int causal;     // prompts
+  int window, sinks;  // kWindowed: at most kMostTokens each
+  const int32_t* prefix_table;  // kShared
+  int64_t ld_prefix;
+  const int32_t* prefix_lens;
+  const int32_t* cu_prefix;
+  int P;
+  float* sums;    // kShared: of the prefixes, then of the sequences' own tokens: [2][Tq][Hq][head_dim]
+  float2* stats;  // and [2][Tq][Hq] (reference, sum of weights)
   float scale;
   void* out;
   int64_t ld_out;
@@ -52,28 +60,100 @@ struct AttnArgs {
 
 // Most tokens of a sequence: the number of a token past its end by up to two blocks of 128 is an int.
 constexpr int kMostTokens = 0x7FFFFF00;
+// Most tokens of a shared prefix: the positions of all queries behind it are ints.
+constexpr int kMostPrefix = 0x7E000000;
 
-// A sequence of the paged call: its first query row, queries and cached tokens. One whose entries are out of
-// range (negative or too long counts) has no queries; `bad` says so.
+// What a query at position p of its sequence sees (of the tokens that the sequence has):
+enum AttnMode {
+  kCausal,    // 0 .. p
+  kWindowed,  // those of 0 .. p among the first `sinks` or the last `window`
+  // The list of sequences is that of the prefixes, each with all queries of its sequences (who see all of it), then the
+  // sequences with their own tokens, as in kCausal. Sums and statistics of both go to the workspace.
+  kShared
+};
+
+// A sequence of the paged call: its first query row, queries, cached tokens and its first query's position (a prefix's
+// queries stand behind it). One whose entries are out of range (negative or too long counts) has no queries; `bad`
+// says so.
 struct PagedSeq {
-  int first, n, len;
+  int first, n, len, at;
   bool bad;
 };
 
+// Sequences in the list of a call.
+template <AttnMode M>
+__device__ __forceinline__ int listed(const AttnArgs& a) {
+  return M == kShared ? a.P + a.B : a.B;
+}
+
+// The page numbers of a sequence.
+template <AttnMode M>
+__device__ __forceinline__ const int32_t* pages_of(const AttnArgs& a, int b) {
+  if constexpr (M == kShared) {
+    if (b < a.P) return a.prefix_table + static_cast<int64_t>(b) * a.ld_prefix;
+    b -= a.P;
+  }
+  return a.table + static_cast<int64_t>(b) * a.ld_table;
+}
+
+template <AttnMode M>
 __device__ __forceinline__ PagedSeq paged_seq(const AttnArgs& a, int b) {
-  const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1), l = __ldg(a.lens + b);
-  const int64_t most = min(a.ld_table << a.page_shift, static_cast<int64_t>(kMostTokens));
   PagedSeq s;
+  int c0 = 0, c1 = 0, l = 0;
+  int64_t ld = a.ld_table, most_q = a.max_q;
+  bool bad = false, prefix = false;
+  if constexpr (M == kShared) {
+    prefix = b < a.P;
+    if (prefix) {
+      const int s0 = __ldg(a.cu_prefix + b), s1 = __ldg(a.cu_prefix + b + 1);
+      bad = s0 < 0 || s1 < s0 || s1 > a.B;
+      c0 = bad ? 0 : __ldg(a.cu + s0);
+      c1 = bad ? 0 : __ldg(a.cu + s1);
+      l = __ldg(a.prefix_lens + b);
+      ld = a.ld_prefix;
+      most_q = min(a.Tq, static_cast<int64_t>(a.B) * a.max_q);
+    } else {
+      b -= a.P;
+    }
+  }
+  if (!prefix) {
+    c0 = __ldg(a.cu + b);
+    c1 = __ldg(a.cu + b + 1);
+    l = __ldg(a.lens + b);
+  }
+  const int64_t most = min(ld << a.page_shift, static_cast<int64_t>(prefix ? kMostPrefix : kMostTokens));
   s.first = c0;
   s.n = c1 - c0;
   s.len = static_cast<int>(min(static_cast<int64_t>(max(l, 0)), most));
-  s.bad = l < 0 || l > most;
-  if (c0 < 0 || c1 < c0 || c1 > a.Tq || s.n > a.max_q) {
+  s.bad = bad || l < 0 || l > most;
+  if (c0 < 0 || c1 < c0 || c1 > a.Tq || s.n > most_q) {
     s.bad = true;
     s.n = 0;
   }
+  s.at = prefix ? s.len : s.len - s.n;
   return s;
 }
+
+// Position of a sequence's first query.
+template <AttnMode M>
+__device__ __forceinline__ int position(const PagedSeq& s) {
+  return M == kShared ? s.at : s.len - s.n;
+}
+
+// What no query of a run sees between the sinks and the window of its first query, which stands at position `at`: the tokens
+// `cut` .. `cut + shift - 1`, both multiples of `step` (a power of two). A kernel leaves them out: it numbers
+// the others 0, 1, ... in order, positions and lengths less `shift`, and only where it loads has to know.
+struct Gap {
+  int cut, shift;
+};
+__device__ __forceinline__ Gap window_gap(const AttnArgs& a, int at, int step) {
+  Gap g;
+  g.cut = (a.sinks + step - 1) & -step;
+  g.shift = at >= a.window ? max(0, ((at + 1 - a.window) & -step) - g.cut) : 0;
+  return g;
+}
+// The first token that the window of a query leaves in, given the tokens up to itself (both in a run's numbers).
+__device__ __forceinline__ int window_from(const AttnArgs& a, int upto) { return upto > a.window ? upto - a.window : 0; }
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -111,16 +191,30 @@ __device__ __forceinline__ void write_lse(const AttnArgs& a, int first, int h, i
       l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
+// kShared: sums over a prefix (b < P) or over a sequence's own tokens, channel 0 of row r of (first query row, key head h),
+// and the row's statistics.
+template <int D>
+__device__ __forceinline__ float* shared_sums(const AttnArgs& a, int b, int first, int h, int r) {
+  const int64_t t = (b < a.P ? 0 : a.Tq) + first + r / a.G;
+  return a.sums + (t * a.Hq + h * a.G + r % a.G) * D;
+}
+__device__ __forceinline__ void write_stats(const AttnArgs& a, int b, int first, int h, int r, float m, float l) {
+  const int64_t t = (b < a.P ? 0 : a.Tq) + first + r / a.G;
+  a.stats[t * a.Hq + h * a.G + r % a.G] = make_float2(m, l);
+}
+
 // The few-row form of offq_paged_attention (csrc/attn_few.cu): rows n * G of a sequence that it takes, its
 // workspace, and its launch with arguments already checked.
 constexpr int kFewRows = 16;
 int64_t paged_few_workspace(int head_dim);
-int paged_few(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
+int paged_few(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s);
 
 // The many-row form (csrc/attn_chunk.cu): sequences with more rows.
 int64_t paged_chunk_workspace(int head_dim);
-int paged_chunk(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
+int paged_chunk(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s);
+// The outputs of a shared-prefix call from its two sums a row (csrc/attn_prefix.cu).
+int join_shared(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
 // Prompts on the tensor cores (csrc/attn_prompt.cu), arguments already checked.
-int prompt_tc(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s);
+int prompt_tc(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s);
 
 }  // namespace offq

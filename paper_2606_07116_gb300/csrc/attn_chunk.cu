@@ -79,10 +79,18 @@ __device__ __forceinline__ float* part_data(void* ws, int ctas, int cta, int whi
   return reinterpret_cast<float*>(static_cast<PartHead*>(ws) + 2 * ctas) + (2 * cta + which) * ChunkLayout<D>::kPartFloats;
 }
 
-// Blocks that row pair tile p of a sequence has to see (one at least, so that rows that see nothing are written).
+constexpr int kGroup = 8;  // keys whose page a lane of the widening warps looks up
+
+// Tokens that row pair tile p leaves out under a window: it numbers those that its rows see, the gap in whole groups.
+template <AttnMode M>
+__device__ __forceinline__ int tile_shift(const AttnArgs& a, const PagedSeq& s, int p) {
+  return M == kWindowed ? window_gap(a, position<M>(s) + kPairRows * p / a.G, kGroup).shift : 0;
+}
+// Blocks that it has to see (one at least, so that rows that see nothing are written).
+template <AttnMode M>
 __device__ __forceinline__ int tile_blocks(const AttnArgs& a, const PagedSeq& s, int p) {
   const int last = min(s.n - 1, (kPairRows * p + kPairRows - 1) / a.G);
-  const int sees = min(s.len, max(0, s.len - s.n + last + 1));
+  const int sees = min(s.len, max(0, position<M>(s) + last + 1)) - tile_shift<M>(a, s, p);
   return max(1, (sees + kKt - 1) / kKt);
 }
 __device__ __forceinline__ int tiles_of(const AttnArgs& a, const PagedSeq& s) {
@@ -90,6 +98,7 @@ __device__ __forceinline__ int tiles_of(const AttnArgs& a, const PagedSeq& s) {
 }
 
 // A place in the list of steps: sequence, head, row pair tile, block.
+template <AttnMode M>
 struct Walk {
   int b, h, p, blk, tiles, blocks;
   PagedSeq s;
@@ -98,9 +107,9 @@ struct Walk {
     h = c->h;
     p = c->p;
     blk = c->blk;
-    s = paged_seq(a, b);
+    s = paged_seq<M>(a, b);
     tiles = tiles_of(a, s);
-    blocks = tile_blocks(a, s, p);
+    blocks = tile_blocks<M>(a, s, p);
   }
   __device__ __forceinline__ void next_tile(const AttnArgs& a) {
     blk = 0;
@@ -109,12 +118,12 @@ struct Walk {
       if (++h == a.H) {
         h = 0;
         do {
-          s = paged_seq(a, ++b);
+          s = paged_seq<M>(a, ++b);
           tiles = tiles_of(a, s);
         } while (tiles == 0);
       }
     }
-    blocks = tile_blocks(a, s, p);
+    blocks = tile_blocks<M>(a, s, p);
   }
 };
 
@@ -147,7 +156,13 @@ __device__ __forceinline__ void write_pair(T* row, int k, int lane, float x, flo
   const uint32_t v1 = __shfl_sync(kAllLanes, u, (lane & ~3) | ((2 * c + 1) & 3));
   if (row != nullptr) *reinterpret_cast<uint32_t*>(row + 8 * k + 2 * c) = __byte_perm(v0, v1, c < 2 ? 0x5410 : 0x7632);
 }
-template <int D, typename T>
+// kShared: the same lanes' channels 8 k + c and 8 k + c + 4 as sums.
+__device__ __forceinline__ void write_sums(float* row, int k, int lane, float x, float y) {
+  if (row == nullptr) return;
+  row[8 * k + (lane & 3)] = x;
+  row[8 * k + (lane & 3) + 4] = y;
+}
+template <int D, typename T, AttnMode M>
 __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   using L = ChunkLayout<D>;
   constexpr bool kHalf = std::is_same<T, __half>::value;
@@ -182,13 +197,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   PartHead* heads = part_heads(a.workspace, blockIdx.x);
   if (warp == 9) {
     auto steps = [&](int b, PagedSeq& s) {  // of one head of sequence b
-      s = paged_seq(a, b);
+      s = paged_seq<M>(a, b);
       long long n = 0;
-      for (int p = 0, tiles = tiles_of(a, s); p < tiles; ++p) n += tile_blocks(a, s, p);
+      for (int p = 0, tiles = tiles_of(a, s); p < tiles; ++p) n += tile_blocks<M>(a, s, p);
       return n;
     };
     long long total = 0;
-    for (int b = lane; b < a.B; b += 32) {
+    const int B = listed<M>(a);
+    for (int b = lane; b < B; b += 32) {
       PagedSeq s;
       total += steps(b, s) * a.H;
       if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
@@ -199,9 +215,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     const long long lo = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
     const long long hi = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
     long long before = 0;
-    for (int first = 0; first < a.B && before <= lo && lo < hi; first += 32) {
+    for (int first = 0; first < B && before <= lo && lo < hi; first += 32) {
       PagedSeq s;
-      const long long one = first + lane < a.B ? steps(first + lane, s) : 0, val = one * a.H;
+      const long long one = first + lane < B ? steps(first + lane, s) : 0, val = one * a.H;
       long long incl = val;
 #pragma unroll
       for (int m = 1; m < 32; m <<= 1) {
@@ -212,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       if (lo >= start && lo < start + val) {
         long long at = (lo - start) % one;
         int p = 0;
-        for (int n = tile_blocks(a, s, 0); at >= n; n = tile_blocks(a, s, ++p)) at -= n;
+        for (int n = tile_blocks<M>(a, s, 0); at >= n; n = tile_blocks<M>(a, s, ++p)) at -= n;
         ctrl->b = first + lane;
         ctrl->h = static_cast<int>((lo - start) / one);
         ctrl->p = p;
@@ -252,19 +268,26 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       float2 kp, vp;
       uint32_t absent;  // reps whose rows have no page
     };
-    struct Pages {  // a block's: head, first token, the sequence's length, the page of this lane's row in each rep
+    // A block's: head, first token, the tokens of the list (less those left out), the page of this lane's row in each rep;
+    // under a window the tokens left out and the first that a window of the tile leaves in.
+    struct Pages {
       int head, first, len, page[kReps];
+      int shift, from;
     };
+    const int cut = M == kWindowed ? window_gap(a, 0, kGroup).cut : 0;
+    auto token_of = [&](const Pages& x, int tok) { return M == kWindowed && tok >= cut ? tok + x.shift : tok; };
     Pages now, after;  // of the block to load and the one after it
-    Walk at;           // the block whose pages were found last
+    Walk<M> at;        // the block whose pages were found last
     auto find_pages = [&](Pages& x) {  // of block `at`
       x.head = at.h;
       x.first = at.blk * kKt;
-      x.len = at.s.len;
+      x.shift = tile_shift<M>(a, at.s, at.p);
+      x.len = at.s.len - x.shift;
+      x.from = M == kWindowed ? window_from(a, position<M>(at.s) + kPairRows * at.p / a.G + 1 - x.shift) : 0;
 #pragma unroll
       for (int i = 0; i < kReps; ++i) {
         const int tok = x.first + kRowsPer * i + (row & ~7);
-        x.page[i] = tok < x.len ? __ldg(a.table + static_cast<int64_t>(at.b) * a.ld_table + (tok >> a.page_shift)) : -1;
+        x.page[i] = tok < x.len ? __ldg(pages_of<M>(a, at.b) + (token_of(x, tok) >> a.page_shift)) : -1;
       }
     };
     auto step = [&](Pages& x) {
@@ -272,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       find_pages(x);
     };
     auto slot_of = [&](const Pages& x, int i) {
-      const int tok = x.first + kRowsPer * i + row;
+      const int tok = token_of(x, x.first + kRowsPer * i + row);
       return ((static_cast<int64_t>(x.page[i]) * a.H + x.head) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
     };
     auto load = [&](Held& x) {
@@ -292,7 +315,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
         const int64_t r = slot_of(now, i);
         x.kc[i] = __ldg(reinterpret_cast<const uint4*>(a.k_codes + r * (D / 2)) + c);
         x.vc[i] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + r * (D / 2)) + c);
-        if (i == c && tok < now.len) {
+        const bool seen = tok < now.len && (M != kWindowed || tok < a.sinks || tok >= now.from);  // by some row of the tile
+        if (i == c && seen) {
           x.kp = __ldg(reinterpret_cast<const float2*>(a.k_params) + r);
           x.vp = __ldg(reinterpret_cast<const float2*>(a.v_params) + r);
         }
@@ -367,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     if (warp == 8 && count > 0) {
       // ---- Products. The whole warp runs the loop; an elected lane issues ----
       constexpr uint32_t kIdescS = idesc_16<T>(128, kKt, false), kIdescO = idesc_16<__half>(128, D, true);
-      Walk w;
+      Walk<M> w;
       w.start(a, ctrl);
       int gb = 0, left = count, nq[2] = {0, 0}, np[2] = {0, 0};
       bool ok = true;
@@ -435,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
       const uint32_t s_tm = tmem + i * 128 + lanes, o_tm = tmem + 256 + i * D + lanes;
       float* sums = reinterpret_cast<float*>(smem + L::kSums) + i * kQt + quad * 32;
-      Walk w;
+      Walk<M> w;
       w.start(a, ctrl);
       int gb = 0, left = count, ns = 0;
       bool ok = true;
@@ -493,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&ctrl->q_full[i]));
-          least = min(w.s.len, max(0, w.s.len - w.s.n + row0 / a.G + 1));
+          least = min(w.s.len, max(0, position<M>(w.s) + row0 / a.G + 1)) - tile_shift<M>(a, w.s, w.p);
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             qs[x] = sums[8 * x + g];   // x = 2 hh + ii
@@ -517,11 +541,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             const float big = fmaxf(fmaxf(sm.x, sm.y), fmaxf(sm.z, sm.w));
             const float lift = static_cast<float>(min(128, max(static_cast<int>(kLeastLog2), static_cast<int>(__float_as_uint(big) >> 23 & 255u) - 126)));
             const float most = ex2(kMostLog2 - lift);
-            const bool masked = key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u;
-            int sees[4] = {0, 0, 0, 0};
+            bool masked = key0 + kKt > least || (gone.x | gone.y | gone.z | gone.w) != 0u;
+            const int past = key0 + 2 * c;  // this lane's first key
+            int at = position<M>(w.s), len = w.s.len;
+            if constexpr (M == kWindowed) {
+              const int shift = tile_shift<M>(a, w.s, w.p);
+              at -= shift;
+              len -= shift;
+              masked |= key0 < window_from(a, at + (row0 + 31) / a.G + 1) && key0 + kKt > a.sinks;
+            }
+            int sees[4] = {0, 0, 0, 0}, from[4] = {0, 0, 0, 0};  // a row's keys end and its window begins
             if (masked) {
 #pragma unroll
-              for (int x = 0; x < 4; ++x) sees[x] = min(w.s.len, w.s.len - w.s.n + (row0 + 8 * x + g) / a.G + 1) - key0 - 2 * c;
+              for (int x = 0; x < 4; ++x) {
+                const int upto = at + (row0 + 8 * x + g) / a.G + 1;
+                sees[x] = min(len, upto) - past;
+                if constexpr (M == kWindowed) from[x] = window_from(a, upto) - past;
+              }
             }
             // 32 keys at a time: scores relative to m, weights, sums; the weights take the place of scores already read.
 #pragma unroll 1
@@ -538,7 +574,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                   for (int x = 0; x < 4; ++x)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                      if (out || 32 * q + 8 * k + e >= sees[x]) s[x >> 1][4 * k + 2 * (x & 1) + e] = 0x7FFFFFFFu;  // NaN: hidden
+                    {
+                      const int key = 32 * q + 8 * k + e;
+                      bool hidden = out || key >= sees[x];
+                      if constexpr (M == kWindowed) hidden |= key < from[x] && key >= a.sinks - past;
+                      if (hidden) s[x >> 1][4 * k + 2 * (x & 1) + e] = 0x7FFFFFFFu;  // NaN
+                    }
                 }
               }
               const float4 *pkq = pk + q * 16, *pvq = pv + q * 16;
@@ -680,7 +721,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           const int which = w.blk == 0 ? 1 : 0;
           float* part = part_data<D>(a.workspace, gridDim.x, blockIdx.x, which);
           float inv[4];
-          T* to[4];
+          using Out = std::conditional_t<M == kShared, float, T>;
+          Out* to[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
 #pragma unroll
@@ -690,13 +732,19 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             }
             inv[x] = l[x] > 0.f ? __fdividef(1.f, l[x]) : 0.f;
             const int r = 8 * x + g;
-            to[x] = row0 + r < rows ? out_row<D, T>(a, w.s, w.h, row0 + r) : nullptr;
+            if constexpr (M == kShared)
+              to[x] = row0 + r < rows ? shared_sums<D>(a, w.b, w.s.first, w.h, row0 + r) : nullptr;
+            else
+              to[x] = row0 + r < rows ? out_row<D, T>(a, w.s, w.h, row0 + r) : nullptr;
             if (c == 0) {
               if (!complete) {
                 part[i * kQt + quad * 32 + r] = m[x];
                 part[kPairRows + i * kQt + quad * 32 + r] = l[x];
               } else if (row0 + r < rows) {
-                write_lse(a, w.s.first, w.h, row0 + r, m[x], l[x]);
+                if constexpr (M == kShared)
+                  write_stats(a, w.b, w.s.first, w.h, row0 + r, m[x], l[x]);
+                else
+                  write_lse(a, w.s.first, w.h, row0 + r, m[x], l[x]);
               }
             }
           }
@@ -713,8 +761,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                 for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(o[hh][4 * k + e]) + off[2 * hh + (e >> 1)];
                 if (complete) {
 #pragma unroll
-                  for (int ii = 0; ii < 2; ++ii)
-                    write_pair<T>(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii] * inv[2 * hh + ii], v[2 * ii + 1] * inv[2 * hh + ii]);
+                  for (int ii = 0; ii < 2; ++ii) {
+                    if constexpr (M == kShared)
+                      write_sums(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii], v[2 * ii + 1]);
+                    else
+                      write_pair<T>(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii] * inv[2 * hh + ii], v[2 * ii + 1] * inv[2 * hh + ii]);
+                  }
                 } else {
                   reinterpret_cast<float4*>(part + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + 4 * q + k) * 32 + lane] =
                       make_float4(v[0], v[1], v[2], v[3]);
@@ -742,7 +794,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
 
 // Row pair tiles that cross CTAs: begun at the end of CTA blockIdx.x, then the first parts of the CTAs after it up to
 // their last. Block y takes one softmax warp's 32 rows; a warp of it a quarter of the channels.
-template <int D, typename T>
+template <int D, typename T, AttnMode M>
 __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int ctas) {
   __shared__ int s_last;
   const int cta = blockIdx.x, tid = threadIdx.x, lane = tid & 31, q = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -759,7 +811,7 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
   __syncthreads();
   const int last = s_last;
   if (last >= ctas) return;  // a CTA gave up: the status word says so
-  const PagedSeq s = paged_seq(a, p.b);
+  const PagedSeq s = paged_seq<M>(a, p.b);
   const int rows = s.n * a.G, warp = blockIdx.y, row0 = p.p * kPairRows + warp * 32;
   if (row0 >= rows) return;
   constexpr int kReps = D / 32;  // of 8 channels, per warp
@@ -803,6 +855,14 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
 #pragma unroll
     for (int ii = 0; ii < 2; ++ii) {
       const int x = 2 * hh + ii, r = row0 + 8 * x + g;
+      if constexpr (M == kShared) {
+        float* to = r < rows ? shared_sums<D>(a, p.b, s.first, p.h, r) : nullptr;
+#pragma unroll
+        for (int k = 0; k < kReps; ++k)
+          write_sums(to, q * kReps + k, lane, ii ? acc[hh][k].z : acc[hh][k].x, ii ? acc[hh][k].w : acc[hh][k].y);
+        if (q == 0 && c == 0 && r < rows) write_stats(a, p.b, s.first, p.h, r, top[x], sum[x]);
+        continue;
+      }
       const float inv = sum[x] > 0.f ? __fdividef(1.f, sum[x]) : 0.f;
       T* to = r < rows ? out_row<D, T>(a, s, p.h, r) : nullptr;
 #pragma unroll
@@ -812,13 +872,20 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
     }
 }
 
-template <int D, typename T>
+template <int D, typename T, AttnMode M>
 int launch_chunk(const AttnArgs& a, cudaStream_t s) {
   using L = ChunkLayout<D>;
   const int sms = device_sms();
-  if (sms == 0 || !smem_optin<chunk_kernel<D, T>>(L::kBytes)) return OFFQ_ERR_CUDA;
-  if (const int rc = launch_pdl(chunk_kernel<D, T>, dim3(sms), dim3(kThreads), L::kBytes, s, a); rc != OFFQ_OK) return rc;
-  return launch_pdl(join_chunks_kernel<D, T>, dim3(sms, 8), dim3(128), 0, s, a, sms);
+  if (sms == 0 || !smem_optin<chunk_kernel<D, T, M>>(L::kBytes)) return OFFQ_ERR_CUDA;
+  if (const int rc = launch_pdl(chunk_kernel<D, T, M>, dim3(sms), dim3(kThreads), L::kBytes, s, a); rc != OFFQ_OK) return rc;
+  return launch_pdl(join_chunks_kernel<D, T, M>, dim3(sms, 8), dim3(128), 0, s, a, sms);
+}
+
+template <AttnMode M>
+int launch_chunk_m(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
+  if (head_dim == 128)
+    return dtype == OFFQ_BF16 ? launch_chunk<128, __nv_bfloat16, M>(a, s) : launch_chunk<128, __half, M>(a, s);
+  return dtype == OFFQ_BF16 ? launch_chunk<64, __nv_bfloat16, M>(a, s) : launch_chunk<64, __half, M>(a, s);
 }
 
 }  // namespace
@@ -830,10 +897,12 @@ int64_t paged_chunk_workspace(int head_dim) {
   return sms == 0 ? -1 : 2 * static_cast<int64_t>(sms) * (static_cast<int64_t>(sizeof(PartHead)) + 4 * kPairRows * (head_dim + 2));
 }
 
-int paged_chunk(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
-  if (head_dim == 128)
-    return dtype == OFFQ_BF16 ? launch_chunk<128, __nv_bfloat16>(a, s) : launch_chunk<128, __half>(a, s);
-  return dtype == OFFQ_BF16 ? launch_chunk<64, __nv_bfloat16>(a, s) : launch_chunk<64, __half>(a, s);
+int paged_chunk(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s) {
+  switch (mode) {
+    case kWindowed: return launch_chunk_m<kWindowed>(a, dtype, head_dim, s);
+    case kShared: return launch_chunk_m<kShared>(a, dtype, head_dim, s);
+    default: return launch_chunk_m<kCausal>(a, dtype, head_dim, s);
+  }
 }
 
 }  // namespace offq

@@ -127,6 +127,16 @@ __device__ __forceinline__ int stages_of(const AttnArgs& a, const PagedSeq& s) {
   return max(1, (s.len + kTile - 1) / kTile);
 }
 
+// A sequence in this form's numbers: under a window without the gap that none of its queries sees, whole stages of it.
+template <AttnMode M>
+__device__ __forceinline__ PagedSeq few_seq(const AttnArgs& a, int b) {
+  PagedSeq s = paged_seq<M>(a, b);
+  if constexpr (M == kWindowed) {
+    s.len -= window_gap(a, position<M>(s), kTile).shift;
+  }
+  return s;
+}
+
 // Header of a part that crosses CTAs: its head's (sequence, head) as one number, negative for none, whether it reaches
 // its sequence's last stage, and the sequence's first query row and rows per key head.
 struct PartHead {
@@ -145,9 +155,15 @@ __device__ __forceinline__ float* part_sums(void* ws, int ctas, int cta, int whi
          static_cast<int64_t>(2 * cta + which) * FewLayout<D, NT>::kPartFloats;
 }
 
-// Channels d .. d + 7 of row r of (sequence starting at query row `first`, head h).
-template <int D, typename T>
-__device__ __forceinline__ void write_out8(const AttnArgs& a, int first, int h, int r, int d, const float (&v)[8]) {
+// Channels d .. d + 7 of row r of (sequence b of the list, which starts at query row `first`, head h): outputs, with kShared sums.
+template <int D, typename T, AttnMode M>
+__device__ __forceinline__ void write_row8(const AttnArgs& a, int b, int first, int h, int r, int d, const float (&v)[8]) {
+  if constexpr (M == kShared) {
+    float4* dst = reinterpret_cast<float4*>(shared_sums<D>(a, b, first, h, r) + d);
+    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+    dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+    return;
+  }
   const int64_t t = static_cast<int64_t>(first) + r / a.G;
   uint32_t w[4];
 #pragma unroll
@@ -161,8 +177,15 @@ __device__ __forceinline__ void write_out8(const AttnArgs& a, int first, int h, 
   *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + static_cast<int64_t>(h * a.G + r % a.G) * D + d) =
       make_uint4(w[0], w[1], w[2], w[3]);
 }
+template <AttnMode M>
+__device__ __forceinline__ void write_row_stats(const AttnArgs& a, int b, int first, int h, int r, float m, float l) {
+  if constexpr (M == kShared)
+    write_stats(a, b, first, h, r, m, l);
+  else
+    write_lse(a, first, h, r, m, l);
+}
 
-template <int D, int NT, typename T>
+template <int D, int NT, typename T, AttnMode M>
 __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_kernel(const AttnArgs a) {
   using L = FewLayout<D, NT>;
   constexpr bool kHalf = std::is_same<T, __half>::value;
@@ -180,8 +203,9 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
 
   // The whole work, this CTA's share and its warps' places in it.
   long long mine = 0;
-  for (int b = tid; b < a.B; b += kThreads) {
-    const PagedSeq s = paged_seq(a, b);
+  const int B = listed<M>(a);
+  for (int b = tid; b < B; b += kThreads) {
+    const PagedSeq s = few_seq<M>(a, b);
     if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
     mine += static_cast<long long>(stages_of(a, s)) * a.H;
   }
@@ -206,9 +230,9 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     return;
   }
   long long before = 0;
-  for (int base = 0; base < a.B && before < hi; base += kThreads) {
+  for (int base = 0; base < B && before < hi; base += kThreads) {
     long long val = 0;
-    if (base + tid < a.B) val = static_cast<long long>(stages_of(a, paged_seq(a, base + tid))) * a.H;
+    if (base + tid < B) val = static_cast<long long>(stages_of(a, few_seq<M>(a, base + tid))) * a.H;
     long long incl = val;
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) {
@@ -241,23 +265,26 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   int todo = static_cast<int>(w1 - w0), ahead = todo;  // stages to compute, to issue
   if (todo > 0) {
     int b = ctrl->seq[warp];
-    PagedSeq s = paged_seq(a, b);
+    PagedSeq s = few_seq<M>(a, b);
     int stages = stages_of(a, s);
     int h = static_cast<int>(ctrl->start[warp] / stages), t = static_cast<int>(ctrl->start[warp] % stages);
 
     // Where the copies are: they run ahead across heads and sequences.
-    int pb = b, ph = h, pt = t, pstages = stages, plen = s.len, window = -64, entry = 0;
+    int pb = b, ph = h, pt = t, pstages = stages, plen = s.len, listed_from = -64, entry = 0;
+    const int cut = M == kWindowed ? window_gap(a, 0, kTile).cut : 0;
+    // Under a window: tokens left out at `cut`, and the first that a window leaves in.
+    int pshift = M == kWindowed ? window_gap(a, position<M>(paged_seq<M>(a, b)), kTile).shift : 0;
+    int pfrom = M == kWindowed ? window_from(a, position<M>(s) + 1) : 0;
     int64_t page_row = -1;   // first row of the page the copies are in
     bool turn = true;        // that page is not known yet
     uint32_t missing = 0;    // bit 2 slot + half: that half of the slot's stage has no page
     auto find_page = [&](int tok) {  // first row of the page of token tok, or -1
       const int index = tok >> a.page_shift;
-      if (index < window || index >= window + 32) {
-        window = index;
-        entry = static_cast<int64_t>(index + lane) << a.page_shift < plen
-                    ? __ldg(a.table + static_cast<int64_t>(pb) * a.ld_table + index + lane) : 0;
+      if (index < listed_from || index >= listed_from + 32) {
+        listed_from = index;
+        entry = static_cast<int64_t>(index + lane) << a.page_shift < plen + pshift ? __ldg(pages_of<M>(a, pb) + index + lane) : 0;
       }
-      const int page = __shfl_sync(kAllLanes, entry, index - window);
+      const int page = __shfl_sync(kAllLanes, entry, index - listed_from);
       if (page >= 0 && page < a.pages) return (static_cast<int64_t>(page) * a.H + ph) << a.page_shift;
       if (lane == 0) *a.status = OFFQ_ERR_INVALID_ARG;
       return static_cast<int64_t>(-1);
@@ -272,16 +299,25 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     };
     auto issue = [&](int slot) {
       const uint32_t stage = ring + slot * L::kStageBytes;
-      const int tok = pt * kTile, in_page = tok & ((1 << a.page_shift) - 1);
+      const int at = pt * kTile, tok = M == kWindowed && at >= cut ? at + pshift : at;
+      const int in_page = tok & ((1 << a.page_shift) - 1);
+      // Halves of which some token may be seen: the others have no page under a window.
+      bool need0 = at < plen, need1 = at + 16 < plen;
+      if constexpr (M == kWindowed) {
+        need0 = need0 && (at < a.sinks || at + 16 > pfrom);
+        need1 = need1 && (at + 16 < a.sinks || at + 32 > pfrom);
+      }
       int64_t r0, r1;  // first rows of the stage's halves, or -1
       if (a.page_shift >= 5) {
-        if (turn || in_page == 0) page_row = tok < plen ? find_page(tok) : -1;
+        if (turn || in_page == 0 || (M == kWindowed && at == cut)) page_row = at < plen ? find_page(tok) : -1;
         turn = false;
         r0 = page_row < 0 ? -1 : page_row + in_page;
         r1 = page_row < 0 ? -1 : r0 + 16;
+        if (M == kWindowed && !need0) r0 = -1;
+        if (M == kWindowed && !need1) r1 = -1;
       } else {  // two pages of 16 tokens
-        r0 = tok < plen ? find_page(tok) : -1;
-        r1 = tok + 16 < plen ? find_page(tok + 16) : -1;
+        r0 = need0 ? find_page(tok) : -1;
+        r1 = need1 ? find_page(tok + 16) : -1;
       }
       missing &= ~(3u << (2 * slot));
       missing |= ((r0 < 0 ? 1u : 0u) | (r1 < 0 ? 2u : 0u)) << (2 * slot);
@@ -295,13 +331,17 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         turn = true;
         if (++ph == a.H) {
           ph = 0;
-          window = -64;
+          listed_from = -64;
           PagedSeq n;
           do {
-            n = paged_seq(a, ++pb);
+            n = few_seq<M>(a, ++pb);
             pstages = stages_of(a, n);
           } while (pstages == 0);
           plen = n.len;
+          if constexpr (M == kWindowed) {
+            pfrom = window_from(a, position<M>(n) + 1);
+            pshift = window_gap(a, position<M>(paged_seq<M>(a, pb)), kTile).shift;
+          }
         }
       }
     };
@@ -325,7 +365,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         begin = false;
         t_first = t;
         rows = s.n * a.G;
-        sees_least = max(0, s.len - s.n + 1);
+        sees_least = M == kShared ? min(s.len, max(0, s.at + 1)) : max(0, s.len - s.n + 1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const int r = 8 * nt + g;
@@ -357,7 +397,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             qs[nt][j] = __shfl_sync(kAllLanes, sum, 4 * (2 * c + j));
             l[nt][j] = w[nt][j] = 0.f;
             const int rr = 8 * nt + 2 * c + j;
-            sees[nt][j] = rr < rows ? max(0, min(s.len, s.len - s.n + rr / a.G + 1)) : 0;
+            sees[nt][j] = rr < rows ? max(0, min(s.len, position<M>(s) + rr / a.G + 1)) : 0;
             m[nt][j] = sees[nt][j] > 0 ? -INFINITY : 0.f;  // a row without keys has no maximum to wait for
           }
 #pragma unroll
@@ -399,6 +439,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         }
       }
       bool redo = (t + 1) * kTile > sees_least || gone != 0;
+      if constexpr (M == kWindowed) redo |= t * kTile < window_from(a, s.len) && (t + 1) * kTile > a.sinks;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float top = -INFINITY, most = 0.f;
@@ -421,7 +462,9 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {  // what nobody sees may hold anything
-            none[half][i] = t * kTile + half * 16 + tok_k + 8 * i >= s.len || (gone >> half & 1u);
+            const int tok = t * kTile + half * 16 + tok_k + 8 * i;
+            none[half][i] = tok >= s.len || (gone >> half & 1u);
+            if constexpr (M == kWindowed) none[half][i] |= tok >= a.sinks && tok < window_from(a, position<M>(s) + 1);
             if (none[half][i]) sv[half][i] = ov[half][i] = 0.f;
             lift[half][i] = fmaxf(__log2f(sv[half][i]), kLeastLog2);
           }
@@ -437,7 +480,9 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
               for (int i = 0; i < 2; ++i) {
                 const int k = 2 * i + j;
                 float z = fmaf(sk[half][i], acc[half][nt][k], bk[half][i] * qs[nt][j]);
-                if (none[half][i] || t * kTile + half * 16 + tok_k + 8 * i >= sees[nt][j]) z = -INFINITY;
+                const int tok = t * kTile + half * 16 + tok_k + 8 * i;
+                if (none[half][i] || tok >= sees[nt][j]) z = -INFINITY;
+                if (M == kWindowed && tok >= a.sinks && tok < window_from(a, sees[nt][j])) z = -INFINITY;
                 acc[half][nt][k] = z;
                 top = fmaxf(top, z + lift[half][i]);
               }
@@ -525,15 +570,15 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
           const int r = 8 * nt + 2 * c + j;
           if (complete) {
             if (r < rows) {
-              const float inv = l[nt][j] > 0.f ? __fdividef(1.f, l[nt][j]) : 0.f;
+              const float inv = M == kShared ? 1.f : l[nt][j] > 0.f ? __fdividef(1.f, l[nt][j]) : 0.f;
 #pragma unroll
               for (int q8 = 0; q8 < kMt / 4; ++q8) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = (o[nt][4 * q8 + e / 2][j + 2 * (e & 1)] + w[nt][j]) * inv;
-                write_out8<D, T>(a, s.first, h, r, g * (D / 8) + 8 * q8, v);
+                write_row8<D, T, M>(a, b, s.first, h, r, g * (D / 8) + 8 * q8, v);
               }
-              if (g == 0) write_lse(a, s.first, h, r, m[nt][j], l[nt][j]);
+              if (g == 0) write_row_stats<M>(a, b, s.first, h, r, m[nt][j], l[nt][j]);
             }
           } else {
 #pragma unroll
@@ -553,7 +598,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         if (++h == a.H) {
           h = 0;
           do {
-            s = paged_seq(a, ++b);
+            s = few_seq<M>(a, ++b);
             stages = stages_of(a, s);
           } while (stages == 0);
         }
@@ -579,7 +624,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     const bool complete = begins == 0 && last < 0;
     const int which = begins == 0 ? 1 : 0, h = id - b * a.H;
     float* dst = part_sums<D, NT>(a.workspace, gridDim.x, blockIdx.x, which);
-    const PagedSeq s = paged_seq(a, b);
+    const PagedSeq s = paged_seq<M>(a, b);
     if (!complete) (which ? have1 : have0) = true;
     if (!complete && tid == 0) heads[which] = PartHead{id, last < 0, s.first, s.n * a.G};
     for (int u = tid; u < L::kRows * (D / 8); u += kThreads) {
@@ -598,11 +643,11 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
       }
       if (complete) {
         if (r < s.n * a.G) {
-          const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+          const float inv = M == kShared ? 1.f : sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= inv;
-          write_out8<D, T>(a, s.first, h, r, d, v);
-          if (d == 0) write_lse(a, s.first, h, r, top, sum);
+          write_row8<D, T, M>(a, b, s.first, h, r, d, v);
+          if (d == 0) write_row_stats<M>(a, b, s.first, h, r, top, sum);
         }
       } else {
         reinterpret_cast<float4*>(dst + r * D + d)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -622,7 +667,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
 }
 
 // A head that crosses CTAs: begun at the end of CTA c, then the first parts of the CTAs after it up to its last.
-template <int D, int NT, typename T>
+template <int D, int NT, typename T, AttnMode M>
 __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int ctas) {
   using L = FewLayout<D, NT>;
   __shared__ int s_last;
@@ -688,31 +733,36 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int c
       }
       top = next;
     }
-    const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
+    const float inv = M == kShared ? 1.f : sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= inv;
-    write_out8<D, T>(a, p.first, h, r, d, v);
-    if (d == 0) write_lse(a, p.first, h, r, top, sum);
+    write_row8<D, T, M>(a, p.id / a.H, p.first, h, r, d, v);
+    if (d == 0) write_row_stats<M>(a, p.id / a.H, p.first, h, r, top, sum);
   }
 }
 
-template <int D, int NT, typename T>
+template <int D, int NT, typename T, AttnMode M>
 int launch_few(const AttnArgs& a, cudaStream_t s) {
   using L = FewLayout<D, NT>;
   static_assert(sizeof(FewCtrl<D, NT>) <= 2048, "control block");
   const int sms = device_sms();
-  if (sms == 0 || !smem_optin<paged_few_kernel<D, NT, T>>(L::kBytes)) return OFFQ_ERR_CUDA;
-  if (const int rc = launch_pdl(paged_few_kernel<D, NT, T>, dim3(sms), dim3(L::kWarps * 32), L::kBytes, s, a);
+  if (sms == 0 || !smem_optin<paged_few_kernel<D, NT, T, M>>(L::kBytes)) return OFFQ_ERR_CUDA;
+  if (const int rc = launch_pdl(paged_few_kernel<D, NT, T, M>, dim3(sms), dim3(L::kWarps * 32), L::kBytes, s, a);
       rc != OFFQ_OK)
     return rc;
-  return launch_pdl(join_parts_kernel<D, NT, T>, dim3(sms), dim3(256), 0, s, a, sms);
+  return launch_pdl(join_parts_kernel<D, NT, T, M>, dim3(sms), dim3(256), 0, s, a, sms);
 }
 
-template <int D>
+template <AttnMode M, int D>
 int launch_few_d(const AttnArgs& a, int dtype, cudaStream_t s) {
   const bool two = std::min<int64_t>(static_cast<int64_t>(a.max_q) * a.G, a.few_rows) > 8;
-  if (dtype == OFFQ_BF16) return two ? launch_few<D, 2, __nv_bfloat16>(a, s) : launch_few<D, 1, __nv_bfloat16>(a, s);
-  return two ? launch_few<D, 2, __half>(a, s) : launch_few<D, 1, __half>(a, s);
+  if (dtype == OFFQ_BF16) return two ? launch_few<D, 2, __nv_bfloat16, M>(a, s) : launch_few<D, 1, __nv_bfloat16, M>(a, s);
+  return two ? launch_few<D, 2, __half, M>(a, s) : launch_few<D, 1, __half, M>(a, s);
+}
+
+template <AttnMode M>
+int launch_few_m(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
+  return head_dim == 128 ? launch_few_d<M, 128>(a, dtype, s) : launch_few_d<M, 64>(a, dtype, s);
 }
 
 }  // namespace
@@ -725,8 +775,12 @@ int64_t paged_few_workspace(int head_dim) {
   return sms == 0 ? -1 : 2 * static_cast<int64_t>(sms) * (static_cast<int64_t>(sizeof(PartHead)) + 4 * floats);
 }
 
-int paged_few(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
-  return head_dim == 128 ? launch_few_d<128>(a, dtype, s) : launch_few_d<64>(a, dtype, s);
+int paged_few(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s) {
+  switch (mode) {
+    case kWindowed: return launch_few_m<kWindowed>(a, dtype, head_dim, s);
+    case kShared: return launch_few_m<kShared>(a, dtype, head_dim, s);
+    default: return launch_few_m<kCausal>(a, dtype, head_dim, s);
+  }
 }
 
 }  // namespace offq

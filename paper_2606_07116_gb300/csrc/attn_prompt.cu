@@ -54,6 +54,11 @@ struct Item {  // first row and rows of a sequence (no rows: no more items), fir
   int first, n, token, unit;
 };
 
+// Rows of queries, keys and values in boxes of 64 channels: 128 rows, and 8 for a block of keys that sinks and window share.
+struct PromptMaps {
+  CUtensorMap q, k, v, k8, v8;
+};
+
 struct PromptCtrl {
   uint64_t q_full[2], q_empty[2], tail, done;
   uint64_t full[8], empty[8];
@@ -101,10 +106,9 @@ __device__ __forceinline__ int taken_over(uint32_t answer) {
   return x;
 }
 
-template <int D, typename T>
+template <int D, typename T, AttnMode M>
 __global__ void __launch_bounds__(kThreads, 1)
-prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-              const __grid_constant__ CUtensorMap vmap) {
+prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
   using L = PromptLayout<D>;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
@@ -151,17 +155,22 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
   };
   // Item number k of this CTA, for the warps that work on it; false at the end.
   int head[2], row0[2], blocks[2], most = 0;
+  Gap gap = {0, 0};  // keys that the item leaves out: the others are numbered without them
   Item item = {};
   auto next_item = [&](int k) {
     if (!wait(&ctrl->item_full, k)) return false;
     item = ctrl->item;
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&ctrl->item_empty));
+    if constexpr (M == kWindowed) {
+      gap.cut = window_gap(a, 0, 8).cut;
+      gap.shift = max(0, window_from(a, item.token + 1) - gap.cut);
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       head[i] = two_heads ? 2 * item.unit + i : item.unit;
       row0[i] = item.token + (two_heads ? 0 : i * kQt);
-      const int sees = a.causal ? min(row0[i] + kQt, item.n) : item.n;
+      const int sees = (M == kWindowed || a.causal ? min(row0[i] + kQt, item.n) : item.n) - gap.shift;
       blocks[i] = row0[i] < item.n ? (sees + kKt - 1) / kKt : 0;
     }
     most = max(blocks[0], blocks[1]);
@@ -274,7 +283,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
       uint32_t last_tail = 0;  // ring slots whose last copy went to the tail barrier
       bool ok = true;
       for (int k = 0; ok && next_item(k); ++k) {
-        const int kv_head = head[0] / a.G, left = item.n - (most - 1) * kKt;  // keys of the last block
+        const int kv_head = head[0] / a.G, left = item.n - gap.shift - (most - 1) * kKt;  // keys of the last block
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (blocks[i] == 0 || !ok) continue;
@@ -283,7 +292,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
             const uint32_t bar = smem_u32(&ctrl->q_full[i]);
             mbar_arrive_expect_tx(bar, L::kTileBytes);
             for (int c = 0; c < D / 64; ++c)
-              tma_load_2d(q_s + i * L::kTileBytes + c * kAtom, &qmap, bar, head[i] * D + 64 * c, item.first + row0[i]);
+              tma_load_2d(q_s + i * L::kTileBytes + c * kAtom, &maps.q, bar, head[i] * D + 64 * c, item.first + row0[i]);
           }
           if (ok) ++nq[i];
         }
@@ -295,8 +304,18 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
           const uint32_t dst = ring + slot * L::kTileBytes, bar = smem_u32(tail ? &ctrl->tail : &ctrl->full[slot]);
           if (lane == 0) {
             mbar_arrive_expect_tx(bar, L::kTileBytes);
-            for (int c = 0; c < D / 64; ++c)
-              tma_load_2d(dst + c * kAtom, is_v ? &vmap : &kmap, bar, kv_head * D + 64 * c, item.first + u / 2 * kKt);
+            int key = u / 2 * kKt;
+            const bool both = M == kWindowed && gap.shift > 0 && key < gap.cut && key + kKt > gap.cut;
+            if (M == kWindowed && key >= gap.cut) key += gap.shift;
+            if (!both) {
+              for (int c = 0; c < D / 64; ++c)
+                tma_load_2d(dst + c * kAtom, is_v ? &maps.v : &maps.k, bar, kv_head * D + 64 * c, item.first + key);
+            } else {  // the last sinks and the first of the window, eight rows (1024 bytes of an atom) at a time
+              for (int r = 0; r < kKt; r += 8)
+                for (int c = 0; c < D / 64; ++c)
+                  tma_load_2d(dst + c * kAtom + r * 128, is_v ? &maps.v8 : &maps.k8, bar, kv_head * D + 64 * c,
+                              item.first + key + r + (key + r >= gap.cut ? gap.shift : 0));
+            }
           }
           __syncwarp();
           last_tail = tail ? last_tail | 1u << slot : last_tail & ~(1u << slot);
@@ -415,6 +434,8 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
       const int my_blocks = i ? blocks[1] : blocks[0], my_row0 = i ? row0[1] : row0[0], my_head = i ? head[1] : head[0];
       if (my_blocks == 0) continue;
       const int n = item.n, row = my_row0 + (warp & 3) * 32 + lane;   // in the sequence
+      const int upto = row + 1 - gap.shift, window_at = window_from(a, upto);
+      const int last_at = window_from(a, my_row0 + kQt - gap.shift);  // of the tile's last row
       float m = -INFINITY, sum = 0.f;
       for (int j = 0; j < my_blocks; ++j) {
         ok = wait(&ctrl->s_full[i], ns++);
@@ -422,7 +443,21 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
         tc_fence_after();
         uint32_t s[kKt];
         tmem_ld_128cols(s_tm, s);
-        if ((j + 1) * kKt > (a.causal ? min(my_row0 + 1, n) : n)) {
+        if constexpr (M == kWindowed) {
+          if ((j + 1) * kKt > min(my_row0 + 1, n) - gap.shift) {
+            const int valid = min(upto, n - gap.shift) - j * kKt;
+#pragma unroll
+            for (int e = 0; e < kKt; ++e)
+              if (e >= valid) s[e] = 0xFF800000u;  // -inf
+          }
+          if (j * kKt < last_at && (j + 1) * kKt > a.sinks) {  // behind the sinks, before the window
+            const int begin = max(0, a.sinks - j * kKt);
+            const uint32_t hidden = max(0, window_at - j * kKt - begin);
+#pragma unroll
+            for (int e = 0; e < kKt; ++e)
+              if (static_cast<uint32_t>(e - begin) < hidden) s[e] = 0xFF800000u;
+          }
+        } else if ((j + 1) * kKt > (a.causal ? min(my_row0 + 1, n) : n)) {
           const int valid = (a.causal ? min(row + 1, n) : n) - j * kKt;
 #pragma unroll
           for (int e = 0; e < kKt; ++e)
@@ -515,12 +550,12 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap qmap, const 
   }
 }
 
-int heads_map(CUtensorMap* map, const void* x, int dtype, int64_t rows, int64_t width, int64_t ld) {
+int heads_map(CUtensorMap* map, const void* x, int dtype, int64_t rows, int64_t width, int64_t ld, int box_rows) {
   const auto enc = tensor_map_encoder();
   if (enc == nullptr) return OFFQ_ERR_CUDA;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
-  const cuuint32_t box[2] = {64, 128};
+  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t elem_strides[2] = {1, 1};
   const CUresult r = enc(map, dtype == OFFQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
                          const_cast<void*>(x), dims, strides, box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -529,31 +564,41 @@ int heads_map(CUtensorMap* map, const void* x, int dtype, int64_t rows, int64_t 
   return r == CUDA_SUCCESS ? OFFQ_OK : OFFQ_ERR_CUDA;
 }
 
-template <int D, typename T>
+template <int D, typename T, AttnMode M>
 int launch_prompt(const AttnArgs& a, int dtype, cudaStream_t s) {
   using L = PromptLayout<D>;
-  if (!smem_optin<prompt_kernel<D, T>>(L::kBytes)) return OFFQ_ERR_CUDA;
-  CUtensorMap q, k, v;
-  if (heads_map(&q, a.q, dtype, a.Tq, static_cast<int64_t>(a.Hq) * D, a.ld_q) != OFFQ_OK ||
-      heads_map(&k, a.k, dtype, a.Tq, static_cast<int64_t>(a.H) * D, a.ld_k) != OFFQ_OK ||
-      heads_map(&v, a.v, dtype, a.Tq, static_cast<int64_t>(a.H) * D, a.ld_v) != OFFQ_OK)
+  if (!smem_optin<prompt_kernel<D, T, M>>(L::kBytes)) return OFFQ_ERR_CUDA;
+  PromptMaps maps = {};
+  const int64_t width = static_cast<int64_t>(a.H) * D;
+  if (heads_map(&maps.q, a.q, dtype, a.Tq, static_cast<int64_t>(a.Hq) * D, a.ld_q, kQt) != OFFQ_OK ||
+      heads_map(&maps.k, a.k, dtype, a.Tq, width, a.ld_k, kKt) != OFFQ_OK ||
+      heads_map(&maps.v, a.v, dtype, a.Tq, width, a.ld_v, kKt) != OFFQ_OK)
+    return OFFQ_ERR_CUDA;
+  if (M == kWindowed && (heads_map(&maps.k8, a.k, dtype, a.Tq, width, a.ld_k, 8) != OFFQ_OK ||
+                         heads_map(&maps.v8, a.v, dtype, a.Tq, width, a.ld_v, 8) != OFFQ_OK))
     return OFFQ_ERR_CUDA;
   const bool two_heads = (a.G & 1) == 0;
   const int64_t step = two_heads ? kQt : 2 * kQt;
   const int64_t tiles = a.Tq / step + std::min<int64_t>(a.B, a.Tq);  // at most: a whole one per step, a ragged one per sequence
   const int64_t grid = tiles * (two_heads ? a.Hq / 2 : a.Hq);
   if (grid > 0x7FFFFFFF) return OFFQ_ERR_UNSUPPORTED;
-  return launch_pdl(prompt_kernel<D, T>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), L::kBytes, s, a, q, k, v);
+  return launch_pdl(prompt_kernel<D, T, M>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), L::kBytes, s, a, maps);
+}
+
+template <AttnMode M>
+int launch_prompt_m(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
+  if (head_dim == 128)
+    return dtype == OFFQ_BF16 ? launch_prompt<128, __nv_bfloat16, M>(a, dtype, s) : launch_prompt<128, __half, M>(a, dtype, s);
+  return dtype == OFFQ_BF16 ? launch_prompt<64, __nv_bfloat16, M>(a, dtype, s) : launch_prompt<64, __half, M>(a, dtype, s);
 }
 
 }  // namespace
 
 namespace offq {
 
-int prompt_tc(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
-  if (head_dim == 128)
-    return dtype == OFFQ_BF16 ? launch_prompt<128, __nv_bfloat16>(a, dtype, s) : launch_prompt<128, __half>(a, dtype, s);
-  return dtype == OFFQ_BF16 ? launch_prompt<64, __nv_bfloat16>(a, dtype, s) : launch_prompt<64, __half>(a, dtype, s);
+int prompt_tc(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s) {
+  return mode == kWindowed ? launch_prompt_m<kWindowed>(a, dtype, head_dim, s)
+                           : launch_prompt_m<kCausal>(a, dtype, head_dim, s);
 }
 
 }  // namespace offq

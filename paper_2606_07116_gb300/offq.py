@@ -100,6 +100,17 @@ _SIGNATURES = {
                                       _c_vp, _c_i64, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i32, _c_i32, _c_f32,
                                       _c_vp, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]),
     "offq_paged_attention_workspace": (_c_i64, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "offq_paged_attention_window": (_c_int, [_c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64, _c_vp, _c_vp, _c_vp,
+                                             _c_vp, _c_i64, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i32, _c_i32, _c_f32,
+                                             _c_i32, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "offq_paged_attention_prefix": (_c_int, [_c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64, _c_vp, _c_vp, _c_vp,
+                                             _c_vp, _c_i64, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i32, _c_i32, _c_vp,
+                                             _c_i64, _c_vp, _c_vp, _c_i32, _c_f32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i64,
+                                             _c_vp]),
+    "offq_paged_attention_prefix_workspace": (_c_i64, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "offq_prompt_attention_window": (_c_int, [_c_vp, _c_vp, _c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64,
+                                              _c_i64, _c_i64, _c_vp, _c_i32, _c_f32, _c_i32, _c_i32, _c_vp, _c_i64,
+                                              _c_vp, _c_vp]),
     "offq_prompt_attention": (_c_int, [_c_vp, _c_vp, _c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64, _c_i64,
                                        _c_i64, _c_vp, _c_i32, _c_f32, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp]),
 }
@@ -696,6 +707,14 @@ class KV4Cache(NamedTuple):
     v_params: torch.Tensor
 
 
+class SharedPrefix(NamedTuple):
+    """Prefixes that sequences of a batch share: prefix g is the first lens[g] ([P] int32) tokens of the pages table[g]
+    ([P, width] int32), and the sequences cu[g] .. cu[g + 1] - 1 (cu [P + 1] int32, non-decreasing) stand behind it."""
+    table: torch.Tensor
+    lens: torch.Tensor
+    cu: torch.Tensor
+
+
 def kv4_cache(pages: int, heads: int, head_dim: int = 128, page_size: int = 64, device=None) -> KV4Cache:
     """Uninitialised pages (a slot means something once a token was written to it)."""
     def codes():
@@ -780,13 +799,41 @@ def offq_paged_attention(q: torch.Tensor, Tq: int, Hq: int, H: int, head_dim: in
         _ptr(cu_q), B, max_q, scale, _ptr(out), ld_out, _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
-def paged_attention_workspace(Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int) -> int:
-    return load_library().offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q)
+def offq_paged_attention_window(q: torch.Tensor, Tq: int, Hq: int, H: int, head_dim: int, ld_q: int, cache: KV4Cache,
+                                pages: int, page_size: int, block_table: torch.Tensor, ld_table: int,
+                                lens: torch.Tensor, cu_q: torch.Tensor, B: int, max_q: int, scale: float, window: int,
+                                sinks: int, out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor],
+                                workspace: Optional[torch.Tensor], workspace_bytes: int, stream=None) -> None:
+    _check("offq_paged_attention_window", load_library().offq_paged_attention_window(
+        _ptr(q), _dtype_code(q), Tq, Hq, H, head_dim, ld_q, _ptr(cache.k_codes), _ptr(cache.k_params),
+        _ptr(cache.v_codes), _ptr(cache.v_params), pages, page_size, _ptr(block_table), ld_table, _ptr(lens),
+        _ptr(cu_q), B, max_q, scale, window, sinks, _ptr(out), ld_out, _ptr(lse), _ptr(workspace), workspace_bytes,
+        _stream(stream)))
+
+
+def offq_paged_attention_prefix(q: torch.Tensor, Tq: int, Hq: int, H: int, head_dim: int, ld_q: int, cache: KV4Cache,
+                                pages: int, page_size: int, block_table: torch.Tensor, ld_table: int,
+                                lens: torch.Tensor, cu_q: torch.Tensor, B: int, max_q: int, prefix_table: torch.Tensor,
+                                ld_prefix: int, prefix_lens: torch.Tensor, cu_prefix: torch.Tensor, P: int,
+                                scale: float, out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor],
+                                workspace: Optional[torch.Tensor], workspace_bytes: int, stream=None) -> None:
+    _check("offq_paged_attention_prefix", load_library().offq_paged_attention_prefix(
+        _ptr(q), _dtype_code(q), Tq, Hq, H, head_dim, ld_q, _ptr(cache.k_codes), _ptr(cache.k_params),
+        _ptr(cache.v_codes), _ptr(cache.v_params), pages, page_size, _ptr(block_table), ld_table, _ptr(lens),
+        _ptr(cu_q), B, max_q, _ptr(prefix_table), ld_prefix, _ptr(prefix_lens), _ptr(cu_prefix), P, scale, _ptr(out),
+        ld_out, _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def paged_attention_workspace(Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int, prefixes: int = 0) -> int:
+    """Bytes of a workspace for such calls, with or without a window, behind that many shared prefixes."""
+    if prefixes == 0:
+        return load_library().offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q)
+    return load_library().offq_paged_attention_prefix_workspace(Tq, Hq, H, head_dim, B, max_q, prefixes)
 
 
 @functools.lru_cache(maxsize=1024)
-def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int) -> int:
-    need = paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q)
+def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int, prefixes: int = 0) -> int:
+    need = paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q, prefixes)
     if need < 0:
         raise LookupError  # not kept; the call itself says what is wrong with its sizes
     return need
@@ -798,6 +845,15 @@ def offq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: 
     _check("offq_prompt_attention", load_library().offq_prompt_attention(
         _ptr(q), _ptr(k), _ptr(v), _dtype_code(q), T, Hq, H, head_dim, ld_q, ld_k, ld_v, _ptr(cu), B, scale,
         1 if causal else 0, _ptr(out), ld_out, _ptr(lse), _stream(stream)))
+
+
+def offq_prompt_attention_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, T: int, Hq: int, H: int,
+                                 head_dim: int, ld_q: int, ld_k: int, ld_v: int, cu: torch.Tensor, B: int, scale: float,
+                                 window: int, sinks: int, out: torch.Tensor, ld_out: int, lse: Optional[torch.Tensor],
+                                 stream=None) -> None:
+    _check("offq_prompt_attention_window", load_library().offq_prompt_attention_window(
+        _ptr(q), _ptr(k), _ptr(v), _dtype_code(q), T, Hq, H, head_dim, ld_q, ld_k, ld_v, _ptr(cu), B, scale, window,
+        sinks, _ptr(out), ld_out, _ptr(lse), _stream(stream)))
 
 
 def _heads(x: torch.Tensor) -> Tuple[int, int, int, int]:
@@ -902,28 +958,58 @@ def kv4_paged_read(cache: KV4Cache, slots: torch.Tensor, rotate: bool = True, ro
     return k, v
 
 
+def _block_table(what: str, table: torch.Tensor, rows: int) -> Tuple[torch.Tensor, int]:
+    """A table of pages [rows, width] as the library takes it, and its width."""
+    if table.dim() != 2:
+        raise ValueError(f"{what} must be int32 [{rows}, width] with contiguous rows")
+    listed, width = table.shape
+    ld, inner = table.stride()
+    if table.dtype is not torch.int32 or listed != rows or (width > 1 and inner != 1):
+        raise ValueError(f"{what} must be int32 [{rows}, width] with contiguous rows")
+    if rows > 1 and ld != width:
+        # The library's leading dimension is the pages a row can hold as well as the way to the next one: columns that
+        # were not given would count as pages.
+        table = table.contiguous()
+    return table, width
+
+
+def _window(window: Optional[int], sinks: int) -> Tuple[int, int]:
+    """Both as the library takes them (32 bits; more tokens than a sequence can hold are all of them)."""
+    if window is None:
+        raise ValueError("sinks go with a window")
+    if window < 1 or sinks < 0:
+        raise ValueError("a window holds one token at least, and sinks are not negative")
+    return min(window, 0x7FFFFFFF), min(sinks, 0x7FFFFFFF)
+
+
 @_on_its_stream
 def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor, lens: torch.Tensor,
                     cu_q: torch.Tensor, max_q: int, scale: Optional[float] = None, lse: bool = False,
-                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None, *,
+                    window: Optional[int] = None, sinks: int = 0, prefix: Optional[SharedPrefix] = None):
     """New tokens' queries q [Tq, Hq, hd] over the pages block_table [B, width] (int32) of lens [B] cached tokens;
     sequence b's queries are rows cu_q[b] .. cu_q[b + 1] - 1 and its last tokens. A length may not pass the columns of
-    block_table (a part of a wider table is copied). Returns out, or (out, lse [Tq, Hq])."""
+    block_table (a part of a wider table is copied). Returns out, or (out, lse [Tq, Hq]).
+
+    With window, a query sees the window newest tokens up to itself and the first `sinks` of its sequence; pages that no
+    query sees may be given back (entries of any value). With prefix, it sees all of its sequence's prefix before those
+    tokens: each prefix is read once for all its sequences. One of the two at a time."""
     Tq, Hq, hd, ld_q = _heads(q)
     pages, H, page_size, _ = _cache_shape(cache, None, hd)
     B = lens.shape[0]
     _like("lens", lens, torch.int32, (B,))
     _like("cu_q", cu_q, torch.int32, (B + 1,))
-    if block_table.dim() != 2:
-        raise ValueError("block_table must be int32 [B, width] with contiguous rows")
-    listed, width = block_table.shape
-    ld_table, inner = block_table.stride()
-    if block_table.dtype is not torch.int32 or listed != B or (width > 1 and inner != 1):
-        raise ValueError("block_table must be int32 [B, width] with contiguous rows")
-    if B > 1 and ld_table != width:
-        # The library's ld_table is the pages a sequence can hold as well as the way to the next row: columns that were
-        # not given would count as pages.
-        block_table = block_table.contiguous()
+    block_table, width = _block_table("block_table", block_table, B)
+    P = 0
+    if window is not None or sinks:
+        window, sinks = _window(window, sinks)
+        if prefix is not None:
+            raise ValueError("a window does not go with shared prefixes")
+    if prefix is not None:
+        P = prefix.lens.shape[0]
+        _like("prefix.lens", prefix.lens, torch.int32, (P,))
+        _like("prefix.cu", prefix.cu, torch.int32, (P + 1,))
+        prefix_table, prefix_width = _block_table("prefix.table", prefix.table, P)
     ld_out = Hq * hd
     if out is None:
         out = torch.empty((Tq, Hq, hd), dtype=q.dtype, device=q.device)
@@ -933,28 +1019,42 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
         ld_out = _heads(out)[3]
     if workspace is None:
         try:
-            need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q)
+            need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q, P)
         except LookupError:
             need = 0
         workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None
     stats = torch.empty((Tq, Hq), dtype=torch.float32, device=q.device) if lse else None
-    offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table,
-                         width, lens, cu_q, B, max_q,
-                         scale if scale is not None else hd ** -0.5, out, ld_out, stats, workspace,
-                         workspace.nbytes if workspace is not None else 0, stream)
+    scale = scale if scale is not None else hd ** -0.5
+    workspace_bytes = workspace.nbytes if workspace is not None else 0
+    if window is not None:
+        offq_paged_attention_window(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table, width, lens, cu_q, B,
+                                    max_q, scale, window, sinks, out, ld_out, stats, workspace, workspace_bytes, stream)
+    elif P > 0:
+        offq_paged_attention_prefix(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table, width, lens, cu_q, B,
+                                    max_q, prefix_table, prefix_width, prefix.lens, prefix.cu, P, scale, out, ld_out,
+                                    stats, workspace, workspace_bytes, stream)
+    else:
+        offq_paged_attention(q, Tq, Hq, H, hd, ld_q, cache, pages, page_size, block_table, width, lens, cu_q, B, max_q,
+                             scale, out, ld_out, stats, workspace, workspace_bytes, stream)
     return (out, stats) if lse else out
 
 
 @_on_its_stream
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, scale: Optional[float] = None,
-                     causal: bool = True, lse: bool = False, out: Optional[torch.Tensor] = None, stream=None):
+                     causal: bool = True, lse: bool = False, out: Optional[torch.Tensor] = None, stream=None, *,
+                     window: Optional[int] = None, sinks: int = 0):
     """Attention inside packed sequences: rows cu[b] .. cu[b + 1] - 1 of q [T, Hq, hd] and k, v [T, H, hd] are sequence
-    b. Returns out, or (out, lse [T, Hq])."""
+    b. Returns out, or (out, lse [T, Hq]). With window (causal attention alone), a query sees the window newest tokens
+    up to itself and the first `sinks` of its sequence."""
     T, Hq, hd, ld_q = _heads(q)
     Tk, H, hk, ld_k = _heads(k)
     if (Tk, hk) != (T, hd) or v.shape != k.shape or k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("queries, keys and values have the same tokens, head size and type")
     _like("cu", cu, torch.int32, cu.shape[:1])
+    if window is not None or sinks:
+        window, sinks = _window(window, sinks)
+        if not causal:
+            raise ValueError("a window goes with causal attention")
     ld_out = Hq * hd
     if out is None:
         out = torch.empty((T, Hq, hd), dtype=q.dtype, device=q.device)
@@ -963,6 +1063,11 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
     else:
         ld_out = _heads(out)[3]
     stats = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if lse else None
-    offq_prompt_attention(q, k, v, T, Hq, H, hd, ld_q, ld_k, _heads(v)[3], cu, cu.shape[0] - 1,
-                          scale if scale is not None else hd ** -0.5, causal, out, ld_out, stats, stream)
+    scale = scale if scale is not None else hd ** -0.5
+    if window is not None:
+        offq_prompt_attention_window(q, k, v, T, Hq, H, hd, ld_q, ld_k, _heads(v)[3], cu, cu.shape[0] - 1, scale, window,
+                                     sinks, out, ld_out, stats, stream)
+    else:
+        offq_prompt_attention(q, k, v, T, Hq, H, hd, ld_q, ld_k, _heads(v)[3], cu, cu.shape[0] - 1, scale, causal, out,
+                              ld_out, stats, stream)
     return (out, stats) if lse else out
