@@ -29,10 +29,10 @@ int check_attention(int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_d
 
 // Calls whose sequences may all have few rows need the small form's parts alone; others may take both forms, one
 // after the other on the same bytes.
-int64_t workspace_bytes_for(int head_dim, int64_t most_rows) {
+int64_t workspace_bytes_for(int head_dim, int64_t most_rows, int few_rows) {
   const int64_t few = paged_few_workspace(head_dim), chunk = paged_chunk_workspace(head_dim);
   if (few < 0 || chunk < 0) return -1;
-  return most_rows > kFewRows ? std::max(few, chunk) : few;
+  return most_rows > few_rows ? std::max(few, chunk) : few;
 }
 
 // Behind shared prefixes: the most rows that a prefix may have, and the bytes of all rows' two sums and statistics.
@@ -53,7 +53,7 @@ extern "C" int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_
       max_q < 0)
     return -1;
   if (Tq == 0 || B == 0 || max_q == 0) return 0;
-  return workspace_bytes_for(head_dim, static_cast<int64_t>(max_q) * (Hq / H));
+  return workspace_bytes_for(head_dim, static_cast<int64_t>(max_q) * (Hq / H), kFewRows);
 }
 
 extern "C" int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
@@ -61,7 +61,7 @@ extern "C" int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq,
   if (P < 0 || P > 65535) return -1;
   const int64_t parts = offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q);
   if (parts <= 0 || P == 0) return parts;
-  const int64_t most = workspace_bytes_for(head_dim, shared_rows(Tq, B, max_q, Hq / H));
+  const int64_t most = workspace_bytes_for(head_dim, shared_rows(Tq, B, max_q, Hq / H), kFewSharedRows);
   return most < 0 ? -1 : most + sums_bytes(Tq, Hq, head_dim);
 }
 
@@ -97,17 +97,14 @@ int paged_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, int32_t 
   a.status = device_status_ptr();
   const int64_t own_rows = static_cast<int64_t>(a.max_q) * a.G;
   const int64_t most_rows = mode == kShared ? shared_rows(a.Tq, a.B, a.max_q, a.G) : own_rows;
-  const int64_t parts = workspace_bytes_for(head_dim, most_rows);
+  a.few_rows = mode == kShared ? kFewSharedRows : kFewRows;
+  const int64_t parts = workspace_bytes_for(head_dim, most_rows, a.few_rows);
   if (a.status == nullptr || parts < 0) return OFFQ_ERR_CUDA;
   const int64_t need = mode == kShared ? parts + sums_bytes(a.Tq, a.Hq, head_dim) : parts;
   if (a.workspace == nullptr || workspace_bytes < need) return OFFQ_ERR_INVALID_ARG;
-  a.few_rows = kFewRows;
   if (mode == kShared) {
     a.sums = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + parts);
     a.stats = reinterpret_cast<float2*>(a.sums + 2 * a.Tq * a.Hq * head_dim);
-    // Sequences of up to 8 rows each keep the few-row form of 8 rows: its 16 warps read faster than the 8 of 16 rows.
-    // The queries of a prefix that has 9 to 16 rows take the many-row form then.
-    if (own_rows <= 8) a.few_rows = 8;
   }
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (const int rc = paged_few(a, mode, dtype, head_dim, s); rc != OFFQ_OK) return rc;

@@ -191,13 +191,16 @@ __device__ __forceinline__ void write_lse(const AttnArgs& a, int first, int h, i
       l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-// kShared: sums over a prefix (b < P) or over a sequence's own tokens, channel 0 of row r of (first query row, key head h),
+// kShared: sums over a prefix (b < P) or over a sequence's own tokens, the channels of row r of (first query row, key head h),
 // and the row's statistics.
 template <int D>
 __device__ __forceinline__ float* shared_sums(const AttnArgs& a, int b, int first, int h, int r) {
   const int64_t t = (b < a.P ? 0 : a.Tq) + first + r / a.G;
   return a.sums + (t * a.Hq + h * a.G + r % a.G) * D;
 }
+// Where channel d stands in a row of sums: of 16 channels, d and d + 4, then d + 8 and d + 12 side by side, as a lane of the
+// many-row form holds them.
+__host__ __device__ constexpr int shared_at(int d) { return (d & ~15) + (d & 3) * 4 + (d >> 3 & 1) * 2 + (d >> 2 & 1); }
 __device__ __forceinline__ void write_stats(const AttnArgs& a, int b, int first, int h, int r, float m, float l) {
   const int64_t t = (b < a.P ? 0 : a.Tq) + first + r / a.G;
   a.stats[t * a.Hq + h * a.G + r % a.G] = make_float2(m, l);
@@ -206,6 +209,8 @@ __device__ __forceinline__ void write_stats(const AttnArgs& a, int b, int first,
 // The few-row form of offq_paged_attention (csrc/attn_few.cu): rows n * G of a sequence that it takes, its
 // workspace, and its launch with arguments already checked.
 constexpr int kFewRows = 16;
+// Behind shared prefixes it takes groups of 8 or 16 rows, up to this many in all.
+constexpr int kFewSharedRows = 32;
 int64_t paged_few_workspace(int head_dim);
 int paged_few(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s);
 

@@ -79,6 +79,10 @@ __device__ __forceinline__ float* part_data(void* ws, int ctas, int cta, int whi
   return reinterpret_cast<float*>(static_cast<PartHead*>(ws) + 2 * ctas) + (2 * cta + which) * ChunkLayout<D>::kPartFloats;
 }
 
+// What a tile costs besides its blocks, in blocks: shares of the list count it (kCausal's tiles are long against it).
+template <AttnMode M>
+constexpr int kTileCost = M == kCausal ? 0 : 4;
+
 constexpr int kGroup = 8;  // keys whose page a lane of the widening warps looks up
 
 // Tokens that row pair tile p leaves out under a window: it numbers those that its rows see, the gap in whole groups.
@@ -156,11 +160,9 @@ __device__ __forceinline__ void write_pair(T* row, int k, int lane, float x, flo
   const uint32_t v1 = __shfl_sync(kAllLanes, u, (lane & ~3) | ((2 * c + 1) & 3));
   if (row != nullptr) *reinterpret_cast<uint32_t*>(row + 8 * k + 2 * c) = __byte_perm(v0, v1, c < 2 ? 0x5410 : 0x7632);
 }
-// kShared: the same lanes' channels 8 k + c and 8 k + c + 4 as sums.
-__device__ __forceinline__ void write_sums(float* row, int k, int lane, float x, float y) {
-  if (row == nullptr) return;
-  row[8 * k + (lane & 3)] = x;
-  row[8 * k + (lane & 3) + 4] = y;
+// kShared: the same lanes' channels of k = 2 u (x, y) and 2 u + 1 (z, w) as sums, in the order of shared_at.
+__device__ __forceinline__ void write_sums(float* row, int u, int lane, float x, float y, float z, float w) {
+  if (row != nullptr) reinterpret_cast<float4*>(row)[4 * u + (lane & 3)] = make_float4(x, y, z, w);
 }
 template <int D, typename T, AttnMode M>
 __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
@@ -196,47 +198,80 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   __syncthreads();
   PartHead* heads = part_heads(a.workspace, blockIdx.x);
   if (warp == 9) {
-    auto steps = [&](int b, PagedSeq& s) {  // of one head of sequence b
+    struct Cost {  // of one head of a sequence, in blocks: with what its tiles cost besides, and without
+      long long all, blocks;
+    };
+    auto cost = [&](int b, PagedSeq& s) {
       s = paged_seq<M>(a, b);
-      long long n = 0;
-      for (int p = 0, tiles = tiles_of(a, s); p < tiles; ++p) n += tile_blocks<M>(a, s, p);
+      Cost n = {0, 0};
+      for (int p = 0, tiles = tiles_of(a, s); p < tiles; ++p) n.blocks += tile_blocks<M>(a, s, p);
+      n.all = n.blocks + static_cast<long long>(kTileCost<M>) * tiles_of(a, s);
       return n;
     };
-    long long total = 0;
+    auto warp_sum = [&](long long v) {
+#pragma unroll
+      for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(kAllLanes, v, m);
+      return v;
+    };
+    Cost sum = {0, 0};
     const int B = listed<M>(a);
     for (int b = lane; b < B; b += 32) {
       PagedSeq s;
-      total += steps(b, s) * a.H;
+      const Cost n = cost(b, s);
+      sum.all += n.all * a.H;
+      sum.blocks += n.blocks * a.H;
       if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
     }
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) total += __shfl_xor_sync(kAllLanes, total, m);
+    const long long total = warp_sum(sum.all), all_blocks = warp_sum(sum.blocks);
     const long long ctas = min(total, static_cast<long long>(gridDim.x));
     const long long lo = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
     const long long hi = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
-    long long before = 0;
-    for (int first = 0; first < B && before <= lo && lo < hi; first += 32) {
+    // Both ends as numbers of blocks before them; the first as a place too.
+    Cost before = {0, 0};
+    long long from = 0, to = lo < hi && hi == total ? all_blocks : 0;
+    for (int first = 0; first < B && before.all <= hi && lo < hi; first += 32) {
       PagedSeq s;
-      const long long one = first + lane < B ? steps(first + lane, s) : 0, val = one * a.H;
-      long long incl = val;
+      Cost one = {0, 0};
+      if (first + lane < B) one = cost(first + lane, s);
+      Cost incl = {one.all * a.H, one.blocks * a.H};
 #pragma unroll
       for (int m = 1; m < 32; m <<= 1) {
-        const long long o = __shfl_up_sync(kAllLanes, incl, m);
-        if (lane >= m) incl += o;
+        const long long x = __shfl_up_sync(kAllLanes, incl.all, m), y = __shfl_up_sync(kAllLanes, incl.blocks, m);
+        if (lane >= m) {
+          incl.all += x;
+          incl.blocks += y;
+        }
       }
-      const long long start = before + incl - val;
-      if (lo >= start && lo < start + val) {
-        long long at = (lo - start) % one;
+      const long long end = before.all + incl.all, start = end - one.all * a.H;
+      const long long blocks = before.blocks + incl.blocks - one.blocks * a.H;
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        const long long x = which ? hi : lo;
+        if (x < start || x >= end) continue;
+        const long long h = (x - start) / one.all;
+        long long at = (x - start) % one.all, passed = blocks + h * one.blocks;
         int p = 0;
-        for (int n = tile_blocks<M>(a, s, 0); at >= n; n = tile_blocks<M>(a, s, ++p)) at -= n;
-        ctrl->b = first + lane;
-        ctrl->h = static_cast<int>((lo - start) / one);
-        ctrl->p = p;
-        ctrl->blk = static_cast<int>(at);
-        ctrl->count = static_cast<int>(hi - lo);
+        for (int n = tile_blocks<M>(a, s, 0); at >= n + kTileCost<M>; n = tile_blocks<M>(a, s, ++p)) {
+          at -= n + kTileCost<M>;
+          passed += n;
+        }
+        at = max(0LL, at - kTileCost<M>);
+        if (which) {
+          to = passed + at;
+        } else {
+          from = passed + at;
+          ctrl->b = first + lane;
+          ctrl->h = static_cast<int>(h);
+          ctrl->p = p;
+          ctrl->blk = static_cast<int>(at);
+        }
       }
-      before += __shfl_sync(kAllLanes, incl, 31);
+      before.all += __shfl_sync(kAllLanes, incl.all, 31);
+      before.blocks += __shfl_sync(kAllLanes, incl.blocks, 31);
     }
+    from = warp_sum(from);  // one lane's each
+    to = hi == total ? to : warp_sum(to);
+    if (lane == 0) ctrl->count = static_cast<int>(to - from);
     if (lane < 2) heads[lane] = PartHead{-1, 0, 0, 0};
   }
   tc_fence_before();
@@ -756,20 +791,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
-                float v[4];
+                float v[4], u[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(o[hh][4 * k + e]) + off[2 * hh + (e >> 1)];
-                if (complete) {
-#pragma unroll
-                  for (int ii = 0; ii < 2; ++ii) {
-                    if constexpr (M == kShared)
-                      write_sums(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii], v[2 * ii + 1]);
-                    else
-                      write_pair<T>(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii] * inv[2 * hh + ii], v[2 * ii + 1] * inv[2 * hh + ii]);
-                  }
-                } else {
+                if (!complete) {
                   reinterpret_cast<float4*>(part + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + 4 * q + k) * 32 + lane] =
                       make_float4(v[0], v[1], v[2], v[3]);
+                } else if constexpr (M == kShared) {
+                  if ((k & 1) == 0) continue;
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) u[e] = __uint_as_float(o[hh][4 * k - 4 + e]) + off[2 * hh + (e >> 1)];
+#pragma unroll
+                  for (int ii = 0; ii < 2; ++ii)
+                    write_sums(to[2 * hh + ii], 2 * q + k / 2, lane, u[2 * ii], u[2 * ii + 1], v[2 * ii], v[2 * ii + 1]);
+                } else {
+#pragma unroll
+                  for (int ii = 0; ii < 2; ++ii)
+                    write_pair<T>(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii] * inv[2 * hh + ii], v[2 * ii + 1] * inv[2 * hh + ii]);
                 }
               }
             __syncwarp();
@@ -793,9 +831,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
 }
 
 // Row pair tiles that cross CTAs: begun at the end of CTA blockIdx.x, then the first parts of the CTAs after it up to
-// their last. Block y takes one softmax warp's 32 rows; a warp of it a quarter of the channels.
+// their last. Block y takes one softmax warp's 32 rows; a warp of it 16 channels. The reads of four parts are in flight
+// together: a part at a time they took most of this kernel's time (34 us where a tile has ten).
 template <int D, typename T, AttnMode M>
-__global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int ctas) {
+__global__ void __launch_bounds__(2 * D) join_chunks_kernel(const AttnArgs a, int ctas) {
   __shared__ int s_last;
   const int cta = blockIdx.x, tid = threadIdx.x, lane = tid & 31, q = tid >> 5, g = lane >> 2, c = lane & 3;
   if (tid == 0) s_last = 0x7FFFFFFF;
@@ -814,7 +853,8 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
   const PagedSeq s = paged_seq<M>(a, p.b);
   const int rows = s.n * a.G, warp = blockIdx.y, row0 = p.p * kPairRows + warp * 32;
   if (row0 >= rows) return;
-  constexpr int kReps = D / 32;  // of 8 channels, per warp
+  constexpr int kReps = 2;  // of 8 channels, per warp
+  constexpr int kAtOnce = 4;
   float top[4], sum[4];
   float4 acc[2][kReps];
 #pragma unroll
@@ -826,29 +866,48 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
   for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
     for (int k = 0; k < kReps; ++k) acc[hh][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int part = cta; part <= last; ++part) {
-    const float* src = part_data<D>(a.workspace, ctas, part, part == cta ? 1 : 0);
-    float x_old[4], x_new[4];
+  for (int part0 = cta; part0 <= last; part0 += kAtOnce) {
+    float mk[kAtOnce][4], lk[kAtOnce][4];
+    float4 v[kAtOnce][2][kReps];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int r = warp * 32 + 8 * x + g;
-      const float mk = src[r], next = fmaxf(top[x], mk);
-      x_old[x] = top[x] == -INFINITY ? 0.f : ex2(top[x] - next);
-      x_new[x] = mk == -INFINITY ? 0.f : ex2(mk - next);
-      sum[x] = sum[x] * x_old[x] + src[kPairRows + r] * x_new[x];
-      top[x] = next;
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (part0 + j > last) continue;
+      const float* src = part_data<D>(a.workspace, ctas, part0 + j, part0 + j == cta ? 1 : 0);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        mk[j][x] = src[warp * 32 + 8 * x + g];
+        lk[j][x] = src[kPairRows + warp * 32 + 8 * x + g];
+      }
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int k = 0; k < kReps; ++k)
+          v[j][hh][k] = reinterpret_cast<const float4*>(src + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + q * kReps + k) * 32 + lane];
     }
 #pragma unroll
-    for (int hh = 0; hh < 2; ++hh)
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (part0 + j > last) continue;
+      float x_old[4], x_new[4];
 #pragma unroll
-      for (int k = 0; k < kReps; ++k) {
-        const float4 v = reinterpret_cast<const float4*>(src + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + q * kReps + k) * 32 + lane];
-        float4& o = acc[hh][k];
-        o.x = o.x * x_old[2 * hh] + v.x * x_new[2 * hh];
-        o.y = o.y * x_old[2 * hh] + v.y * x_new[2 * hh];
-        o.z = o.z * x_old[2 * hh + 1] + v.z * x_new[2 * hh + 1];
-        o.w = o.w * x_old[2 * hh + 1] + v.w * x_new[2 * hh + 1];
+      for (int x = 0; x < 4; ++x) {
+        const float next = fmaxf(top[x], mk[j][x]);
+        x_old[x] = top[x] == -INFINITY ? 0.f : ex2(top[x] - next);
+        x_new[x] = mk[j][x] == -INFINITY ? 0.f : ex2(mk[j][x] - next);
+        sum[x] = sum[x] * x_old[x] + lk[j][x] * x_new[x];
+        top[x] = next;
       }
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) {
+          const float4 n = v[j][hh][k];
+          float4& o = acc[hh][k];
+          o.x = o.x * x_old[2 * hh] + n.x * x_new[2 * hh];
+          o.y = o.y * x_old[2 * hh] + n.y * x_new[2 * hh];
+          o.z = o.z * x_old[2 * hh + 1] + n.z * x_new[2 * hh + 1];
+          o.w = o.w * x_old[2 * hh + 1] + n.w * x_new[2 * hh + 1];
+        }
+    }
   }
 #pragma unroll
   for (int hh = 0; hh < 2; ++hh)
@@ -857,9 +916,8 @@ __global__ void __launch_bounds__(128) join_chunks_kernel(const AttnArgs a, int 
       const int x = 2 * hh + ii, r = row0 + 8 * x + g;
       if constexpr (M == kShared) {
         float* to = r < rows ? shared_sums<D>(a, p.b, s.first, p.h, r) : nullptr;
-#pragma unroll
-        for (int k = 0; k < kReps; ++k)
-          write_sums(to, q * kReps + k, lane, ii ? acc[hh][k].z : acc[hh][k].x, ii ? acc[hh][k].w : acc[hh][k].y);
+        const float4 u = acc[hh][0], v = acc[hh][1];
+        write_sums(to, q, lane, ii ? u.z : u.x, ii ? u.w : u.y, ii ? v.z : v.x, ii ? v.w : v.y);
         if (q == 0 && c == 0 && r < rows) write_stats(a, p.b, s.first, p.h, r, top[x], sum[x]);
         continue;
       }
@@ -878,7 +936,7 @@ int launch_chunk(const AttnArgs& a, cudaStream_t s) {
   const int sms = device_sms();
   if (sms == 0 || !smem_optin<chunk_kernel<D, T, M>>(L::kBytes)) return OFFQ_ERR_CUDA;
   if (const int rc = launch_pdl(chunk_kernel<D, T, M>, dim3(sms), dim3(kThreads), L::kBytes, s, a); rc != OFFQ_OK) return rc;
-  return launch_pdl(join_chunks_kernel<D, T, M>, dim3(sms, 8), dim3(128), 0, s, a, sms);
+  return launch_pdl(join_chunks_kernel<D, T, M>, dim3(sms, 8), dim3(2 * D), 0, s, a, sms);
 }
 
 template <AttnMode M>

@@ -127,6 +127,28 @@ __device__ __forceinline__ int stages_of(const AttnArgs& a, const PagedSeq& s) {
   return max(1, (s.len + kTile - 1) / kTile);
 }
 
+// Behind shared prefixes a sequence's rows may be several groups of what the kernel holds. A unit of its work is a group and a
+// head, number group * H + head, and the groups read the same pages one after the other, from the L2 but for the first.
+constexpr int kMostGroups = 4;
+template <AttnMode M, int ROWS>
+__device__ __forceinline__ int groups_of(const AttnArgs& a, const PagedSeq& s) {
+  return M == kShared ? (s.n * a.G + ROWS - 1) / ROWS : 1;
+}
+// The units of all sequences as one list: unit u of sequence b (fits an int: two lists of 65535 sequences, 4096 heads).
+template <AttnMode M>
+__device__ __forceinline__ int unit_id(const AttnArgs& a, int b, int u) {
+  return b * (M == kShared ? kMostGroups : 1) * a.H + u;
+}
+struct Unit {
+  int b, h, row0;
+};
+template <AttnMode M, int ROWS>
+__device__ __forceinline__ Unit unit_at(const AttnArgs& a, int id) {
+  const int b = id / a.H;
+  if constexpr (M == kShared) return {b / kMostGroups, id - b * a.H, b % kMostGroups * ROWS};
+  return {b, id - b * a.H, 0};
+}
+
 // A sequence in this form's numbers: under a window without the gap that none of its queries sees, whole stages of it.
 template <AttnMode M>
 __device__ __forceinline__ PagedSeq few_seq(const AttnArgs& a, int b) {
@@ -159,9 +181,9 @@ __device__ __forceinline__ float* part_sums(void* ws, int ctas, int cta, int whi
 template <int D, typename T, AttnMode M>
 __device__ __forceinline__ void write_row8(const AttnArgs& a, int b, int first, int h, int r, int d, const float (&v)[8]) {
   if constexpr (M == kShared) {
-    float4* dst = reinterpret_cast<float4*>(shared_sums<D>(a, b, first, h, r) + d);
-    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
-    dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+    float* dst = shared_sums<D>(a, b, first, h, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<float2*>(dst + shared_at(d + e)) = make_float2(v[e], v[e + 4]);
     return;
   }
   const int64_t t = static_cast<int64_t>(first) + r / a.G;
@@ -207,7 +229,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   for (int b = tid; b < B; b += kThreads) {
     const PagedSeq s = few_seq<M>(a, b);
     if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-    mine += static_cast<long long>(stages_of(a, s)) * a.H;
+    mine += static_cast<long long>(stages_of(a, s)) * a.H * groups_of<M, L::kRows>(a, s);
   }
   auto warp_sum = [&](long long v) {
 #pragma unroll
@@ -232,7 +254,10 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   long long before = 0;
   for (int base = 0; base < B && before < hi; base += kThreads) {
     long long val = 0;
-    if (base + tid < B) val = static_cast<long long>(stages_of(a, few_seq<M>(a, base + tid))) * a.H;
+    if (base + tid < B) {
+      const PagedSeq s = few_seq<M>(a, base + tid);
+      val = static_cast<long long>(stages_of(a, s)) * a.H * groups_of<M, L::kRows>(a, s);
+    }
     long long incl = val;
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) {
@@ -268,6 +293,13 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     PagedSeq s = few_seq<M>(a, b);
     int stages = stages_of(a, s);
     int h = static_cast<int>(ctrl->start[warp] / stages), t = static_cast<int>(ctrl->start[warp] % stages);
+    int row0 = 0, pgroup = 0, pgroups = 1;  // this unit's first row; where the copies are
+    if constexpr (M == kShared) {
+      pgroup = h / a.H;
+      pgroups = groups_of<M, L::kRows>(a, s);
+      h %= a.H;
+      row0 = pgroup * L::kRows;
+    }
 
     // Where the copies are: they run ahead across heads and sequences.
     int pb = b, ph = h, pt = t, pstages = stages, plen = s.len, listed_from = -64, entry = 0;
@@ -329,8 +361,16 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
       if (--ahead > 0 && ++pt == pstages) {
         pt = 0;
         turn = true;
+        bool next = false;  // the next sequence
         if (++ph == a.H) {
           ph = 0;
+          next = true;
+          if constexpr (M == kShared) {
+            next = ++pgroup == pgroups;
+            if (next) pgroup = 0;
+          }
+        }
+        if (next) {
           listed_from = -64;
           PagedSeq n;
           do {
@@ -338,6 +378,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             pstages = stages_of(a, n);
           } while (pstages == 0);
           plen = n.len;
+          if constexpr (M == kShared) pgroups = groups_of<M, L::kRows>(a, n);
           if constexpr (M == kWindowed) {
             pfrom = window_from(a, position<M>(n) + 1);
             pshift = window_gap(a, position<M>(paged_seq<M>(a, pb)), kTile).shift;
@@ -365,12 +406,13 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         begin = false;
         t_first = t;
         rows = s.n * a.G;
+        if constexpr (M == kShared) rows = min(rows - row0, L::kRows);
         sees_least = M == kShared ? min(s.len, max(0, s.at + 1)) : max(0, s.len - s.n + 1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const int r = 8 * nt + g;
-          const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first) + r / a.G) * a.ld_q +
-                         static_cast<int64_t>(h * a.G + r % a.G) * D + c * (D / 4);
+          const int r = 8 * nt + g, rr = row0 + r;
+          const T* src = static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first) + rr / a.G) * a.ld_q +
+                         static_cast<int64_t>(h * a.G + rr % a.G) * D + c * (D / 4);
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < kKw; ++i) {
@@ -397,7 +439,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             qs[nt][j] = __shfl_sync(kAllLanes, sum, 4 * (2 * c + j));
             l[nt][j] = w[nt][j] = 0.f;
             const int rr = 8 * nt + 2 * c + j;
-            sees[nt][j] = rr < rows ? max(0, min(s.len, position<M>(s) + rr / a.G + 1)) : 0;
+            sees[nt][j] = rr < rows ? max(0, min(s.len, position<M>(s) + (row0 + rr) / a.G + 1)) : 0;
             m[nt][j] = sees[nt][j] > 0 ? -INFINITY : 0.f;  // a row without keys has no maximum to wait for
           }
 #pragma unroll
@@ -576,9 +618,9 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = (o[nt][4 * q8 + e / 2][j + 2 * (e & 1)] + w[nt][j]) * inv;
-                write_row8<D, T, M>(a, b, s.first, h, r, g * (D / 8) + 8 * q8, v);
+                write_row8<D, T, M>(a, b, s.first, h, row0 + r, g * (D / 8) + 8 * q8, v);
               }
-              if (g == 0) write_row_stats<M>(a, b, s.first, h, r, m[nt][j], l[nt][j]);
+              if (g == 0) write_row_stats<M>(a, b, s.first, h, row0 + r, m[nt][j], l[nt][j]);
             }
           } else {
 #pragma unroll
@@ -590,13 +632,22 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
           }
         }
       }
-      if (!complete && lane == 0) ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, h, t_first, t == stages ? -1 : t);
+      if (!complete && lane == 0) ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, M == kShared ? row0 / L::kRows * a.H + h : h, t_first, t == stages ? -1 : t);
       first_part = false;
       begin = true;
       if (it + 1 < todo) {
         t = 0;
+        bool next = false;  // the next sequence
         if (++h == a.H) {
           h = 0;
+          next = true;
+          if constexpr (M == kShared) {
+            row0 += L::kRows;
+            next = row0 >= s.n * a.G;
+            if (next) row0 = 0;
+          }
+        }
+        if (next) {
           do {
             s = few_seq<M>(a, ++b);
             stages = stages_of(a, s);
@@ -612,21 +663,23 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   constexpr int kParts = 2 * L::kWarps;
   static_assert(kParts <= 32, "a lane for each part");
   const int4 mypart = lane < kParts ? ctrl->part[lane] : make_int4(-1, 0, 0, 0);
-  const int my_id = mypart.x < 0 ? -1 : mypart.x * a.H + mypart.y;
+  const int my_id = mypart.x < 0 ? -1 : unit_id<M>(a, mypart.x, mypart.y);
   uint32_t left = __ballot_sync(kAllLanes, my_id >= 0);
   bool have0 = false, have1 = false;
   while (left != 0) {
     const int i = __ffs(left) - 1;
-    const int id = __shfl_sync(kAllLanes, my_id, i), b = __shfl_sync(kAllLanes, mypart.x, i);
+    const int id = __shfl_sync(kAllLanes, my_id, i);
+    const Unit unit = unit_at<M, L::kRows>(a, id);
     const uint32_t same = __ballot_sync(kAllLanes, my_id == id);
     const int begins = __shfl_sync(kAllLanes, mypart.z, i), last = __shfl_sync(kAllLanes, mypart.w, 31 - __clz(same));
     left &= ~same;
     const bool complete = begins == 0 && last < 0;
-    const int which = begins == 0 ? 1 : 0, h = id - b * a.H;
+    const int which = begins == 0 ? 1 : 0;
     float* dst = part_sums<D, NT>(a.workspace, gridDim.x, blockIdx.x, which);
-    const PagedSeq s = paged_seq<M>(a, b);
+    const PagedSeq s = paged_seq<M>(a, unit.b);
+    const int rows = min(s.n * a.G - unit.row0, L::kRows);
     if (!complete) (which ? have1 : have0) = true;
-    if (!complete && tid == 0) heads[which] = PartHead{id, last < 0, s.first, s.n * a.G};
+    if (!complete && tid == 0) heads[which] = PartHead{id, last < 0, s.first, rows};
     for (int u = tid; u < L::kRows * (D / 8); u += kThreads) {
       const int r = u / (D / 8), d = u % (D / 8) * 8;
       float top = -INFINITY, sum = 0.f, v[8] = {};
@@ -642,12 +695,12 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         top = next;
       }
       if (complete) {
-        if (r < s.n * a.G) {
+        if (r < rows) {
           const float inv = M == kShared ? 1.f : sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= inv;
-          write_row8<D, T, M>(a, b, s.first, h, r, d, v);
-          if (d == 0) write_row_stats<M>(a, b, s.first, h, r, top, sum);
+          write_row8<D, T, M>(a, unit.b, s.first, unit.h, unit.row0 + r, d, v);
+          if (d == 0) write_row_stats<M>(a, unit.b, s.first, unit.h, unit.row0 + r, top, sum);
         }
       } else {
         reinterpret_cast<float4*>(dst + r * D + d)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -690,7 +743,8 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int c
   __syncthreads();
   const int last = s_last;
   if (last >= ctas) return;  // not this call's parts (a workspace that another call writes): none is read past them
-  const int rows = p.rows, h = p.id % a.H;
+  const int rows = p.rows;
+  const Unit unit = unit_at<M, L::kRows>(a, p.id);
   for (int u = tid; u < rows * (D / 8); u += blockDim.x) {
     const int r = u / (D / 8), d = u % (D / 8) * 8;
     float top = -INFINITY, sum = 0.f, v[8] = {};
@@ -736,8 +790,8 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const AttnArgs a, int c
     const float inv = M == kShared ? 1.f : sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= inv;
-    write_row8<D, T, M>(a, p.id / a.H, p.first, h, r, d, v);
-    if (d == 0) write_row_stats<M>(a, p.id / a.H, p.first, h, r, top, sum);
+    write_row8<D, T, M>(a, unit.b, p.first, unit.h, unit.row0 + r, d, v);
+    if (d == 0) write_row_stats<M>(a, unit.b, p.first, unit.h, unit.row0 + r, top, sum);
   }
 }
 
@@ -755,7 +809,7 @@ int launch_few(const AttnArgs& a, cudaStream_t s) {
 
 template <AttnMode M, int D>
 int launch_few_d(const AttnArgs& a, int dtype, cudaStream_t s) {
-  const bool two = std::min<int64_t>(static_cast<int64_t>(a.max_q) * a.G, a.few_rows) > 8;
+  const bool two = std::min<int64_t>(static_cast<int64_t>(a.max_q) * a.G, kFewRows) > 8;
   if (dtype == OFFQ_BF16) return two ? launch_few<D, 2, __nv_bfloat16, M>(a, s) : launch_few<D, 1, __nv_bfloat16, M>(a, s);
   return two ? launch_few<D, 2, __half, M>(a, s) : launch_few<D, 1, __half, M>(a, s);
 }

@@ -13,7 +13,6 @@ namespace {
 using namespace offq;
 
 constexpr int kThreads = 256;
-constexpr int kItems = 2;  // of 8 channels, per thread of the longest sequence's blocks
 
 // The prefix whose sequences b is one of, or -1. The warp looks at 32 of them at once.
 __device__ __forceinline__ int prefix_of(const AttnArgs& a, int b) {
@@ -34,21 +33,21 @@ __global__ void __launch_bounds__(kThreads) join_shared_kernel(const AttnArgs a)
   griddep_launch_dependents();
   const int b = blockIdx.x;
   const PagedSeq s = paged_seq<kShared>(a, a.P + b);
-  const int64_t items = static_cast<int64_t>(s.n) * a.Hq * (D / 8);
+  const int64_t items = static_cast<int64_t>(s.n) * a.Hq * (D / 16);
   int64_t u = static_cast<int64_t>(blockIdx.y) * kThreads + threadIdx.x;
-  if (u - (threadIdx.x & 31) >= items) return;  // a warp at a time: they look for the prefix together
+  if (u - (threadIdx.x & 31) >= items) return;  // whole warps: their lanes look for the prefix together
   // Sums of a prefix are there for the rows of its own range alone.
   const int g = prefix_of(a, b);
   const PagedSeq p = paged_seq<kShared>(a, max(g, 0));
   const bool shared = g >= 0 && p.first <= s.first && s.first + s.n <= p.first + p.n;
   for (; u < items; u += static_cast<int64_t>(gridDim.y) * kThreads) {
-    const int d = static_cast<int>(u % (D / 8)) * 8;
-    const int64_t row = static_cast<int64_t>(s.first) * a.Hq + u / (D / 8), own = a.Tq * a.Hq + row;
+    const int d = static_cast<int>(u % (D / 16)) * 16;
+    const int64_t row = static_cast<int64_t>(s.first) * a.Hq + u / (D / 16), own = a.Tq * a.Hq + row;
     const float2 none = make_float2(-INFINITY, 0.f);
     const float2 s0 = shared ? a.stats[row] : none, s1 = a.stats[own];
-    float4 x[2] = {}, y[2];
+    float4 x[4] = {}, y[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if (shared) x[i] = reinterpret_cast<const float4*>(a.sums + row * D + d)[i];
       y[i] = reinterpret_cast<const float4*>(a.sums + own * D + d)[i];
     }
@@ -56,33 +55,37 @@ __global__ void __launch_bounds__(kThreads) join_shared_kernel(const AttnArgs a)
     const float e0 = m0 == -INFINITY ? 0.f : ex2(m0 - m), e1 = m1 == -INFINITY ? 0.f : ex2(m1 - m);
     const float l = e0 * s0.y + e1 * s1.y, inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
     const float f0 = e0 * inv, f1 = e1 * inv;
-    uint32_t w[4];
+    float v[16];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float v[4] = {fmaf(x[i].x, f0, y[i].x * f1), fmaf(x[i].y, f0, y[i].y * f1), fmaf(x[i].z, f0, y[i].z * f1),
-                          fmaf(x[i].w, f0, y[i].w * f1)};
+    for (int i = 0; i < 4; ++i) {
+      const float p0[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, p1[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-          w[2 * i + k] = *reinterpret_cast<const uint32_t*>(&h);
-        } else {
-          const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-          w[2 * i + k] = *reinterpret_cast<const uint32_t*>(&h);
-        }
+      for (int e = 0; e < 4; ++e) v[i + 8 * (e >> 1) + 4 * (e & 1)] = fmaf(p0[e], f0, p1[e] * f1);  // shared_at's order undone
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
       }
     }
     const int64_t t = row / a.Hq;
-    *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + (row - t * a.Hq) * D + d) = make_uint4(w[0], w[1], w[2], w[3]);
+    uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + (row - t * a.Hq) * D + d);
+    to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    to[1] = make_uint4(w[4], w[5], w[6], w[7]);
     if (d == 0 && a.lse != nullptr) a.lse[row] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
 template <int D, typename T>
 int launch_join(const AttnArgs& a, cudaStream_t s) {
-  const int64_t items = static_cast<int64_t>(std::min<int64_t>(a.max_q, a.Tq)) * a.Hq * (D / 8);
+  const int64_t items = static_cast<int64_t>(std::min<int64_t>(a.max_q, a.Tq)) * a.Hq * (D / 16);
   // The longest sequence's items, but no more blocks in all than a few waves.
-  const int64_t blocks = std::min((items + kThreads * kItems - 1) / (kThreads * kItems), std::max(int64_t{1}, int64_t{32768} / a.B));
+  const int64_t blocks = std::min((items + kThreads - 1) / kThreads, std::max(int64_t{1}, int64_t{32768} / a.B));
   return launch_pdl(join_shared_kernel<D, T>, dim3(a.B, static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, a);
 }
 
