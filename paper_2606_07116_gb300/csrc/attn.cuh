@@ -155,6 +155,29 @@ __device__ __forceinline__ Gap window_gap(const AttnArgs& a, int at, int step) {
 // The first token that the window of a query leaves in, given the tokens up to itself (both in a run's numbers).
 __device__ __forceinline__ int window_from(const AttnArgs& a, int upto) { return upto > a.window ? upto - a.window : 0; }
 
+// x / y and the rest, x >= 0 and y > 0. A division of 64 bits is a call of some hundred instructions, a quarter of a microsecond
+// where they are not in a cache yet; few numbers here need one.
+struct Divided {
+  long long q, r;
+};
+__device__ __forceinline__ Divided divide(long long x, long long y) {
+  if (((x | y) >> 32) != 0) return {x / y, x % y};
+  const uint32_t a = static_cast<uint32_t>(x), b = static_cast<uint32_t>(y), q = a / b;
+  return {q, a - q * b};
+}
+
+// Sequences of a list that a CTA looks at together, in shared memory: where each begins in units of cost, and in steps.
+struct Listed {
+  long long start, steps;
+  PagedSeq s;
+};
+// Of `count` (up to 512, a multiple of 32) the last that begins at x or before it. The lanes of a warp look together.
+__device__ __forceinline__ int find_listed(const Listed* list, int count, long long x) {
+  const int lane = threadIdx.x & 31, per = count / 32;
+  const int block = __popc(__ballot_sync(kAllLanes, list[lane * per].start <= x)) - 1;
+  return block * per + __popc(__ballot_sync(kAllLanes, lane < per && list[block * per + min(lane, per - 1)].start <= x)) - 1;
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

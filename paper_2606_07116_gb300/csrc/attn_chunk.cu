@@ -21,8 +21,8 @@
 // far is rescaled before that. Little is held in registers on purpose: spilled registers miss the L1 that 200 KB of shared
 // memory leave (four reloads in a row cost more than the products of a block).
 //
-// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warp 9 finds the CTA's work, warps
-// 12-15 widen.
+// Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warps 12-15 widen; all find the
+// CTA's work before that.
 //
 // Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 599 us, 805 TFLOP/s; 16 sequences of
 // 8 tokens over 500 to 6000 122 us. What bounds it: with softmax, widening and reads left out the products take 341 us, since S has
@@ -45,15 +45,24 @@ constexpr float kMostLog2 = 14.f;
 constexpr int kSoftmaxRegs = 144, kIssueRegs = 96, kWidenRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kWidenRegs <= 4 * 128, "register shares");
 
-struct PartHead {  // a part that crosses CTAs: sequence (negative: none), head, row pair tile, whether it is its last
-  int b, h, p, ends;
+// A part that crosses CTAs: sequence (negative: none), head, row pair tile, whether it is its last; the sequence's first query
+// row and its rows.
+struct alignas(16) PartHead {
+  int b, h, p, ends, first, rows, unused[2];
+};
+
+// What sequences cost, in blocks: with what its tiles cost besides, and without.
+struct Cost {
+  long long all, blocks;
 };
 
 struct ChunkCtrl {
   uint64_t q_full[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_ready[2], done;
   uint32_t tmem;
   int abort;
-  int b, h, p, blk, count;
+  int b, h, p, blk;     // the CTA's first step
+  PagedSeq seq;         // and its sequence
+  long long from, to;   // blocks of the list before the CTA's share, and up to its end
   alignas(16) float smax[2][4];        // the widening warps' largest value scales (read 16 bytes at a time)
   alignas(16) uint8_t missing[2][16];  // per 8 keys of the block: no page (the same)
 };
@@ -70,7 +79,7 @@ struct ChunkLayout {
   static constexpr int kCtrl = kSums + 1024;
   static constexpr int kBytes = kCtrl + 512 + 1024;         // alignment to 1024
   static constexpr int64_t kPartFloats = kPairRows * (D + 2);
-  static_assert(kCtrl % 16 == 0 && sizeof(ChunkCtrl) <= 512 && kBytes <= 232448, "shared memory");
+  static_assert(kCtrl % 16 == 0 && sizeof(ChunkCtrl) <= 512 && 2 * (kThreads / 32) * sizeof(Cost) <= 1024 && kBytes <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ PartHead* part_heads(void* ws, int cta) { return static_cast<PartHead*>(ws) + 2 * cta; }
@@ -111,7 +120,7 @@ struct Walk {
     h = c->h;
     p = c->p;
     blk = c->blk;
-    s = paged_seq<M>(a, b);
+    s = c->seq;
     tiles = tiles_of(a, s);
     blocks = tile_blocks<M>(a, s, p);
   }
@@ -146,8 +155,8 @@ __device__ __forceinline__ float4 lds128f(const float4* p) {
 
 // Where row `row` of a (sequence, key head) goes.
 template <int D, typename T>
-__device__ __forceinline__ T* out_row(const AttnArgs& a, const PagedSeq& s, int h, int row) {
-  return static_cast<T*>(a.out) + (static_cast<int64_t>(s.first) + row / a.G) * a.ld_out +
+__device__ __forceinline__ T* out_row(const AttnArgs& a, int first, int h, int row) {
+  return static_cast<T*>(a.out) + (static_cast<int64_t>(first) + row / a.G) * a.ld_out +
          static_cast<int64_t>(h * a.G + row % a.G) * D;
 }
 // The four lanes c of a row hold its channels 8 k + c and 8 k + c + 4 in (x, y); each writes channels 8 k + 2 c and the
@@ -186,7 +195,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
     }
     mbar_init(smem_u32(&ctrl->done), 1);
     ctrl->abort = 0;
-    ctrl->count = 0;
     mbar_fence_init();
   }
   if (warp == 8) {
@@ -197,43 +205,74 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   griddep_launch_dependents();
   __syncthreads();
   PartHead* heads = part_heads(a.workspace, blockIdx.x);
-  if (warp == 9) {
-    struct Cost {  // of one head of a sequence, in blocks: with what its tiles cost besides, and without
-      long long all, blocks;
-    };
-    auto cost = [&](int b, PagedSeq& s) {
-      s = paged_seq<M>(a, b);
+  // The list of steps and this CTA's share of it. Some threads a sequence add up its tiles; they keep their first sequence, as
+  // most lists are no longer than the CTA.
+  {
+    constexpr int kWarps = kThreads / 32;
+    Cost* scan = reinterpret_cast<Cost*>(smem + L::kSums);      // [2][kWarps]: the queries' sums come there later
+    Listed* list = reinterpret_cast<Listed*>(smem);             // and the tiles here
+    static_assert(kThreads * sizeof(Listed) <= L::kSums, "the list fits");
+    const int B = listed<M>(a);
+    int team = 1;  // threads of a sequence
+    while (team < 32 && 2 * team * B <= kThreads) team *= 2;
+    const int place = tid / team, at_once = kThreads / team;
+    auto cost = [&](const PagedSeq& s) {  // of all heads
       Cost n = {0, 0};
-      for (int p = 0, tiles = tiles_of(a, s); p < tiles; ++p) n.blocks += tile_blocks<M>(a, s, p);
-      n.all = n.blocks + static_cast<long long>(kTileCost<M>) * tiles_of(a, s);
+      const int tiles = tiles_of(a, s);
+      if (M == kShared && s.at == s.len) {  // a prefix's tiles are alike
+        if (tiles > 0 && tid % team == 0) n.blocks = static_cast<long long>(tiles) * tile_blocks<M>(a, s, 0);
+      } else {
+        for (int p = tid % team; p < tiles; p += team) n.blocks += tile_blocks<M>(a, s, p);
+      }
+      for (int m = 1; m < team; m <<= 1) n.blocks += __shfl_xor_sync(kAllLanes, n.blocks, m);
+      n.all = (n.blocks + static_cast<long long>(kTileCost<M>) * tiles) * a.H;
+      n.blocks *= a.H;
       return n;
     };
-    auto warp_sum = [&](long long v) {
-#pragma unroll
-      for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(kAllLanes, v, m);
-      return v;
-    };
-    Cost sum = {0, 0};
-    const int B = listed<M>(a);
-    for (int b = lane; b < B; b += 32) {
-      PagedSeq s;
-      const Cost n = cost(b, s);
-      sum.all += n.all * a.H;
-      sum.blocks += n.blocks * a.H;
+    PagedSeq own = {};
+    Cost mine = {0, 0}, n = {0, 0};
+    for (int first = 0; first < B; first += at_once) {
+      PagedSeq s = {};
+      if (first + place < B) s = paged_seq<M>(a, first + place);
       if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+      Cost c = cost(s);
+      if (tid % team != 0) c = {0, 0};
+      if (first == 0) {
+        own = s;
+        n = c;
+      }
+      mine.all += c.all;
+      mine.blocks += c.blocks;
     }
-    const long long total = warp_sum(sum.all), all_blocks = warp_sum(sum.blocks);
-    const long long ctas = min(total, static_cast<long long>(gridDim.x));
-    const long long lo = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
-    const long long hi = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
-    // Both ends as numbers of blocks before them; the first as a place too.
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) {
+      mine.all += __shfl_xor_sync(kAllLanes, mine.all, m);
+      mine.blocks += __shfl_xor_sync(kAllLanes, mine.blocks, m);
+    }
+    if (lane == 0) scan[warp] = mine;
+    __syncthreads();
+    Cost total = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      total.all += scan[i].all;
+      total.blocks += scan[i].blocks;
+    }
+    const int ctas = static_cast<int>(min(total.all, static_cast<long long>(gridDim.x))), cta = blockIdx.x;
+    const long long lo = cta < ctas ? divide(total.all * cta, ctas).q : 0;
+    const long long hi = cta < ctas ? divide(total.all * (cta + 1), ctas).q : 0;
+    if (tid == 0) {
+      ctrl->from = 0;
+      ctrl->to = lo < hi ? total.blocks : 0;
+    }
     Cost before = {0, 0};
-    long long from = 0, to = lo < hi && hi == total ? all_blocks : 0;
-    for (int first = 0; first < B && before.all <= hi && lo < hi; first += 32) {
-      PagedSeq s;
-      Cost one = {0, 0};
-      if (first + lane < B) one = cost(first + lane, s);
-      Cost incl = {one.all * a.H, one.blocks * a.H};
+    for (int first = 0; first < B && before.all <= hi && lo < hi; first += at_once) {
+      if (first > 0) {
+        own = {};
+        if (first + place < B) own = paged_seq<M>(a, first + place);
+        n = cost(own);
+        if (tid % team != 0) n = {0, 0};
+      }
+      Cost incl = n;
 #pragma unroll
       for (int m = 1; m < 32; m <<= 1) {
         const long long x = __shfl_up_sync(kAllLanes, incl.all, m), y = __shfl_up_sync(kAllLanes, incl.blocks, m);
@@ -242,43 +281,80 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           incl.blocks += y;
         }
       }
-      const long long end = before.all + incl.all, start = end - one.all * a.H;
-      const long long blocks = before.blocks + incl.blocks - one.blocks * a.H;
-#pragma unroll 1
-      for (int which = 0; which < 2; ++which) {
-        const long long x = which ? hi : lo;
-        if (x < start || x >= end) continue;
-        const long long h = (x - start) / one.all;
-        long long at = (x - start) % one.all, passed = blocks + h * one.blocks;
-        int p = 0;
-        for (int n = tile_blocks<M>(a, s, 0); at >= n + kTileCost<M>; n = tile_blocks<M>(a, s, ++p)) {
-          at -= n + kTileCost<M>;
-          passed += n;
+      if (lane == 31) scan[kWarps + warp] = incl;
+      __syncthreads();
+      Cost chunk = {0, 0};
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        if (i == warp) {
+          incl.all += chunk.all;
+          incl.blocks += chunk.blocks;
         }
-        at = max(0LL, at - kTileCost<M>);
-        if (which) {
-          to = passed + at;
+        chunk.all += scan[kWarps + i].all;
+        chunk.blocks += scan[kWarps + i].blocks;
+      }
+      list[tid] = Listed{before.all + incl.all - n.all, before.blocks + incl.blocks - n.blocks, own};
+      __syncthreads();
+      const long long x = warp == 0 ? lo : hi;
+      if (warp < 2 && x >= before.all && x < before.all + chunk.all) {  // a warp finds an end
+        // A team's other threads cost nothing and begin where the next team does, which is found then.
+        const int at = find_listed(list, kThreads, x);
+        const Listed found = list[at];
+        const int tiles = tiles_of(a, found.s);
+        const Cost next = at + team < kThreads ? Cost{list[at + team].start, list[at + team].steps}
+                                               : Cost{before.all + chunk.all, before.blocks + chunk.blocks};
+        const long long one = divide(next.all - found.start, a.H).q, blocks = divide(next.blocks - found.steps, a.H).q;
+        const Divided in = divide(x - found.start, one);
+        long long passed = found.steps + in.q * blocks, rest = in.r;
+        int p = 0;
+        if (M == kShared && found.s.at == found.s.len) {
+          const int each = tile_blocks<M>(a, found.s, 0);
+          const Divided tile = divide(rest, each + kTileCost<M>);
+          p = static_cast<int>(tile.q);
+          rest = tile.r;
+          passed += tile.q * each;
         } else {
-          from = passed + at;
-          ctrl->b = first + lane;
-          ctrl->h = static_cast<int>(h);
-          ctrl->p = p;
-          ctrl->blk = static_cast<int>(at);
+          for (int p0 = 0; p0 < tiles; p0 += 32) {  // 32 tiles at a time
+            const int each = p0 + lane < tiles ? tile_blocks<M>(a, found.s, p0 + lane) + kTileCost<M> : 0;
+            long long sum = each;
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) {
+              const long long y = __shfl_up_sync(kAllLanes, sum, m);
+              if (lane >= m) sum += y;
+            }
+            const uint32_t past = __ballot_sync(kAllLanes, sum > rest);
+            const int stop = past != 0 ? __ffs(past) - 1 : 31;
+            const long long sums = __shfl_sync(kAllLanes, sum - (past != 0 ? each : 0), stop);  // of the tiles passed
+            const int passes = past != 0 ? stop : min(32, tiles - p0);
+            passed += sums - static_cast<long long>(passes) * kTileCost<M>;
+            rest -= sums;
+            p = p0 + passes;
+            if (past != 0) break;
+          }
+        }
+        rest = max(0LL, rest - kTileCost<M>);
+        if (lane == 0) {
+          (warp == 0 ? ctrl->from : ctrl->to) = passed + rest;
+          if (warp == 0) {
+            ctrl->b = first + at / team;
+            ctrl->seq = found.s;
+            ctrl->h = static_cast<int>(in.q);
+            ctrl->p = p;
+            ctrl->blk = static_cast<int>(rest);
+          }
         }
       }
-      before.all += __shfl_sync(kAllLanes, incl.all, 31);
-      before.blocks += __shfl_sync(kAllLanes, incl.blocks, 31);
+      before.all += chunk.all;
+      before.blocks += chunk.blocks;
+      __syncthreads();
     }
-    from = warp_sum(from);  // one lane's each
-    to = hi == total ? to : warp_sum(to);
-    if (lane == 0) ctrl->count = static_cast<int>(to - from);
-    if (lane < 2) heads[lane] = PartHead{-1, 0, 0, 0};
+    if (tid < 2) heads[tid] = PartHead{-1};
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctrl->tmem;
-  const int count = ctrl->count;
+  const int count = static_cast<int>(ctrl->to - ctrl->from);  // blocks
   auto wait = [&](uint64_t* bar, int phase) {  // the warp goes on together
     return __all_sync(kAllLanes, mbar_wait(smem_u32(bar), phase & 1, abort));
   };
@@ -509,15 +585,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
         if (active && !live && lane == 0) mbar_arrive(smem_u32(&ctrl->q_full[i]));
         if (live) {
           // This warp's query rows, in the widened channel order, and their sums.
-          constexpr int kCh = D / 8, kPer = 32 / kCh;
+          constexpr int kCh = D / 8, kPer = 32 / kCh, kFlight = 8;
           const int ch = lane % kCh, r0 = lane / kCh, dt = kPer / a.G, dg = kPer % a.G;
           int token = (row0 + r0) / a.G, gh = (row0 + r0) % a.G;
           const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>(w.s.first) * a.ld_q + static_cast<int64_t>(w.h) * a.G * D + ch * 8;
 #pragma unroll 1
-          for (int it0 = 0; it0 < kCh; it0 += 8) {  // eight rows' reads in flight
-            uint4 u[8];
+          for (int it0 = 0; it0 < kCh; it0 += kFlight) {  // that many reads of a lane in flight
+            uint4 u[kFlight];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kFlight; ++k) {
               u[k] = make_uint4(0u, 0u, 0u, 0u);
               if (row0 + (it0 + k) * kPer + r0 < rows)
                 u[k] = __ldg(reinterpret_cast<const uint4*>(src + token * a.ld_q + gh * D));
@@ -529,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
               }
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kFlight; ++k) {
               const int r = (it0 + k) * kPer + r0;
               sts128(base + i * L::kTileBytes + tile_off(quad * 32 + r, ch), __byte_perm(u[k].x, u[k].z, 0x5410),
                      __byte_perm(u[k].x, u[k].z, 0x7632), __byte_perm(u[k].y, u[k].w, 0x5410), __byte_perm(u[k].y, u[k].w, 0x7632));
@@ -770,7 +846,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             if constexpr (M == kShared)
               to[x] = row0 + r < rows ? shared_sums<D>(a, w.b, w.s.first, w.h, row0 + r) : nullptr;
             else
-              to[x] = row0 + r < rows ? out_row<D, T>(a, w.s, w.h, row0 + r) : nullptr;
+              to[x] = row0 + r < rows ? out_row<D, T>(a, w.s.first, w.h, row0 + r) : nullptr;
             if (c == 0) {
               if (!complete) {
                 part[i * kQt + quad * 32 + r] = m[x];
@@ -813,7 +889,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
             __syncwarp();
           }
           if (!complete && i == 0 && warp == 0 && lane == 0)
-            heads[which] = PartHead{w.b, w.h, w.p, w.blk + nb == w.blocks};
+            heads[which] = PartHead{w.b, w.h, w.p, w.blk + nb == w.blocks, w.s.first, rows};
           tc_fence_before();
         }
         left -= nb;
@@ -840,19 +916,24 @@ __global__ void __launch_bounds__(2 * D) join_chunks_kernel(const AttnArgs a, in
   if (tid == 0) s_last = 0x7FFFFFFF;
   griddep_wait();
   griddep_launch_dependents();
+  const int warp = blockIdx.y;
   const PartHead p = part_heads(a.workspace, cta)[1];
-  if (p.b < 0) return;
+  PartHead n = {-1};  // with it the first parts of all CTAs after it
+  if (cta + 1 + tid < ctas) n = part_heads(a.workspace, cta + 1 + tid)[0];
+  const int row0 = p.p * kPairRows + warp * 32;
+  if (p.b < 0 || row0 >= p.rows) return;
   __syncthreads();
-  for (int k = cta + 1 + tid; k < ctas; k += blockDim.x) {
-    const PartHead n = part_heads(a.workspace, k)[0];
+  auto ends = [&](int k) {
     if (n.b == p.b && n.h == p.h && n.p == p.p && n.ends) atomicMin(&s_last, k);
+  };
+  ends(cta + 1 + tid);
+  for (int k = cta + 1 + tid + blockDim.x; k < ctas; k += blockDim.x) {
+    n = part_heads(a.workspace, k)[0];
+    ends(k);
   }
   __syncthreads();
   const int last = s_last;
   if (last >= ctas) return;  // a CTA gave up: the status word says so
-  const PagedSeq s = paged_seq<M>(a, p.b);
-  const int rows = s.n * a.G, warp = blockIdx.y, row0 = p.p * kPairRows + warp * 32;
-  if (row0 >= rows) return;
   constexpr int kReps = 2;  // of 8 channels, per warp
   constexpr int kAtOnce = 4;
   float top[4], sum[4];
@@ -915,18 +996,18 @@ __global__ void __launch_bounds__(2 * D) join_chunks_kernel(const AttnArgs a, in
     for (int ii = 0; ii < 2; ++ii) {
       const int x = 2 * hh + ii, r = row0 + 8 * x + g;
       if constexpr (M == kShared) {
-        float* to = r < rows ? shared_sums<D>(a, p.b, s.first, p.h, r) : nullptr;
+        float* to = r < p.rows ? shared_sums<D>(a, p.b, p.first, p.h, r) : nullptr;
         const float4 u = acc[hh][0], v = acc[hh][1];
         write_sums(to, q, lane, ii ? u.z : u.x, ii ? u.w : u.y, ii ? v.z : v.x, ii ? v.w : v.y);
-        if (q == 0 && c == 0 && r < rows) write_stats(a, p.b, s.first, p.h, r, top[x], sum[x]);
+        if (q == 0 && c == 0 && r < p.rows) write_stats(a, p.b, p.first, p.h, r, top[x], sum[x]);
         continue;
       }
       const float inv = sum[x] > 0.f ? __fdividef(1.f, sum[x]) : 0.f;
-      T* to = r < rows ? out_row<D, T>(a, s, p.h, r) : nullptr;
+      T* to = r < p.rows ? out_row<D, T>(a, p.first, p.h, r) : nullptr;
 #pragma unroll
       for (int k = 0; k < kReps; ++k)
         write_pair<T>(to, q * kReps + k, lane, (ii ? acc[hh][k].z : acc[hh][k].x) * inv, (ii ? acc[hh][k].w : acc[hh][k].y) * inv);
-      if (q == 0 && c == 0 && r < rows) write_lse(a, s.first, p.h, r, top[x], sum[x]);
+      if (q == 0 && c == 0 && r < p.rows) write_lse(a, p.first, p.h, r, top[x], sum[x]);
     }
 }
 

@@ -42,6 +42,9 @@ using namespace offq;
 constexpr int kTile = 32;   // tokens per stage
 constexpr float kBias = 24.0f;
 constexpr int kLeastStages = 8;   // of a CTA
+// What a unit costs a warp besides its stages (queries, the output), in stages.
+template <AttnMode M>
+constexpr int kUnitCost = M == kCausal ? 0 : 2;
 
 template <int D, int NT>
 struct FewLayout {
@@ -60,13 +63,17 @@ struct FewLayout {
   static_assert(kBytes <= 232448, "shared memory");
 };
 
+// What sequences cost, in stages: with what their units cost besides, and without.
+struct Cost {
+  long long all, stages;
+};
+
 // Control block behind the parts.
 template <int D, int NT>
 struct FewCtrl {
-  long long scan[FewLayout<D, NT>::kWarps];
-  long long start[FewLayout<D, NT>::kWarps];  // unit offset inside sequence seq
-  int seq[FewLayout<D, NT>::kWarps];
-  int4 part[2 * FewLayout<D, NT>::kWarps];    // (sequence or -1, head, first stage, last stage) of each part
+  Cost scan[2][FewLayout<D, NT>::kWarps];
+  int4 part[2 * FewLayout<D, NT>::kWarps];    // (sequence or -1, unit in it, first stage, last stage) of each part
+  int2 rows[2 * FewLayout<D, NT>::kWarps];    // first query row of its sequence, rows of the unit
 };
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool half) {
@@ -223,76 +230,118 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   griddep_wait();
   griddep_launch_dependents();
 
-  // The whole work, this CTA's share and its warps' places in it.
-  long long mine = 0;
+  // The whole work, this CTA's share and its warps' places in it. A thread keeps its first sequence, as most lists are no
+  // longer than the CTA.
   const int B = listed<M>(a);
+  auto cost = [&](const PagedSeq& s) {
+    const int stages = stages_of(a, s);
+    const long long units = stages > 0 ? static_cast<long long>(a.H) * groups_of<M, L::kRows>(a, s) : 0;
+    return Cost{units * (stages + kUnitCost<M>), units * stages};
+  };
+  PagedSeq own = {};
+  Cost mine = {0, 0}, n = {0, 0};
   for (int b = tid; b < B; b += kThreads) {
     const PagedSeq s = few_seq<M>(a, b);
     if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-    mine += static_cast<long long>(stages_of(a, s)) * a.H * groups_of<M, L::kRows>(a, s);
+    const Cost x = cost(s);
+    if (b == tid) {
+      own = s;
+      n = x;
+    }
+    mine.all += x.all;
+    mine.stages += x.stages;
   }
-  auto warp_sum = [&](long long v) {
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) v += __shfl_xor_sync(kAllLanes, v, m);
-    return v;
-  };
-  const long long wsum = warp_sum(mine);
-  if (lane == 0) ctrl->scan[warp] = wsum;
+  for (int m = 16; m > 0; m >>= 1) {
+    mine.all += __shfl_xor_sync(kAllLanes, mine.all, m);
+    mine.stages += __shfl_xor_sync(kAllLanes, mine.stages, m);
+  }
+  if (lane == 0) ctrl->scan[0][warp] = mine;
   __syncthreads();
-  long long total = 0;
+  Cost total = {0, 0};
 #pragma unroll
-  for (int i = 0; i < L::kWarps; ++i) total += ctrl->scan[i];
+  for (int i = 0; i < L::kWarps; ++i) {
+    total.all += ctrl->scan[0][i].all;
+    total.stages += ctrl->scan[0][i].stages;
+  }
   // Little work goes to fewer CTAs, some stages each: their warps take them at once, and joining inside a CTA is cheaper.
-  const long long ctas = min((total + kLeastStages - 1) / kLeastStages, static_cast<long long>(gridDim.x));
-  const long long lo = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
-  const long long hi = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
+  const int ctas = static_cast<int>(min((total.all + kLeastStages - 1) / kLeastStages, static_cast<long long>(gridDim.x)));
+  const int cta = blockIdx.x;
+  const long long lo = cta < ctas ? divide(total.all * cta, ctas).q : 0;
+  const long long hi = cta < ctas ? divide(total.all * (cta + 1), ctas).q : 0;
   PartHead* heads = part_head<D, NT>(a.workspace, blockIdx.x, 0);
   if (lo == hi) {
     if (tid < 2) heads[tid] = PartHead{-1, 0, 0, 0};
     return;
   }
-  long long before = 0;
-  for (int base = 0; base < B && before < hi; base += kThreads) {
-    long long val = 0;
-    if (base + tid < B) {
-      const PagedSeq s = few_seq<M>(a, base + tid);
-      val = static_cast<long long>(stages_of(a, s)) * a.H * groups_of<M, L::kRows>(a, s);
-    }
-    long long incl = val;
-#pragma unroll
-    for (int m = 1; m < 32; m <<= 1) {
-      const long long o = __shfl_up_sync(kAllLanes, incl, m);
-      if (lane >= m) incl += o;
-    }
-    __syncthreads();
-    if (lane == 31) ctrl->scan[warp] = incl;
-    __syncthreads();
-    long long chunk = 0;
-#pragma unroll
-    for (int i = 0; i < L::kWarps; ++i) {
-      if (i < warp) incl += ctrl->scan[i];
-      chunk += ctrl->scan[i];
-    }
-    const long long first = before + incl - val;
-#pragma unroll 1
-    for (int k = 0; k < L::kWarps; ++k) {
-      const long long at = lo + (hi - lo) * k / L::kWarps;
-      if (at >= first && at < first + val) {
-        ctrl->seq[k] = base + tid;
-        ctrl->start[k] = at - first;
+  const long long w0 = lo + (hi - lo) * warp / L::kWarps, w1 = lo + (hi - lo) * (warp + 1) / L::kWarps;
+  Listed* list = reinterpret_cast<Listed*>(smem);  // where the rings will be
+  static_assert(kThreads * sizeof(Listed) <= L::kPartOff, "the list fits");
+  int b0 = 0, unit0 = 0, t0 = 0;  // of this warp's first stage: sequence, unit in it, stage
+  PagedSeq s0 = {};
+  long long from = 0, to = total.stages;  // stages before it, and up to the warp's end
+  Cost before = {0, 0};
+  for (int base = 0; base < B && before.all <= hi; base += kThreads) {
+    if (base > 0) {
+      n = {0, 0};
+      if (base + tid < B) {
+        own = few_seq<M>(a, base + tid);
+        n = cost(own);
       }
     }
-    before += chunk;
+    Cost incl = n;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const long long x = __shfl_up_sync(kAllLanes, incl.all, m), y = __shfl_up_sync(kAllLanes, incl.stages, m);
+      if (lane >= m) {
+        incl.all += x;
+        incl.stages += y;
+      }
+    }
+    if (lane == 31) ctrl->scan[1][warp] = incl;
+    __syncthreads();
+    Cost chunk = {0, 0};
+#pragma unroll
+    for (int i = 0; i < L::kWarps; ++i) {
+      if (i == warp) {
+        incl.all += chunk.all;
+        incl.stages += chunk.stages;
+      }
+      chunk.all += ctrl->scan[1][i].all;
+      chunk.stages += ctrl->scan[1][i].stages;
+    }
+    list[tid] = Listed{before.all + incl.all - n.all, before.stages + incl.stages - n.stages, own};
+    __syncthreads();
+#pragma unroll 1
+    for (int end = 0; end < 2; ++end) {
+      const long long x = end ? w1 : w0;
+      if (x < before.all || x >= before.all + chunk.all) continue;
+      const int at = find_listed(list, kThreads, x);
+      const Listed found = list[at];
+      const int stages = stages_of(a, found.s);
+      const Divided in = divide(x - found.start, stages + kUnitCost<M>);
+      const int t = max(0, static_cast<int>(in.r) - kUnitCost<M>);
+      const long long passed = found.steps + in.q * stages + t;
+      if (end) {
+        to = passed;
+      } else {
+        from = passed;
+        b0 = base + at;
+        s0 = found.s;
+        unit0 = static_cast<int>(in.q);
+        t0 = t;
+      }
+    }
+    before.all += chunk.all;
+    before.stages += chunk.stages;
+    __syncthreads();
   }
-  __syncthreads();
 
-  const long long w0 = lo + (hi - lo) * warp / L::kWarps, w1 = lo + (hi - lo) * (warp + 1) / L::kWarps;
-  int todo = static_cast<int>(w1 - w0), ahead = todo;  // stages to compute, to issue
+  int todo = static_cast<int>(to - from), ahead = todo;  // stages to compute, to issue
   if (todo > 0) {
-    int b = ctrl->seq[warp];
-    PagedSeq s = few_seq<M>(a, b);
+    int b = b0, h = unit0, t = t0;
+    PagedSeq s = s0;
     int stages = stages_of(a, s);
-    int h = static_cast<int>(ctrl->start[warp] / stages), t = static_cast<int>(ctrl->start[warp] % stages);
     int row0 = 0, pgroup = 0, pgroups = 1;  // this unit's first row; where the copies are
     if constexpr (M == kShared) {
       pgroup = h / a.H;
@@ -632,7 +681,10 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
           }
         }
       }
-      if (!complete && lane == 0) ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, M == kShared ? row0 / L::kRows * a.H + h : h, t_first, t == stages ? -1 : t);
+      if (!complete && lane == 0) {
+        ctrl->rows[2 * warp + (first_part ? 0 : 1)] = make_int2(s.first, rows);
+        ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, M == kShared ? row0 / L::kRows * a.H + h : h, t_first, t == stages ? -1 : t);
+      }
       first_part = false;
       begin = true;
       if (it + 1 < todo) {
@@ -657,30 +709,33 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     }
   }
 
-  // Parts of the same head, in order of their stages, into one: an output where they are all of it, else a part
-  // for the joining kernel. Each warp looks at all of them at once, a lane a part.
+  // Parts of the same unit, in order of their stages, into one: an output where they are all of it, else a part
+  // for the joining kernel. Each warp looks at all of them at once, a lane a part, and joins its share of the units (some
+  // warps a unit where units are few): by all warps one after the other they took up to 10 us.
   __syncthreads();
   constexpr int kParts = 2 * L::kWarps;
   static_assert(kParts <= 32, "a lane for each part");
   const int4 mypart = lane < kParts ? ctrl->part[lane] : make_int4(-1, 0, 0, 0);
   const int my_id = mypart.x < 0 ? -1 : unit_id<M>(a, mypart.x, mypart.y);
-  uint32_t left = __ballot_sync(kAllLanes, my_id >= 0);
+  const uint32_t same_id = __match_any_sync(kAllLanes, my_id);
+  uint32_t left = __ballot_sync(kAllLanes, my_id >= 0 && __ffs(same_id) - 1 == lane);  // the first part of each unit
+  const int slices = max(1, min(L::kRows * (D / 8) / 32, L::kWarps / max(1, __popc(left))));
   bool have0 = false, have1 = false;
-  while (left != 0) {
+  for (int turn = warp / slices; left != 0; left &= left - 1, turn = turn == 0 ? L::kWarps / slices - 1 : turn - 1) {
     const int i = __ffs(left) - 1;
     const int id = __shfl_sync(kAllLanes, my_id, i);
-    const Unit unit = unit_at<M, L::kRows>(a, id);
-    const uint32_t same = __ballot_sync(kAllLanes, my_id == id);
+    const uint32_t same = __shfl_sync(kAllLanes, same_id, i);
     const int begins = __shfl_sync(kAllLanes, mypart.z, i), last = __shfl_sync(kAllLanes, mypart.w, 31 - __clz(same));
-    left &= ~same;
     const bool complete = begins == 0 && last < 0;
     const int which = begins == 0 ? 1 : 0;
-    float* dst = part_sums<D, NT>(a.workspace, gridDim.x, blockIdx.x, which);
-    const PagedSeq s = paged_seq<M>(a, unit.b);
-    const int rows = min(s.n * a.G - unit.row0, L::kRows);
     if (!complete) (which ? have1 : have0) = true;
-    if (!complete && tid == 0) heads[which] = PartHead{id, last < 0, s.first, rows};
-    for (int u = tid; u < L::kRows * (D / 8); u += kThreads) {
+    if (turn != 0 || warp / slices >= L::kWarps / slices) continue;
+    const Unit unit = unit_at<M, L::kRows>(a, id);
+    float* dst = part_sums<D, NT>(a.workspace, gridDim.x, blockIdx.x, which);
+    const int first = ctrl->rows[i].x, rows = ctrl->rows[i].y;
+    const int slice = warp % slices;
+    if (!complete && slice == 0 && lane == 0) heads[which] = PartHead{id, last < 0, first, rows};
+    for (int u = slice * 32 + lane; u < L::kRows * (D / 8); u += slices * 32) {
       const int r = u / (D / 8), d = u % (D / 8) * 8;
       float top = -INFINITY, sum = 0.f, v[8] = {};
       for (uint32_t rest = same; rest != 0; rest &= rest - 1) {
@@ -699,8 +754,8 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
           const float inv = M == kShared ? 1.f : sum > 0.f ? __fdividef(1.f, sum) : 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= inv;
-          write_row8<D, T, M>(a, unit.b, s.first, unit.h, unit.row0 + r, d, v);
-          if (d == 0) write_row_stats<M>(a, unit.b, s.first, unit.h, unit.row0 + r, top, sum);
+          write_row8<D, T, M>(a, unit.b, first, unit.h, unit.row0 + r, d, v);
+          if (d == 0) write_row_stats<M>(a, unit.b, first, unit.h, unit.row0 + r, top, sum);
         }
       } else {
         reinterpret_cast<float4*>(dst + r * D + d)[0] = make_float4(v[0], v[1], v[2], v[3]);
