@@ -74,6 +74,26 @@ struct PromptCtrl {
 };
 static_assert(sizeof(PromptCtrl) <= 512, "control block");
 
+// The lowest n bits.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1u; }
+
+// Word k of the four lanes c of a quad becomes word c of lane k.
+__device__ __forceinline__ void transpose_words(uint32_t (&w)[4], int c) {
+#pragma unroll
+  for (int step = 2; step > 0; step >>= 1) {
+    const bool high = (c & step) != 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = step == 2 ? i : 2 * i;  // words k and k + step change places between the lanes
+      const uint32_t got = __shfl_xor_sync(kAllLanes, high ? w[k] : w[k + step], step);
+      if (high)
+        w[k] = got;
+      else
+        w[k + step] = got;
+    }
+  }
+}
+
 // Queries of sequence b (its first row in `first`); none where its entries are out of range.
 __device__ __forceinline__ int prompt_seq(const AttnArgs& a, int b, int& first, bool& bad) {
   const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
@@ -143,6 +163,11 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
     tmem_alloc(smem_u32(&ctrl->tmem), 512);
     tmem_relinquish();
   }
+  if (warp == 9 && lane == 0) {
+    tma_prefetch_desc(&maps.q);
+    tma_prefetch_desc(&maps.k);
+    tma_prefetch_desc(&maps.v);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -154,7 +179,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
     return __all_sync(kAllLanes, mbar_wait(smem_u32(bar), phase & 1, abort));
   };
   // Item number k of this CTA, for the warps that work on it; false at the end.
-  int head[2], row0[2], blocks[2], most = 0;
+  int head[2], row0[2], blocks[2], most = 0;  // no block at all: the item has no rows
   Gap gap = {0, 0};  // keys that the item leaves out: the others are numbered without them
   Item item = {};
   auto next_item = [&](int k) {
@@ -162,14 +187,25 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
     item = ctrl->item;
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&ctrl->item_empty));
-    if constexpr (M == kWindowed) {
-      gap.cut = window_gap(a, 0, 8).cut;
-      gap.shift = max(0, window_from(a, item.token + 1) - gap.cut);
-    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       head[i] = two_heads ? 2 * item.unit + i : item.unit;
       row0[i] = item.token + (two_heads ? 0 : i * kQt);
+    }
+    if constexpr (M == kWindowed) {
+      // An odd number of heads per key head: 256 tokens are G items, two of 128 tokens for each pair of heads and one for the last
+      // head. Tiles of the same tokens see the same keys: their items have a block less under a short window.
+      const int of_kv = item.unit % a.G;
+      if (!two_heads && of_kv < a.G - 1) {
+        head[0] = item.unit - (of_kv & 1);
+        head[1] = head[0] + 1;
+        row0[0] = row0[1] = item.token + (of_kv & 1) * kQt;
+      }
+      gap.cut = window_gap(a, 0, 8).cut;
+      gap.shift = max(0, window_from(a, row0[0] + 1) - gap.cut);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       const int sees = (M == kWindowed || a.causal ? min(row0[i] + kQt, item.n) : item.n) - gap.shift;
       blocks[i] = row0[i] < item.n ? (sees + kKt - 1) / kKt : 0;
     }
@@ -181,8 +217,18 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
     fewer_registers<kOtherRegs>();
     if (warp == 10) {
       // ---- Items: level t of the list holds the t-th tile of every sequence that has one, the highest level first ----
+      // The lane's first sequence stays in registers: up to 32 of them are read once.
+      int first0 = 0;
+      bool bad0 = false;
+      const int n0 = lane < a.B ? prompt_seq(a, lane, first0, bad0) : 0;
       auto tiles_at = [&](int b, int& first, int& n, bool& bad) {
-        n = b < a.B ? prompt_seq(a, b, first, bad) : 0;
+        if (b < 32) {
+          first = first0;
+          n = n0;
+          bad = bad0;
+        } else {
+          n = b < a.B ? prompt_seq(a, b, first, bad) : 0;
+        }
         return (n + step - 1) / step;
       };
       int longest = 0;
@@ -302,19 +348,21 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
           if (it >= L::kSlots) ok = wait(&ctrl->empty[slot], it / L::kSlots - 1);
           if (!ok) break;
           const uint32_t dst = ring + slot * L::kTileBytes, bar = smem_u32(tail ? &ctrl->tail : &ctrl->full[slot]);
+          int key = u / 2 * kKt;
+          const bool both = M == kWindowed && gap.shift > 0 && key < gap.cut && key + kKt > gap.cut;
+          if (M == kWindowed && key >= gap.cut) key += gap.shift;
           if (lane == 0) {
             mbar_arrive_expect_tx(bar, L::kTileBytes);
-            int key = u / 2 * kKt;
-            const bool both = M == kWindowed && gap.shift > 0 && key < gap.cut && key + kKt > gap.cut;
-            if (M == kWindowed && key >= gap.cut) key += gap.shift;
-            if (!both) {
+            if (!both)
               for (int c = 0; c < D / 64; ++c)
                 tma_load_2d(dst + c * kAtom, is_v ? &maps.v : &maps.k, bar, kv_head * D + 64 * c, item.first + key);
-            } else {  // the last sinks and the first of the window, eight rows (1024 bytes of an atom) at a time
-              for (int r = 0; r < kKt; r += 8)
-                for (int c = 0; c < D / 64; ++c)
-                  tma_load_2d(dst + c * kAtom + r * 128, is_v ? &maps.v8 : &maps.k8, bar, kv_head * D + 64 * c,
-                              item.first + key + r + (key + r >= gap.cut ? gap.shift : 0));
+          }
+          if (both) {  // the last sinks and the first of the window, eight rows (1024 bytes of an atom) a lane
+            __syncwarp();
+            if (lane < kKt / 8 * (D / 64)) {
+              const int r = lane % (kKt / 8) * 8, c = lane / (kKt / 8);
+              tma_load_2d(dst + c * kAtom + r * 128, is_v ? &maps.v8 : &maps.k8, bar, kv_head * D + 64 * c,
+                          item.first + key + r + (key + r >= gap.cut ? gap.shift : 0));
             }
           }
           __syncwarp();
@@ -363,6 +411,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
       int it = 0, nq[2] = {0, 0}, np[2] = {0, 0};  // ring uses, query tiles, weights so far
       bool ok = true;
       for (int k = 0; ok && next_item(k); ++k) {
+        if (most == 0) continue;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           if (blocks[i] > 0 && ok) ok = wait(&ctrl->q_full[i], nq[i]++);
@@ -444,18 +493,18 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
         uint32_t s[kKt];
         tmem_ld_128cols(s_tm, s);
         if constexpr (M == kWindowed) {
-          if ((j + 1) * kKt > min(my_row0 + 1, n) - gap.shift) {
-            const int valid = min(upto, n - gap.shift) - j * kKt;
+          // Hidden: behind the row's last key, and between the sinks and the window. A bit for each of 32 keys, and only those 32
+          // are looked at of which some row of the warp hides one: a comparison for each key took as long as the softmax.
+          if ((j + 1) * kKt > min(my_row0 + 1, n) - gap.shift || (j * kKt < last_at && (j + 1) * kKt > a.sinks)) {
+            const int valid = min(upto, n - gap.shift) - j * kKt, open = window_at - j * kKt, kept = a.sinks - j * kKt;
 #pragma unroll
-            for (int e = 0; e < kKt; ++e)
-              if (e >= valid) s[e] = 0xFF800000u;  // -inf
-          }
-          if (j * kKt < last_at && (j + 1) * kKt > a.sinks) {  // behind the sinks, before the window
-            const int begin = max(0, a.sinks - j * kKt);
-            const uint32_t hidden = max(0, window_at - j * kKt - begin);
+            for (int q = 0; q < 4; ++q) {
+              const uint32_t hidden = ~first_bits(valid - 32 * q) | (first_bits(open - 32 * q) & ~first_bits(kept - 32 * q));
+              if (!__any_sync(kAllLanes, hidden != 0u)) continue;
 #pragma unroll
-            for (int e = 0; e < kKt; ++e)
-              if (static_cast<uint32_t>(e - begin) < hidden) s[e] = 0xFF800000u;
+              for (int e = 0; e < 32; ++e)
+                if (hidden >> e & 1u) s[32 * q + e] = 0xFF800000u;  // -inf
+            }
           }
         } else if ((j + 1) * kKt > (a.causal ? min(my_row0 + 1, n) : n)) {
           const int valid = (a.causal ? min(row + 1, n) : n) - j * kKt;
@@ -516,24 +565,28 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
       if (ok) ok = wait(&ctrl->o_full[i], no++);
       if (ok) {
         tc_fence_after();
+        // Outputs as fragments, four words of a row from four lanes: a lane then writes 16 bytes next to its neighbours' (64 bytes of
+        // a row). With a row a lane each store touched 32 lines, and an item's took 4 us.
         const float inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;
         const int64_t t = static_cast<int64_t>(item.first) + row;
+        const int g = lane >> 2, c = lane & 3, row_w = my_row0 + (warp & 3) * 32 + g;
+        T* dst = static_cast<T*>(a.out) + (static_cast<int64_t>(item.first) + row_w) * a.ld_out + static_cast<int64_t>(my_head) * D + 8 * c;
+        float scale_of[4];  // rows 8 x + g
+#pragma unroll
+        for (int x = 0; x < 4; ++x) scale_of[x] = __shfl_sync(kAllLanes, inv, 8 * x + g);
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
-          uint32_t o[32];
-          tmem_ld_32cols(o_tm + 32 * q, o);
-          tmem_ld_wait_for(o);
-          if (row < n) {
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out +
-                                                  static_cast<int64_t>(my_head) * D + 32 * q);
+          uint32_t o[2][16];
+          tmem_ld_fragments(o_tm + 32 * q, o[0], o[1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t w[4];
+          for (int x = 0; x < 4; ++x) {
+            uint32_t w[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                w[k] = pack_16<T>(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
-              dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            for (int k = 0; k < 4; ++k)
+              w[k] = pack_16<T>(__uint_as_float(o[x >> 1][4 * k + 2 * (x & 1)]) * scale_of[x],
+                                __uint_as_float(o[x >> 1][4 * k + 2 * (x & 1) + 1]) * scale_of[x]);
+            transpose_words(w, c);
+            if (row_w + 8 * x < n) *reinterpret_cast<uint4*>(dst + 8 * x * a.ld_out + 32 * q) = make_uint4(w[0], w[1], w[2], w[3]);
           }
           __syncwarp();
         }
