@@ -207,6 +207,23 @@ __device__ __forceinline__ void widen_signed(uint32_t w, uint32_t& even, uint32_
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(odd) : "r"(y), "r"(0x2C002C00u), "r"(0xD480D480u));  // / 16 - 72
 }
 
+// Word k of the four lanes c of a quad becomes word c of lane k.
+__device__ __forceinline__ void transpose_words(uint32_t (&w)[4], int c) {
+#pragma unroll
+  for (int step = 2; step > 0; step >>= 1) {
+    const bool high = (c & step) != 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = step == 2 ? i : 2 * i;  // words k and k + step change places between the lanes
+      const uint32_t got = __shfl_xor_sync(kAllLanes, high ? w[k] : w[k + step], step);
+      if (high)
+        w[k] = got;
+      else
+        w[k + step] = got;
+    }
+  }
+}
+
 // The log of a row's sum l of exponentials 2^(z - m), row r of (sequence starting at query row `first`, key head h).
 __device__ __forceinline__ void write_lse(const AttnArgs& a, int first, int h, int r, float m, float l) {
   if (a.lse == nullptr) return;

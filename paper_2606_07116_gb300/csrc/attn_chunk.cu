@@ -863,29 +863,44 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           for (int q = 0; q < D / 32; ++q) {
             uint32_t o[2][16];
             tmem_ld_fragments(o_tm + 32 * q, o[0], o[1]);
+            if (!complete) {
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh)
+              for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                float v[4], u[4];
+                for (int k = 0; k < 4; ++k) {
+                  float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(o[hh][4 * k + e]) + off[2 * hh + (e >> 1)];
-                if (!complete) {
+                  for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(o[hh][4 * k + e]) + off[2 * hh + (e >> 1)];
                   reinterpret_cast<float4*>(part + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + 4 * q + k) * 32 + lane] =
                       make_float4(v[0], v[1], v[2], v[3]);
-                } else if constexpr (M == kShared) {
-                  if ((k & 1) == 0) continue;
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) u[e] = __uint_as_float(o[hh][4 * k - 4 + e]) + off[2 * hh + (e >> 1)];
-#pragma unroll
-                  for (int ii = 0; ii < 2; ++ii)
-                    write_sums(to[2 * hh + ii], 2 * q + k / 2, lane, u[2 * ii], u[2 * ii + 1], v[2 * ii], v[2 * ii + 1]);
-                } else {
-#pragma unroll
-                  for (int ii = 0; ii < 2; ++ii)
-                    write_pair<T>(to[2 * hh + ii], 4 * q + k, lane, v[2 * ii] * inv[2 * hh + ii], v[2 * ii + 1] * inv[2 * hh + ii]);
                 }
-              }
+            } else {
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+                for (int ii = 0; ii < 2; ++ii) {  // row 32 quad + 8 x + g
+                  const int x = 2 * hh + ii;
+                  float v[4][2];
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) v[k][e] = __uint_as_float(o[hh][4 * k + 2 * ii + e]) + off[x];
+                  if constexpr (M == kShared) {
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2)
+                      write_sums(to[x], 2 * q + k / 2, lane, v[k][0], v[k][1], v[k + 1][0], v[k + 1][1]);
+                  } else {
+                    uint32_t u[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) u[k] = pack_16<T>(v[k][0] * inv[x], v[k][1] * inv[x]);
+                    transpose_words(u, c);  // this lane's: channels m and m + 4 of eight, m = 0 .. 3
+                    if (to[x] != nullptr)
+                      *reinterpret_cast<uint4*>(to[x] + 32 * q + 8 * c) =
+                          make_uint4(__byte_perm(u[0], u[1], 0x5410), __byte_perm(u[2], u[3], 0x5410),
+                                     __byte_perm(u[0], u[1], 0x7632), __byte_perm(u[2], u[3], 0x7632));
+                  }
+                }
+            }
             __syncwarp();
           }
           if (!complete && i == 0 && warp == 0 && lane == 0)
@@ -906,109 +921,120 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   }
 }
 
-// Row pair tiles that cross CTAs: begun at the end of CTA blockIdx.x, then the first parts of the CTAs after it up to
-// their last. Block y takes one softmax warp's 32 rows; a warp of it 16 channels. The reads of four parts are in flight
-// together: a part at a time they took most of this kernel's time (34 us where a tile has ten).
+// Row pair tiles that cross CTAs: begun at the end of one CTA, then the first parts of the CTAs after it up to their last. Two
+// blocks an SM share the tiles' eighths, one softmax warp's 32 rows each; a warp takes 16 channels of them. The reads of three
+// parts are in flight together. (Eight blocks for each CTA, most with nothing to do, kept those that had waiting: 12 us where 16
+// tiles have ten parts, 5 where none has any.)
 template <int D, typename T, AttnMode M>
-__global__ void __launch_bounds__(2 * D) join_chunks_kernel(const AttnArgs a, int ctas) {
-  __shared__ int s_last;
-  const int cta = blockIdx.x, tid = threadIdx.x, lane = tid & 31, q = tid >> 5, g = lane >> 2, c = lane & 3;
-  if (tid == 0) s_last = 0x7FFFFFFF;
+__global__ void __launch_bounds__(2 * D, 256 / D) join_chunks_kernel(const AttnArgs a, int ctas) {
+  constexpr int kMostListed = 1024;
+  __shared__ int s_begun[kMostListed], s_count, s_last;
+  const int tid = threadIdx.x, lane = tid & 31, q = tid >> 5, g = lane >> 2, c = lane & 3;
   griddep_wait();
   griddep_launch_dependents();
-  const int warp = blockIdx.y;
-  const PartHead p = part_heads(a.workspace, cta)[1];
-  PartHead n = {-1};  // with it the first parts of all CTAs after it
-  if (cta + 1 + tid < ctas) n = part_heads(a.workspace, cta + 1 + tid)[0];
-  const int row0 = p.p * kPairRows + warp * 32;
-  if (p.b < 0 || row0 >= p.rows) return;
-  __syncthreads();
-  auto ends = [&](int k) {
-    if (n.b == p.b && n.h == p.h && n.p == p.p && n.ends) atomicMin(&s_last, k);
-  };
-  ends(cta + 1 + tid);
-  for (int k = cta + 1 + tid + blockDim.x; k < ctas; k += blockDim.x) {
-    n = part_heads(a.workspace, k)[0];
-    ends(k);
+  if (q == 0) {  // the CTAs that left a part, in order
+    int count = 0;
+#pragma unroll 5
+    for (int base = 0; base < min(ctas, kMostListed); base += 32) {
+      const bool left = base + lane < ctas && part_heads(a.workspace, base + lane)[1].b >= 0;
+      const uint32_t mask = __ballot_sync(kAllLanes, left);
+      if (left) s_begun[count + __popc(mask & ((1u << lane) - 1u))] = base + lane;
+      count += __popc(mask);
+    }
+    if (lane == 0) s_count = count;
   }
   __syncthreads();
-  const int last = s_last;
-  if (last >= ctas) return;  // a CTA gave up: the status word says so
-  constexpr int kReps = 2;  // of 8 channels, per warp
-  constexpr int kAtOnce = 4;
-  float top[4], sum[4];
-  float4 acc[2][kReps];
+  auto join = [&](int cta, int warp) {
+    const PartHead p = part_heads(a.workspace, cta)[1];
+    const int row0 = p.p * kPairRows + warp * 32;
+    __syncthreads();
+    if (tid == 0) s_last = 0x7FFFFFFF;
+    __syncthreads();
+    for (int k = cta + 1 + tid; k < ctas; k += blockDim.x) {
+      const PartHead n = part_heads(a.workspace, k)[0];
+      if (n.b == p.b && n.h == p.h && n.p == p.p && n.ends) atomicMin(&s_last, k);
+    }
+    __syncthreads();
+    const int last = s_last;
+    if (last >= ctas) return;  // a CTA gave up: the status word says so
+    if (row0 >= p.rows) return;
+    constexpr int kReps = 2;  // of 8 channels, per warp
+    constexpr int kAtOnce = 3;
+    float top[4], sum[4];
+    float4 acc[2][kReps];
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    top[x] = -INFINITY;
-    sum[x] = 0.f;
-  }
+    for (int x = 0; x < 4; ++x) {
+      top[x] = -INFINITY;
+      sum[x] = 0.f;
+    }
 #pragma unroll
-  for (int hh = 0; hh < 2; ++hh)
+    for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-    for (int k = 0; k < kReps; ++k) acc[hh][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int part0 = cta; part0 <= last; part0 += kAtOnce) {
-    float mk[kAtOnce][4], lk[kAtOnce][4];
-    float4 v[kAtOnce][2][kReps];
+      for (int k = 0; k < kReps; ++k) acc[hh][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int part0 = cta; part0 <= last; part0 += kAtOnce) {
+      float mk[kAtOnce][4], lk[kAtOnce][4];
+      float4 v[kAtOnce][2][kReps];
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      if (part0 + j > last) continue;
-      const float* src = part_data<D>(a.workspace, ctas, part0 + j, part0 + j == cta ? 1 : 0);
+      for (int j = 0; j < kAtOnce; ++j) {
+        if (part0 + j > last) continue;
+        const float* src = part_data<D>(a.workspace, ctas, part0 + j, part0 + j == cta ? 1 : 0);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        mk[j][x] = src[warp * 32 + 8 * x + g];
-        lk[j][x] = src[kPairRows + warp * 32 + 8 * x + g];
+        for (int x = 0; x < 4; ++x) {
+          mk[j][x] = src[warp * 32 + 8 * x + g];
+          lk[j][x] = src[kPairRows + warp * 32 + 8 * x + g];
+        }
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int k = 0; k < kReps; ++k)
+            v[j][hh][k] = reinterpret_cast<const float4*>(src + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + q * kReps + k) * 32 + lane];
       }
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
+      for (int j = 0; j < kAtOnce; ++j) {
+        if (part0 + j > last) continue;
+        float x_old[4], x_new[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float next = fmaxf(top[x], mk[j][x]);
+          x_old[x] = top[x] == -INFINITY ? 0.f : ex2(top[x] - next);
+          x_new[x] = mk[j][x] == -INFINITY ? 0.f : ex2(mk[j][x] - next);
+          sum[x] = sum[x] * x_old[x] + lk[j][x] * x_new[x];
+          top[x] = next;
+        }
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int k = 0; k < kReps; ++k) {
+            const float4 n = v[j][hh][k];
+            float4& o = acc[hh][k];
+            o.x = o.x * x_old[2 * hh] + n.x * x_new[2 * hh];
+            o.y = o.y * x_old[2 * hh] + n.y * x_new[2 * hh];
+            o.z = o.z * x_old[2 * hh + 1] + n.z * x_new[2 * hh + 1];
+            o.w = o.w * x_old[2 * hh + 1] + n.w * x_new[2 * hh + 1];
+          }
+      }
+    }
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+      for (int ii = 0; ii < 2; ++ii) {
+        const int x = 2 * hh + ii, r = row0 + 8 * x + g;
+        if constexpr (M == kShared) {
+          float* to = r < p.rows ? shared_sums<D>(a, p.b, p.first, p.h, r) : nullptr;
+          const float4 u = acc[hh][0], v = acc[hh][1];
+          write_sums(to, q, lane, ii ? u.z : u.x, ii ? u.w : u.y, ii ? v.z : v.x, ii ? v.w : v.y);
+          if (q == 0 && c == 0 && r < p.rows) write_stats(a, p.b, p.first, p.h, r, top[x], sum[x]);
+          continue;
+        }
+        const float inv = sum[x] > 0.f ? __fdividef(1.f, sum[x]) : 0.f;
+        T* to = r < p.rows ? out_row<D, T>(a, p.first, p.h, r) : nullptr;
 #pragma unroll
         for (int k = 0; k < kReps; ++k)
-          v[j][hh][k] = reinterpret_cast<const float4*>(src + 2 * kPairRows)[(warp * (D / 4) + hh * (D / 8) + q * kReps + k) * 32 + lane];
-    }
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      if (part0 + j > last) continue;
-      float x_old[4], x_new[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const float next = fmaxf(top[x], mk[j][x]);
-        x_old[x] = top[x] == -INFINITY ? 0.f : ex2(top[x] - next);
-        x_new[x] = mk[j][x] == -INFINITY ? 0.f : ex2(mk[j][x] - next);
-        sum[x] = sum[x] * x_old[x] + lk[j][x] * x_new[x];
-        top[x] = next;
+          write_pair<T>(to, q * kReps + k, lane, (ii ? acc[hh][k].z : acc[hh][k].x) * inv, (ii ? acc[hh][k].w : acc[hh][k].y) * inv);
+        if (q == 0 && c == 0 && r < p.rows) write_lse(a, p.first, p.h, r, top[x], sum[x]);
       }
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-        for (int k = 0; k < kReps; ++k) {
-          const float4 n = v[j][hh][k];
-          float4& o = acc[hh][k];
-          o.x = o.x * x_old[2 * hh] + n.x * x_new[2 * hh];
-          o.y = o.y * x_old[2 * hh] + n.y * x_new[2 * hh];
-          o.z = o.z * x_old[2 * hh + 1] + n.z * x_new[2 * hh + 1];
-          o.w = o.w * x_old[2 * hh + 1] + n.w * x_new[2 * hh + 1];
-        }
-    }
-  }
-#pragma unroll
-  for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-    for (int ii = 0; ii < 2; ++ii) {
-      const int x = 2 * hh + ii, r = row0 + 8 * x + g;
-      if constexpr (M == kShared) {
-        float* to = r < p.rows ? shared_sums<D>(a, p.b, p.first, p.h, r) : nullptr;
-        const float4 u = acc[hh][0], v = acc[hh][1];
-        write_sums(to, q, lane, ii ? u.z : u.x, ii ? u.w : u.y, ii ? v.z : v.x, ii ? v.w : v.y);
-        if (q == 0 && c == 0 && r < p.rows) write_stats(a, p.b, p.first, p.h, r, top[x], sum[x]);
-        continue;
-      }
-      const float inv = sum[x] > 0.f ? __fdividef(1.f, sum[x]) : 0.f;
-      T* to = r < p.rows ? out_row<D, T>(a, p.first, p.h, r) : nullptr;
-#pragma unroll
-      for (int k = 0; k < kReps; ++k)
-        write_pair<T>(to, q * kReps + k, lane, (ii ? acc[hh][k].z : acc[hh][k].x) * inv, (ii ? acc[hh][k].w : acc[hh][k].y) * inv);
-      if (q == 0 && c == 0 && r < p.rows) write_lse(a, p.first, p.h, r, top[x], sum[x]);
-    }
+  };
+  for (int task = blockIdx.x; task < 8 * s_count; task += gridDim.x) join(s_begun[task / 8], task % 8);
 }
 
 template <int D, typename T, AttnMode M>
@@ -1017,7 +1043,7 @@ int launch_chunk(const AttnArgs& a, cudaStream_t s) {
   const int sms = device_sms();
   if (sms == 0 || !smem_optin<chunk_kernel<D, T, M>>(L::kBytes)) return OFFQ_ERR_CUDA;
   if (const int rc = launch_pdl(chunk_kernel<D, T, M>, dim3(sms), dim3(kThreads), L::kBytes, s, a); rc != OFFQ_OK) return rc;
-  return launch_pdl(join_chunks_kernel<D, T, M>, dim3(sms, 8), dim3(2 * D), 0, s, a, sms);
+  return launch_pdl(join_chunks_kernel<D, T, M>, dim3(2 * sms), dim3(2 * D), 0, s, a, sms);
 }
 
 template <AttnMode M>

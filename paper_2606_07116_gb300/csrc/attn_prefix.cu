@@ -13,6 +13,7 @@ namespace {
 using namespace offq;
 
 constexpr int kThreads = 256;
+constexpr int kFlight = 4;  // rows of a thread whose reads are in flight together
 
 // The prefix whose sequences b is one of, or -1. The warp looks at 32 of them at once.
 __device__ __forceinline__ int prefix_of(const AttnArgs& a, int b) {
@@ -29,63 +30,75 @@ __device__ __forceinline__ int prefix_of(const AttnArgs& a, int b) {
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads) join_shared_kernel(const AttnArgs a) {
+  constexpr int kLanes = D / 4;             // of a (query, head): four channels each
+  constexpr int kRows = kThreads / kLanes;  // that a block covers at once
   griddep_wait();
   griddep_launch_dependents();
   const int b = blockIdx.x;
   const PagedSeq s = paged_seq<kShared>(a, a.P + b);
-  const int64_t items = static_cast<int64_t>(s.n) * a.Hq * (D / 16);
-  int64_t u = static_cast<int64_t>(blockIdx.y) * kThreads + threadIdx.x;
-  if (u - (threadIdx.x & 31) >= items) return;  // whole warps: their lanes look for the prefix together
+  const int64_t rows = static_cast<int64_t>(s.n) * a.Hq;
+  if (static_cast<int64_t>(blockIdx.y) * kRows * kFlight >= rows) return;
   // Sums of a prefix are there for the rows of its own range alone.
   const int g = prefix_of(a, b);
   const PagedSeq p = paged_seq<kShared>(a, max(g, 0));
   const bool shared = g >= 0 && p.first <= s.first && s.first + s.n <= p.first + p.n;
-  for (; u < items; u += static_cast<int64_t>(gridDim.y) * kThreads) {
-    const int d = static_cast<int>(u % (D / 16)) * 16;
-    const int64_t row = static_cast<int64_t>(s.first) * a.Hq + u / (D / 16), own = a.Tq * a.Hq + row;
-    const float2 none = make_float2(-INFINITY, 0.f);
-    const float2 s0 = shared ? a.stats[row] : none, s1 = a.stats[own];
-    float4 x[4] = {}, y[4];
+  const int at = threadIdx.x % kLanes, c = threadIdx.x & 3;
+  const int64_t row0 = static_cast<int64_t>(s.first) * a.Hq, own = a.Tq * a.Hq;
+  for (int64_t base = static_cast<int64_t>(blockIdx.y) * kRows * kFlight; base < rows;
+       base += static_cast<int64_t>(gridDim.y) * kRows * kFlight) {
+    float2 s0[kFlight], s1[kFlight];
+    float4 x[kFlight], y[kFlight];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (shared) x[i] = reinterpret_cast<const float4*>(a.sums + row * D + d)[i];
-      y[i] = reinterpret_cast<const float4*>(a.sums + own * D + d)[i];
-    }
-    const float m0 = s0.y > 0.f ? s0.x : -INFINITY, m1 = s1.y > 0.f ? s1.x : -INFINITY, m = fmaxf(m0, m1);
-    const float e0 = m0 == -INFINITY ? 0.f : ex2(m0 - m), e1 = m1 == -INFINITY ? 0.f : ex2(m1 - m);
-    const float l = e0 * s0.y + e1 * s1.y, inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
-    const float f0 = e0 * inv, f1 = e1 * inv;
-    float v[16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float p0[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, p1[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[i + 8 * (e >> 1) + 4 * (e & 1)] = fmaf(p0[e], f0, p1[e] * f1);  // shared_at's order undone
-    }
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-      } else {
-        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    for (int i = 0; i < kFlight; ++i) {  // reads in flight together
+      const int64_t r = base + i * kRows + threadIdx.x / kLanes, row = row0 + r;
+      s0[i] = s1[i] = make_float2(-INFINITY, 0.f);
+      x[i] = y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r >= rows) continue;
+      if (shared) {
+        s0[i] = a.stats[row];
+        x[i] = reinterpret_cast<const float4*>(a.sums + row * D)[at];
       }
+      s1[i] = a.stats[own + row];
+      y[i] = reinterpret_cast<const float4*>(a.sums + (own + row) * D)[at];
     }
-    const int64_t t = row / a.Hq;
-    uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.ld_out + (row - t * a.Hq) * D + d);
-    to[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    to[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    if (d == 0 && a.lse != nullptr) a.lse[row] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const int64_t r = base + i * kRows + threadIdx.x / kLanes, row = row0 + r;
+      const float m0 = s0[i].y > 0.f ? s0[i].x : -INFINITY, m1 = s1[i].y > 0.f ? s1[i].x : -INFINITY, m = fmaxf(m0, m1);
+      const float e0 = m0 == -INFINITY ? 0.f : ex2(m0 - m), e1 = m1 == -INFINITY ? 0.f : ex2(m1 - m);
+      const float l = e0 * s0[i].y + e1 * s1[i].y, inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+      const float f0 = e0 * inv, f1 = e1 * inv;
+      // Channels c, c + 4, c + 8, c + 12 of 16 become 4 c .. 4 c + 3.
+      uint32_t w[4] = {__float_as_uint(fmaf(x[i].x, f0, y[i].x * f1)), __float_as_uint(fmaf(x[i].y, f0, y[i].y * f1)),
+                       __float_as_uint(fmaf(x[i].z, f0, y[i].z * f1)), __float_as_uint(fmaf(x[i].w, f0, y[i].w * f1))};
+      transpose_words(w, c);
+      if (r >= rows) continue;
+      uint2 u;
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 h0 = __floats2bfloat162_rn(__uint_as_float(w[0]), __uint_as_float(w[1]));
+        const __nv_bfloat162 h1 = __floats2bfloat162_rn(__uint_as_float(w[2]), __uint_as_float(w[3]));
+        u = make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
+      } else {
+        const __half2 h0 = __floats2half2_rn(__uint_as_float(w[0]), __uint_as_float(w[1]));
+        const __half2 h1 = __floats2half2_rn(__uint_as_float(w[2]), __uint_as_float(w[3]));
+        u = make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
+      }
+      const int64_t t = row / a.Hq;
+      reinterpret_cast<uint2*>(static_cast<T*>(a.out) + t * a.ld_out + (row - t * a.Hq) * D)[at] = u;
+      if (at == 0 && a.lse != nullptr) a.lse[row] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+    }
   }
 }
 
 template <int D, typename T>
 int launch_join(const AttnArgs& a, cudaStream_t s) {
-  const int64_t items = static_cast<int64_t>(std::min<int64_t>(a.max_q, a.Tq)) * a.Hq * (D / 16);
-  // The longest sequence's items, but no more blocks in all than a few waves.
-  const int64_t blocks = std::min((items + kThreads - 1) / kThreads, std::max(int64_t{1}, int64_t{32768} / a.B));
+  constexpr int kAtOnce = kThreads / (D / 4) * kFlight;
+  // The longest sequence's rows, but no more blocks in all than some waves: each looks for its prefix first (48 us for 2400
+  // tokens of 32 heads with a block for every 16 rows).
+  const int sms = device_sms();
+  if (sms == 0) return OFFQ_ERR_CUDA;
+  const int64_t rows = static_cast<int64_t>(std::min<int64_t>(a.max_q, a.Tq)) * a.Hq;
+  const int64_t blocks = std::min((rows + kAtOnce - 1) / kAtOnce, std::max(int64_t{1}, int64_t{16} * sms / a.B));
   return launch_pdl(join_shared_kernel<D, T>, dim3(a.B, static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, a);
 }
 

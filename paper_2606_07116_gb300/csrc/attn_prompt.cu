@@ -77,23 +77,6 @@ static_assert(sizeof(PromptCtrl) <= 512, "control block");
 // The lowest n bits.
 __device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1u; }
 
-// Word k of the four lanes c of a quad becomes word c of lane k.
-__device__ __forceinline__ void transpose_words(uint32_t (&w)[4], int c) {
-#pragma unroll
-  for (int step = 2; step > 0; step >>= 1) {
-    const bool high = (c & step) != 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int k = step == 2 ? i : 2 * i;  // words k and k + step change places between the lanes
-      const uint32_t got = __shfl_xor_sync(kAllLanes, high ? w[k] : w[k + step], step);
-      if (high)
-        w[k] = got;
-      else
-        w[k + step] = got;
-    }
-  }
-}
-
 // Queries of sequence b (its first row in `first`); none where its entries are out of range.
 __device__ __forceinline__ int prompt_seq(const AttnArgs& a, int b, int& first, bool& bad) {
   const int c0 = __ldg(a.cu + b), c1 = __ldg(a.cu + b + 1);
