@@ -79,7 +79,7 @@ struct ChunkLayout {
   static constexpr int kCtrl = kSums + 1024;
   static constexpr int kBytes = kCtrl + 512 + 1024;         // alignment to 1024
   static constexpr int64_t kPartFloats = kPairRows * (D + 2);
-  static_assert(kCtrl % 16 == 0 && sizeof(ChunkCtrl) <= 512 && 2 * (kThreads / 32) * sizeof(Cost) <= 1024 && kBytes <= 232448, "shared memory");
+  static_assert(kCtrl % 16 == 0 && sizeof(ChunkCtrl) <= 512 && (kThreads / 32) * sizeof(Cost) <= 1024 && kBytes <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ PartHead* part_heads(void* ws, int cta) { return static_cast<PartHead*>(ws) + 2 * cta; }
@@ -205,11 +205,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
   griddep_launch_dependents();
   __syncthreads();
   PartHead* heads = part_heads(a.workspace, blockIdx.x);
-  // The list of steps and this CTA's share of it. Some threads a sequence add up its tiles; they keep their first sequence, as
-  // most lists are no longer than the CTA.
+  // The list of steps and this CTA's share of it. Some threads a sequence add up its tiles.
   {
     constexpr int kWarps = kThreads / 32;
-    Cost* scan = reinterpret_cast<Cost*>(smem + L::kSums);      // [2][kWarps]: the queries' sums come there later
+    Cost* scan = reinterpret_cast<Cost*>(smem + L::kSums);      // [kWarps]: the queries' sums come there later
     Listed* list = reinterpret_cast<Listed*>(smem);             // and the tiles here
     static_assert(kThreads * sizeof(Listed) <= L::kSums, "the list fits");
     const int B = listed<M>(a);
@@ -229,33 +228,44 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       n.blocks *= a.H;
       return n;
     };
-    PagedSeq own = {};
-    Cost mine = {0, 0}, n = {0, 0};
-    for (int first = 0; first < B; first += at_once) {
+    // The sequences from `base` on into the list, behind what cost `before`; their cost.
+    auto enlist = [&](int base, const Cost& before) {
       PagedSeq s = {};
-      if (first + place < B) s = paged_seq<M>(a, first + place);
-      if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-      Cost c = cost(s);
-      if (tid % team != 0) c = {0, 0};
-      if (first == 0) {
-        own = s;
-        n = c;
+      if (base + place < B) s = paged_seq<M>(a, base + place);
+      Cost n = cost(s);
+      if (tid % team != 0) n = {0, 0};
+      Cost incl = n;
+#pragma unroll 1
+      for (int m = 1; m < 32; m <<= 1) {
+        const long long x = __shfl_up_sync(kAllLanes, incl.all, m), y = __shfl_up_sync(kAllLanes, incl.blocks, m);
+        if (lane >= m) {
+          incl.all += x;
+          incl.blocks += y;
+        }
       }
-      mine.all += c.all;
-      mine.blocks += c.blocks;
-    }
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) {
-      mine.all += __shfl_xor_sync(kAllLanes, mine.all, m);
-      mine.blocks += __shfl_xor_sync(kAllLanes, mine.blocks, m);
-    }
-    if (lane == 0) scan[warp] = mine;
-    __syncthreads();
-    Cost total = {0, 0};
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      total.all += scan[i].all;
-      total.blocks += scan[i].blocks;
+      if (lane == 31) scan[warp] = incl;
+      __syncthreads();
+      Cost chunk = {0, 0};
+#pragma unroll 4
+      for (int i = 0; i < kWarps; ++i) {
+        if (i == warp) {
+          incl.all += chunk.all;
+          incl.blocks += chunk.blocks;
+        }
+        chunk.all += scan[i].all;
+        chunk.blocks += scan[i].blocks;
+      }
+      list[tid] = Listed{before.all + incl.all - n.all, before.blocks + incl.blocks - n.blocks, s};
+      __syncthreads();
+      if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+      return chunk;
+    };
+    // Most lists are no longer than the CTA and are read once; others a second time, to find this CTA's share in them.
+    Cost head = enlist(0, Cost{0, 0}), total = head;
+    for (int base = at_once; base < B; base += at_once) {
+      const Cost more = enlist(base, Cost{0, 0});
+      total.all += more.all;
+      total.blocks += more.blocks;
     }
     const int ctas = static_cast<int>(min(total.all, static_cast<long long>(gridDim.x))), cta = blockIdx.x;
     const long long lo = cta < ctas ? divide(total.all * cta, ctas).q : 0;
@@ -264,37 +274,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
       ctrl->from = 0;
       ctrl->to = lo < hi ? total.blocks : 0;
     }
+    __syncthreads();
     Cost before = {0, 0};
     for (int first = 0; first < B && before.all <= hi && lo < hi; first += at_once) {
-      if (first > 0) {
-        own = {};
-        if (first + place < B) own = paged_seq<M>(a, first + place);
-        n = cost(own);
-        if (tid % team != 0) n = {0, 0};
-      }
-      Cost incl = n;
-#pragma unroll
-      for (int m = 1; m < 32; m <<= 1) {
-        const long long x = __shfl_up_sync(kAllLanes, incl.all, m), y = __shfl_up_sync(kAllLanes, incl.blocks, m);
-        if (lane >= m) {
-          incl.all += x;
-          incl.blocks += y;
-        }
-      }
-      if (lane == 31) scan[kWarps + warp] = incl;
-      __syncthreads();
-      Cost chunk = {0, 0};
-#pragma unroll
-      for (int i = 0; i < kWarps; ++i) {
-        if (i == warp) {
-          incl.all += chunk.all;
-          incl.blocks += chunk.blocks;
-        }
-        chunk.all += scan[kWarps + i].all;
-        chunk.blocks += scan[kWarps + i].blocks;
-      }
-      list[tid] = Listed{before.all + incl.all - n.all, before.blocks + incl.blocks - n.blocks, own};
-      __syncthreads();
+      const Cost chunk = B <= at_once ? head : enlist(first, before);
       const long long x = warp == 0 ? lo : hi;
       if (warp < 2 && x >= before.all && x < before.all + chunk.all) {  // a warp finds an end
         // A team's other threads cost nothing and begin where the next team does, which is found then.

@@ -71,7 +71,7 @@ struct Cost {
 // Control block behind the parts.
 template <int D, int NT>
 struct FewCtrl {
-  Cost scan[2][FewLayout<D, NT>::kWarps];
+  Cost scan[FewLayout<D, NT>::kWarps];
   int4 part[2 * FewLayout<D, NT>::kWarps];    // (sequence or -1, unit in it, first stage, last stage) of each part
   int2 rows[2 * FewLayout<D, NT>::kWarps];    // first query row of its sequence, rows of the unit
 };
@@ -230,67 +230,25 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   griddep_wait();
   griddep_launch_dependents();
 
-  // The whole work, this CTA's share and its warps' places in it. A thread keeps its first sequence, as most lists are no
-  // longer than the CTA.
+  // The whole work, this CTA's share and its warps' places in it.
   const int B = listed<M>(a);
   auto cost = [&](const PagedSeq& s) {
     const int stages = stages_of(a, s);
     const long long units = stages > 0 ? static_cast<long long>(a.H) * groups_of<M, L::kRows>(a, s) : 0;
     return Cost{units * (stages + kUnitCost<M>), units * stages};
   };
-  PagedSeq own = {};
-  Cost mine = {0, 0}, n = {0, 0};
-  for (int b = tid; b < B; b += kThreads) {
-    const PagedSeq s = few_seq<M>(a, b);
-    if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
-    const Cost x = cost(s);
-    if (b == tid) {
-      own = s;
-      n = x;
-    }
-    mine.all += x.all;
-    mine.stages += x.stages;
-  }
-#pragma unroll
-  for (int m = 16; m > 0; m >>= 1) {
-    mine.all += __shfl_xor_sync(kAllLanes, mine.all, m);
-    mine.stages += __shfl_xor_sync(kAllLanes, mine.stages, m);
-  }
-  if (lane == 0) ctrl->scan[0][warp] = mine;
-  __syncthreads();
-  Cost total = {0, 0};
-#pragma unroll
-  for (int i = 0; i < L::kWarps; ++i) {
-    total.all += ctrl->scan[0][i].all;
-    total.stages += ctrl->scan[0][i].stages;
-  }
-  // Little work goes to fewer CTAs, some stages each: their warps take them at once, and joining inside a CTA is cheaper.
-  const int ctas = static_cast<int>(min((total.all + kLeastStages - 1) / kLeastStages, static_cast<long long>(gridDim.x)));
-  const int cta = blockIdx.x;
-  const long long lo = cta < ctas ? divide(total.all * cta, ctas).q : 0;
-  const long long hi = cta < ctas ? divide(total.all * (cta + 1), ctas).q : 0;
-  PartHead* heads = part_head<D, NT>(a.workspace, blockIdx.x, 0);
-  if (lo == hi) {
-    if (tid < 2) heads[tid] = PartHead{-1, 0, 0, 0};
-    return;
-  }
-  const long long w0 = lo + (hi - lo) * warp / L::kWarps, w1 = lo + (hi - lo) * (warp + 1) / L::kWarps;
   Listed* list = reinterpret_cast<Listed*>(smem);  // where the rings will be
   static_assert(kThreads * sizeof(Listed) <= L::kPartOff, "the list fits");
-  int b0 = 0, unit0 = 0, t0 = 0;  // of this warp's first stage: sequence, unit in it, stage
-  PagedSeq s0 = {};
-  long long from = 0, to = total.stages;  // stages before it, and up to the warp's end
-  Cost before = {0, 0};
-  for (int base = 0; base < B && before.all <= hi; base += kThreads) {
-    if (base > 0) {
-      n = {0, 0};
-      if (base + tid < B) {
-        own = few_seq<M>(a, base + tid);
-        n = cost(own);
-      }
+  // The sequences base .. base + kThreads - 1 into the list, behind what cost `before`; their cost.
+  auto enlist = [&](int base, const Cost& before) {
+    PagedSeq s = {};
+    Cost n = {0, 0};
+    if (base + tid < B) {
+      s = few_seq<M>(a, base + tid);
+      n = cost(s);
     }
     Cost incl = n;
-#pragma unroll
+#pragma unroll 1
     for (int m = 1; m < 32; m <<= 1) {
       const long long x = __shfl_up_sync(kAllLanes, incl.all, m), y = __shfl_up_sync(kAllLanes, incl.stages, m);
       if (lane >= m) {
@@ -298,20 +256,46 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         incl.stages += y;
       }
     }
-    if (lane == 31) ctrl->scan[1][warp] = incl;
+    if (lane == 31) ctrl->scan[warp] = incl;
     __syncthreads();
     Cost chunk = {0, 0};
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < L::kWarps; ++i) {
       if (i == warp) {
         incl.all += chunk.all;
         incl.stages += chunk.stages;
       }
-      chunk.all += ctrl->scan[1][i].all;
-      chunk.stages += ctrl->scan[1][i].stages;
+      chunk.all += ctrl->scan[i].all;
+      chunk.stages += ctrl->scan[i].stages;
     }
-    list[tid] = Listed{before.all + incl.all - n.all, before.stages + incl.stages - n.stages, own};
+    list[tid] = Listed{before.all + incl.all - n.all, before.stages + incl.stages - n.stages, s};
     __syncthreads();
+    if (s.bad && blockIdx.x == 0) *a.status = OFFQ_ERR_INVALID_ARG;
+    return chunk;
+  };
+  // Most lists are no longer than the CTA and are read once; others a second time, to find this CTA's share in them.
+  Cost first = enlist(0, Cost{0, 0}), total = first;
+  for (int base = kThreads; base < B; base += kThreads) {
+    const Cost more = enlist(base, Cost{0, 0});
+    total.all += more.all;
+    total.stages += more.stages;
+  }
+  // Little work goes to fewer CTAs, some stages each: their warps take them at once, and joining inside a CTA is cheaper.
+  const int ctas = static_cast<int>(min((total.all + kLeastStages - 1) / kLeastStages, static_cast<long long>(gridDim.x)));
+  const int cta = blockIdx.x;
+  PartHead* heads = part_head<D, NT>(a.workspace, blockIdx.x, 0);
+  if (cta >= ctas) {
+    if (tid < 2) heads[tid] = PartHead{-1, 0, 0, 0};
+    return;
+  }
+  const long long lo = divide(total.all * cta, ctas).q, hi = divide(total.all * (cta + 1), ctas).q;
+  const long long w0 = lo + (hi - lo) * warp / L::kWarps, w1 = lo + (hi - lo) * (warp + 1) / L::kWarps;
+  int b0 = 0, unit0 = 0, t0 = 0;  // of this warp's first stage: sequence, unit in it, stage
+  PagedSeq s0 = {};
+  long long from = 0, to = total.stages;  // stages before it, and up to the warp's end
+  Cost before = {0, 0};
+  for (int base = 0; base < B && before.all <= hi; base += kThreads) {
+    const Cost chunk = B <= kThreads ? first : enlist(base, before);
 #pragma unroll 1
     for (int end = 0; end < 2; ++end) {
       const long long x = end ? w1 : w0;
