@@ -57,7 +57,7 @@ def test_one_prefix_single_tokens(prefix, Hq, H, D, page, dt):
 
 
 @pytest.mark.parametrize("Hq,H,D,page,dt", HEADS)
-@pytest.mark.parametrize("news", [[2, 1, 3, 1, 4], [4] * 5, [1, 17, 9, 2, 1], [33, 5, 1, 64, 1], [150, 40, 1, 1, 129]])
+@pytest.mark.parametrize("news", [[2, 1, 3, 1, 4], [4] * 5, [7, 8, 5, 1, 6], [1, 17, 9, 2, 1], [33, 5, 1, 64, 1], [150, 40, 1, 1, 129]])
 def test_several_prefixes_and_new_tokens(news, Hq, H, D, page, dt):
     lens = [n + past for n, past in zip(news, (77, 0, 300, 5, 130))]
     _shared([130, 1, 700], [0, 2, 3, 5], lens, news, Hq, H, D, page, dt, seed=sum(news))

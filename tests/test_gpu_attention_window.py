@@ -211,3 +211,24 @@ def test_a_graph_follows_the_window():
         torch.cuda.synchronize()
         assert torch.equal(out, Q.paged_attention(x, cache, table, n, cu, 1, window=40, sinks=4))
     assert Q.offq_get_device_status() == Q.OFFQ_OK
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_the_longest_context(new):
+    """Token numbers up to the last that the library takes, of which the window and the sinks alone have pages."""
+    most, page, window, sinks, D = 0x7FFFFF00, 256, 300, 4, 64
+    rows = np.zeros(3 * page, bool)  # the first page, and the last two
+    rows[:sinks] = True
+    rows[page + 2 * page - window - new + 1:] = True
+    pages = Pages([rows], 1, D, page, 17, table_pad=0)
+    table = torch.full((1, most // page), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = int(pages.table[0, 0])
+    table[0, -2:] = torch.from_numpy(pages.table[0, 1:]).cuda()
+    qb, q64 = queries(new, 4, D, "bf16", 18)
+    out, lse = Q.paged_attention(qb.cuda(), pages.cache(), table, i32([most]), i32([0, new]), new, lse=True, window=window,
+                                 sinks=sinks)
+    assert Q.offq_get_device_status() == Q.OFFQ_OK
+    at = 3 * page - new  # as positions of a sequence of three pages, whose window is the same
+    seen = A.in_window(at, new, 3 * page, window, sinks)
+    k, k_mag, v, v_mag = pages.tokens(0, 3 * page)
+    check(out.cpu().double().numpy(), lse.cpu().double().numpy(), q64, k_mag, k, v, v_mag, D ** -0.5, seen, "bf16")
