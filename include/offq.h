@@ -722,7 +722,9 @@ int offq_paged_attention(const void* q, int dtype, int64_t Tq, int32_t Hq, int32
  * j <= p with j > p - window or j < sinks. Tokens that no query of the sequence
  * sees are not read, and may have been given back: the slots may hold anything,
  * and entries of block_table whose pages hold nothing else are not looked at.
- * The same rows, workspace, roundings and errors.
+ * The same rows, roundings and errors; a workspace of
+ * offq_paged_attention_window_workspace(...) bytes (none where sequences are few
+ * and short; offq_paged_attention's is enough for any call).
  *   window    newest tokens up to the query itself, 1 at least.
  *   sinks     first tokens of the sequence that stay visible, 0 at least.
  */
@@ -732,6 +734,9 @@ int offq_paged_attention_window(const void* q, int dtype, int64_t Tq, int32_t Hq
                                 int64_t ld_table, const int32_t* lens, const int32_t* cu_q, int32_t B, int32_t max_q,
                                 float scale, int32_t window, int32_t sinks, void* out, int64_t ld_out, float* lse,
                                 void* workspace, int64_t workspace_bytes, void* stream);
+int64_t offq_paged_attention_window_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
+                                              int32_t max_q, int32_t page_size, int64_t ld_table, int32_t window,
+                                              int32_t sinks);
 
 /*
  * offq_paged_attention_prefix -- offq_paged_attention for batches whose sequences
@@ -764,7 +769,7 @@ int offq_paged_attention_prefix(const void* q, int dtype, int64_t Tq, int32_t Hq
 int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
                                               int32_t max_q, int32_t P);
 
-/* Bytes of offq_paged_attention's workspace (and of the call's with a window) on the current device (-1 on sizes
+/* Bytes of offq_paged_attention's workspace on the current device (-1 on sizes
  * it refuses). */
 int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B, int32_t max_q);
 

@@ -65,6 +65,26 @@ extern "C" int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq,
   return most < 0 ? -1 : most + sums_bytes(Tq, Hq, head_dim);
 }
 
+extern "C" int64_t offq_paged_attention_window_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
+                                                         int32_t max_q, int32_t page_size, int64_t ld_table,
+                                                         int32_t window, int32_t sinks) {
+  if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || ld_table < 0 || window < 1 || sinks < 0) return -1;
+  const int64_t parts = offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q);
+  if (parts <= 0) return parts;
+  AttnArgs a = {};
+  a.Tq = Tq;
+  a.H = H;
+  a.G = Hq / H;
+  a.B = B;
+  a.max_q = max_q;
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  a.ld_table = ld_table;
+  a.window = std::min(window, kMostTokens);
+  a.sinks = std::min(sinks, kMostTokens);
+  a.few_rows = kFewRows;
+  return static_cast<int64_t>(max_q) * a.G <= kFewRows && paged_few_whole(a, kWindowed) ? 0 : parts;
+}
+
 namespace {
 
 // The paged calls' own arguments: checks and launches. `mode` says which of them was made.
@@ -100,8 +120,10 @@ int paged_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, int32_t 
   a.few_rows = mode == kShared ? kFewSharedRows : kFewRows;
   const int64_t parts = workspace_bytes_for(head_dim, most_rows, a.few_rows);
   if (a.status == nullptr || parts < 0) return OFFQ_ERR_CUDA;
-  const int64_t need = mode == kShared ? parts + sums_bytes(a.Tq, a.Hq, head_dim) : parts;
-  if (a.workspace == nullptr || workspace_bytes < need) return OFFQ_ERR_INVALID_ARG;
+  a.whole = paged_few_whole(a, mode);
+  int64_t need = mode == kShared ? parts + sums_bytes(a.Tq, a.Hq, head_dim) : parts;
+  if (mode == kWindowed && a.whole && most_rows <= a.few_rows) need = 0;
+  if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return OFFQ_ERR_INVALID_ARG;
   if (mode == kShared) {
     a.sums = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + parts);
     a.stats = reinterpret_cast<float2*>(a.sums + 2 * a.Tq * a.Hq * head_dim);

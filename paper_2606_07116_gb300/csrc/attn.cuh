@@ -43,6 +43,7 @@ struct AttnArgs {
   int few_rows;   // sequences with at most this many rows n * G take the few-row form
   int causal;     // prompts
   int window, sinks;  // kWindowed: at most kMostTokens each
+  int whole;          // the few-row form gives every CTA a whole unit: no part crosses CTAs
   const int32_t* prefix_table;  // kShared
   int64_t ld_prefix;
   const int32_t* prefix_lens;
@@ -251,6 +252,12 @@ __device__ __forceinline__ void write_stats(const AttnArgs& a, int b, int first,
 constexpr int kFewRows = 16;
 // Behind shared prefixes it takes groups of 8 or 16 rows, up to this many in all.
 constexpr int kFewSharedRows = 32;
+// Under a window or behind shared prefixes: whether every CTA gets a whole unit, so that no parts are joined behind it and a call
+// under a window needs no workspace. So where there are no more units than CTAs and none is longer than this many stages of 32
+// tokens. One token of a stream with a window of 1024: 19.8 us a call against 25.1 split, where the host bounds it; 13.5 against
+// 12.5 in a graph; two streams behind 500 shared tokens 14.1 against 15.2 there.
+constexpr int64_t kMostWhole = 40;
+bool paged_few_whole(const AttnArgs& a, AttnMode mode);
 int64_t paged_few_workspace(int head_dim);
 int paged_few(const AttnArgs& a, AttnMode mode, int dtype, int head_dim, cudaStream_t s);
 

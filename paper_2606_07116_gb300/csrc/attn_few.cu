@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   auto cost = [&](const PagedSeq& s) {
     const int stages = stages_of(a, s);
     const long long units = stages > 0 ? static_cast<long long>(a.H) * groups_of<M, L::kRows>(a, s) : 0;
+    if (M != kCausal && a.whole) return Cost{units, units * stages};
     return Cost{units * (stages + kUnitCost<M>), units * stages};
   };
   Listed* list = reinterpret_cast<Listed*>(smem);  // where the rings will be
@@ -281,11 +282,12 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     total.stages += more.stages;
   }
   // Little work goes to fewer CTAs, some stages each: their warps take them at once, and joining inside a CTA is cheaper.
-  const int ctas = static_cast<int>(min((total.all + kLeastStages - 1) / kLeastStages, static_cast<long long>(gridDim.x)));
+  const int least = M != kCausal && a.whole ? 1 : kLeastStages;
+  const int ctas = static_cast<int>(min((total.all + least - 1) / least, static_cast<long long>(gridDim.x)));
   const int cta = blockIdx.x;
-  PartHead* heads = part_head<D, NT>(a.workspace, blockIdx.x, 0);
+  PartHead* heads = M != kCausal && a.whole ? nullptr : part_head<D, NT>(a.workspace, blockIdx.x, 0);
   if (cta >= ctas) {
-    if (tid < 2) heads[tid] = PartHead{-1, 0, 0, 0};
+    if (tid < 2 && heads != nullptr) heads[tid] = PartHead{-1, 0, 0, 0};
     return;
   }
   const long long lo = divide(total.all * cta, ctas).q, hi = divide(total.all * (cta + 1), ctas).q;
@@ -296,6 +298,22 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   Cost before = {0, 0};
   for (int base = 0; base < B && before.all <= hi; base += kThreads) {
     const Cost chunk = B <= kThreads ? first : enlist(base, before);
+    if (M != kCausal && a.whole) {  // unit number lo, a share of its stages for each warp
+      if (lo >= before.all && lo < before.all + chunk.all) {
+        const int at = find_listed(list, kThreads, lo);
+        const Listed found = list[at];
+        const int stages = stages_of(a, found.s);
+        unit0 = static_cast<int>(lo - found.start);
+        t0 = static_cast<int>(static_cast<long long>(stages) * warp / L::kWarps);
+        from = t0;
+        to = static_cast<long long>(stages) * (warp + 1) / L::kWarps;
+        b0 = base + at;
+        s0 = found.s;
+      }
+      before.all += chunk.all;
+      __syncthreads();
+      continue;
+    }
 #pragma unroll 1
     for (int end = 0; end < 2; ++end) {
       const long long x = end ? w1 : w0;
@@ -752,7 +770,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     }
     __syncwarp();
   }
-  if (tid == 0) {
+  if (tid == 0 && heads != nullptr) {
     if (!have0) heads[0] = PartHead{-1, 0, 0, 0};
     if (!have1) heads[1] = PartHead{-1, 0, 0, 0};
   }
@@ -843,6 +861,7 @@ int launch_few(const AttnArgs& a, cudaStream_t s) {
   if (const int rc = launch_pdl(paged_few_kernel<D, NT, T, M>, dim3(sms), dim3(L::kWarps * 32), L::kBytes, s, a);
       rc != OFFQ_OK)
     return rc;
+  if (a.whole) return OFFQ_OK;
   return launch_pdl(join_parts_kernel<D, NT, T, M>, dim3(sms), dim3(256), 0, s, a, sms);
 }
 
@@ -861,6 +880,19 @@ int launch_few_m(const AttnArgs& a, int dtype, int head_dim, cudaStream_t s) {
 }  // namespace
 
 namespace offq {
+
+bool paged_few_whole(const AttnArgs& a, AttnMode mode) {
+  if (mode == kCausal) return false;
+  const int64_t own = static_cast<int64_t>(a.max_q) * a.G, held = std::min<int64_t>(own, kFewRows) > 8 ? 16 : 8;
+  auto groups = [&](int64_t rows) { return mode == kShared ? (std::min<int64_t>(rows, a.few_rows) + held - 1) / held : 1; };
+  int64_t units = groups(own) * a.B, tokens = a.ld_table << a.page_shift;
+  if (mode == kWindowed) tokens = std::min(tokens, static_cast<int64_t>(a.window) + a.sinks + a.max_q + 2 * kTile);
+  if (mode == kShared) {
+    units += groups(std::min(a.Tq, static_cast<int64_t>(a.B) * a.max_q) * a.G) * a.P;
+    tokens = std::max(tokens, a.ld_prefix << a.page_shift);
+  }
+  return units * a.H <= device_sms() && tokens <= kMostWhole * kTile;
+}
 
 int64_t paged_few_workspace(int head_dim) {
   const int sms = device_sms();

@@ -107,6 +107,8 @@ _SIGNATURES = {
                                              _c_vp, _c_i64, _c_i32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i32, _c_i32, _c_vp,
                                              _c_i64, _c_vp, _c_vp, _c_i32, _c_f32, _c_vp, _c_i64, _c_vp, _c_vp, _c_i64,
                                              _c_vp]),
+    "offq_paged_attention_window_workspace": (_c_i64, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i64,
+                                                       _c_i32, _c_i32]),
     "offq_paged_attention_prefix_workspace": (_c_i64, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
     "offq_prompt_attention_window": (_c_int, [_c_vp, _c_vp, _c_vp, _c_int, _c_i64, _c_i32, _c_i32, _c_i32, _c_i64,
                                               _c_i64, _c_i64, _c_vp, _c_i32, _c_f32, _c_i32, _c_i32, _c_vp, _c_i64,
@@ -832,8 +834,13 @@ def paged_attention_workspace(Tq: int, Hq: int, H: int, head_dim: int, B: int, m
 
 
 @functools.lru_cache(maxsize=1024)
-def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int, prefixes: int = 0) -> int:
-    need = paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q, prefixes)
+def _workspace_bytes(device: int, Tq: int, Hq: int, H: int, head_dim: int, B: int, max_q: int, prefixes: int = 0,
+                     windowed: Optional[tuple] = None) -> int:
+    """windowed: (page_size, ld_table, window, sinks) of a call with a window, which may need less."""
+    if windowed is not None:
+        need = load_library().offq_paged_attention_window_workspace(Tq, Hq, H, head_dim, B, max_q, *windowed)
+    else:
+        need = paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q, prefixes)
     if need < 0:
         raise LookupError  # not kept; the call itself says what is wrong with its sizes
     return need
@@ -1019,7 +1026,8 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
         ld_out = _heads(out)[3]
     if workspace is None:
         try:
-            need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q, P)
+            need = _workspace_bytes(q.get_device(), Tq, Hq, H, hd, B, max_q, P,
+                                    None if window is None else (page_size, width, window, sinks))
         except LookupError:
             need = 0
         workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None

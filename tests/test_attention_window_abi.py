@@ -143,3 +143,12 @@ def test_helpers_reach_the_calls(monkeypatch):
     Q.prompt_attention(q, kv, kv, i32(2), window=7, sinks=2)
     assert lib.calls[-1][0] == "offq_prompt_attention_window" and lib.calls[-1][1][14:16] == (7, 2)
     Q._workspace_bytes.cache_clear()
+
+
+def test_window_workspace_refusals(lib):
+    f = lib.offq_paged_attention_window_workspace
+    good = (4, 8, 2, 128, 2, 2, 16, 9, 30, 4)
+    for at, x in ((0, -1), (1, 7), (3, 96), (4, -1), (5, -1), (6, 8), (6, 48), (6, 512), (7, -1), (8, 0), (9, -1)):
+        assert f(*good[:at], x, *good[at + 1:]) == -1, (at, x)
+    for at in (0, 4, 5):
+        assert f(*good[:at], 0, *good[at + 1:]) == 0

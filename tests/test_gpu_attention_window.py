@@ -232,3 +232,33 @@ def test_the_longest_context(new):
     seen = A.in_window(at, new, 3 * page, window, sinks)
     k, k_mag, v, v_mag = pages.tokens(0, 3 * page)
     check(out.cpu().double().numpy(), lse.cpu().double().numpy(), q64, k_mag, k, v, v_mag, D ** -0.5, seen, "bf16")
+
+
+def test_calls_that_need_no_workspace():
+    """Few and short sequences, and tables that are too wide or batches too large for that: the same results with the
+    workspace that the call asks for, a larger one, and none where it asks for none."""
+    for L, B_, width, news in ((300, 2, 20, 1), (300, 2, 20, 4), (300, 2, 200, 1), (40, 70, 4, 1), (1000, 16, 70, 3)):
+        pages = Pages([np.ones(L, bool)] * B_, 2, 128, 16, 21, table_pad=max(1, width - -(-L // 16)))
+        qb, q64 = queries(B_ * news, 8, 128, "bf16", 22)
+        args = (qb.cuda(), pages.cache(), i32(pages.table), i32([L] * B_), i32(cumulative([news] * B_)), news)
+        for window, sinks in ((30, 4), (900, 0), (4000, 40)):
+            need = Q.load_library().offq_paged_attention_window_workspace(B_ * news, 8, 2, 128, B_, news, 16,
+                                                                          pages.table.shape[1], window, sinks)
+            most = Q.paged_attention_workspace(B_ * news, 8, 2, 128, B_, news)
+            tokens = min(pages.table.shape[1] * 16, window + sinks + news + 64)
+            assert need == (0 if B_ * 2 <= torch.cuda.get_device_properties(0).multi_processor_count and tokens <= 1280
+                            else most)
+            kw = dict(window=window, sinks=sinks, lse=True)
+            a = Q.paged_attention(*args, **kw)
+            b = Q.paged_attention(*args, workspace=torch.empty(most, dtype=torch.uint8, device="cuda"), **kw)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+            if need > 0:
+                with pytest.raises(Q.OffqError):
+                    Q.paged_attention(*args, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"), **kw)
+            seen = A.in_window(L - news, news, L, window, sinks)
+            for s in (0, B_ - 1):
+                k, k_mag, v, v_mag = pages.tokens(s, L)
+                rows = slice(s * news, (s + 1) * news)
+                check(a[0][rows].cpu().double().numpy(), a[1][rows].cpu().double().numpy(), q64[rows], k_mag, k, v, v_mag,
+                      128 ** -0.5, seen, "bf16")
+    assert Q.offq_get_device_status() == Q.OFFQ_OK
