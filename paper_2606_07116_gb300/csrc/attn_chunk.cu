@@ -1,5 +1,6 @@
 // Attention of many query rows over the paged 4-bit cache (offq_paged_attention where a sequence brings more
-// than 16 rows n * Hq / H per key head: chunks of a prompt, whole prompts, long drafts) on the tensor cores.
+// than 16 rows n * Hq / H per key head: chunks of a prompt, whole prompts, long drafts; under a window; all queries behind a
+// shared prefix where they are more than 32 rows) on the tensor cores.
 //
 // A row is one query of one head; the rows of a sequence and key head are taken 256 at a time (two tiles of
 // 128) against blocks of 128 cached tokens, as in the prompt kernel: scores, weights and outputs stay in
@@ -13,7 +14,11 @@
 //     scales, which with a row a thread would take twice the time of the products themselves.
 //   * out = (O + sum p o_v) / sum p: the values' offsets add the same to every channel.
 //   * Work is the list of (row pair tile, block) steps; the CTAs take equal shares of it, and what crosses CTAs
-//     is joined by a second kernel from at most two parts per CTA.
+//     is joined by a second kernel from at most two parts per CTA. With windows and prefixes tiles may be short, and count as four
+//     blocks more than they have: queries, first scores and outputs take 10 us (six chunks behind 6000 tokens 922 us without).
+//   * Under a window each row pair tile leaves out what none of its rows sees between the sinks and its first query's window, in
+//     groups of eight keys: sinks and window share a block. Only the widening warps know; the softmax hides keys in the blocks at
+//     either edge. Behind shared prefixes the list is that of csrc/attn_few.cu; sums go to memory in the order lanes hold them.
 // P' is a half, and the values q are: the reference m of a row's exponentials is the largest z + log2(s_v) of the keys that
 // it sees (or up to kMostLog2 below it), so that the largest P' is 1 to 2^kMostLog2 whatever the values' size is. 32 keys at a
 // time are weighed against the reference they meet; only where a row's weights times the block's largest s_v could pass
@@ -24,10 +29,14 @@
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warps 12-15 widen; all find the
 // CTA's work before that.
 //
-// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 599 us, 805 TFLOP/s; 16 sequences of
-// 8 tokens over 500 to 6000 122 us. What bounds it: with softmax, widening and reads left out the products take 341 us, since S has
+// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 601 us, 800 TFLOP/s, under a window
+// of 4096 with 16 sinks 220 us, 580 TFLOP/s; 256 single tokens behind 32768 shared ones 170 us of 240, 750 TFLOP/s; 16 sequences of
+// 8 tokens over 500 to 6000 122 us. A step (256 rows, 128 keys) takes 2.76 us: a tile's softmax (1.9) and its two products (0.87)
+// follow each other, the other tile's in between. A CTA's first step ends 26 us after the launch. What bounds it: with softmax, widening and reads left out the products take 341 us, since S has
 // both operands in shared memory, which delivers them at 77 % of the tensor rate; reads add about 80, widening 50, the
-// softmax 130. 16 softmax warps of 16 rows were slower (671 against 640), as were maxima taken before the weights (901).
+// softmax 130. 16 softmax warps of 16 rows were slower (671 against 640), as were maxima taken before the weights (901), products
+// with the first 64 weights while the others are made (window: 239 against 225), scores of 64 keys at a time (328) and queries staged
+// ahead by idle warps (232).
 #include <algorithm>
 #include <cstddef>
 

@@ -1,5 +1,5 @@
 // Attention of few query rows over the paged 4-bit cache (offq_paged_attention with up to 16 rows
-// n * Hq / H per sequence and key head: single tokens, drafted tokens).
+// n * Hq / H per sequence and key head: single tokens, drafted tokens; under a window; behind shared prefixes up to 32).
 //
 // Every cached byte is read once for all rows of its key head, so the cache bounds it: D + 16 bytes per
 // token and head (144 at D = 128) against 4 D multiply-adds per row.
@@ -9,6 +9,14 @@
 // evenly and in one wave. A warp that holds a whole (sequence, head) writes its output; parts are joined
 // in shared memory at the CTA's end, and what crosses CTAs in a second small kernel (at most a first and a
 // last part per CTA: the workspace does not grow with the batch).
+//
+// Window and sinks: a sequence's stages leave out the gap between the sinks and the window of its first query, whole stages of it,
+// and number the rest 0, 1, ...; only the copies know the difference. Halves of a stage that no query sees are not copied (their
+// page may be gone), and a row's hidden keys are taken out in the stages at the gap alone, as the last stage's are.
+// Shared prefixes: the list begins with the prefixes, each a sequence with all queries that stand behind it, in groups of 8 or 16
+// rows, and goes on with the sequences' own tokens. Sums and statistics of both go to memory (csrc/attn_prefix.cu). A group more
+// reads its pages from the L2 and costs less than the many-row form up to 32 rows (30 sequences of 1 to 3 tokens behind five
+// prefixes, 12 rows each: 99 us, 119 with groups up to 16, 133 in the many-row form).
 //
 // A warp stages its tokens itself, by asynchronous copies of 16 bytes a lane (a head's tokens of a page are contiguous)
 // into a ring of its own, and all lanes read fragments for warp-level MMAs of 16 tokens:
@@ -29,7 +37,9 @@
 // tokens 233 against 212 us; pages of 16 tokens, 64 streams of 1 to 8191, 96 against 84). 16 warps of 8 rows (128 registers, two
 // stages each) or 8 of 16 rows (250, four stages): more warps spill (12 of 16 rows: 50 us where 8 take 36).
 // Measured: 4 x 65536 tokens, 32 heads of 128: 212 us, 5.7 TB/s, integer pipe and issue slots at 60 %. 64 streams of 1 to 8191,
-// 64 heads on 8: 84 us, 4.0 TB/s, 17 us of them whatever the lengths. 16 x 4 tokens over 500 to 6000: 36 us.
+// 64 heads on 8: 82 us, 4.1 TB/s. 16 x 4 tokens over 500 to 6000: 36 us. 64 streams of 1 to 40000 under a window of 4096 and 4
+// sinks: 70 us, 4.1 TB/s over all and 5.1 while it streams (issue slots 61 %, integer pipe 55 %); 11 us pass before the first
+// stage is there, most of it code that no cache holds yet, and 3 after the last. 30 sequences behind five prefixes: 59 us of 76.
 #include <algorithm>
 #include <type_traits>
 

@@ -17,13 +17,20 @@
 // by the softmax threads themselves: when S is complete, so is every product issued before it, O's among them. The
 // weights of the first 64 keys go to the products while those of the other 64 are made.
 //
+// Under a window an item's blocks leave out the keys between the sinks (rounded up to eight) and its first query's window, and
+// number the others 0, 1, ...; a block that holds both is copied in boxes of eight rows, one a lane. Hidden keys are bits, 32 a
+// word, looked at only in the blocks and words at an edge. An odd number of heads per key head is taken in pairs of heads and
+// one last head (256 tokens): tiles of the same tokens have a block less to see than neighbours under a short window.
+//
 // Rows past a sequence's end are the next sequence's. As queries they are not written, as keys their
 // scores are replaced, and as values they are zeroed in shared memory (0 times infinity is not 0).
 //
-// Measured (causal): one prompt of 8192, 32 heads on 8 of 128, bf16: 388 us, 1416 TFLOP/s, tensor pipe 58 % on a prompt of 4096;
+// Measured (causal): one prompt of 8192, 32 heads on 8 of 128, bf16: 360 us, 1530 TFLOP/s, tensor pipe 58 % on a prompt of 4096;
 // S with both operands in shared memory runs at 77 % of the tensor rate at best. 24 prompts of 5 to 2000, 16 heads on 4 of
-// 64, f16: 125 us, 680 TFLOP/s: 1.33 us a block of 128 keys and about 2 us an item, latency and not any one pipe (exponentials
-// 28 %). Without taking over items 151 us; with two threads a row 148.
+// 64, f16: 119 us, 710 TFLOP/s: 1.33 us a block of 128 keys and about 1.2 us an item, latency and not any one pipe (exponentials
+// 28 %). Without taking over items 151 us (of 125 then); with two threads a row 148.
+// Under a window: one prompt of 16384, 4096 keys and 4 sinks, 680 us, 1420 TFLOP/s; one of 5001, 20 heads on 4 of 128, 512 and 64:
+// 46 us, 606 TFLOP/s (three items a CTA, 1.85 us a block, 5.5 us before the first scores); the 24 prompts, 300 and 1: 61 us.
 #include <algorithm>
 
 #include "attn_tc.cuh"
