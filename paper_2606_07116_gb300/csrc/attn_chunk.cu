@@ -634,6 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
           if (ok && active) ok = wait(&ctrl->s_full[i], ns++);
           if (!ok) break;
           if (live) {
+            __syncwarp();  // tensor memory is read by whole warps: a vote alone may leave lanes apart
             tc_fence_after();
             const float4* pk = reinterpret_cast<const float4*>(smem + L::kParK + slot * 1024) + c;
             const float4* pv = reinterpret_cast<const float4*>(smem + L::kParV + slot * 1024) + c;

@@ -479,6 +479,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
       for (int j = 0; j < my_blocks; ++j) {
         ok = wait(&ctrl->s_full[i], ns++);
         if (!ok) break;
+        __syncwarp();  // tensor memory is read by whole warps: a vote alone may leave lanes apart
         tc_fence_after();
         uint32_t s[kKt];
         tmem_ld_128cols(s_tm, s);

@@ -205,3 +205,28 @@ def test_another_stream_and_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, call())
     assert Q.offq_get_device_status() == Q.OFFQ_OK
+
+
+def test_calls_on_two_streams_at_once():
+    """Behind prefixes and under a window, single tokens and chunks, side by side on two streams: each call has a workspace of
+    its own, and gives what it gives alone."""
+    pages = Pages([np.ones(L, bool) for L in (900, 400, 700, 333)], 2, 128, 16, 31)
+    cache, prefix = pages.cache(), Q.SharedPrefix(i32(pages.table[:1]), i32([900]), i32([0, 3]))
+    table, lens = i32(pages.table[1:]), i32([400, 700, 333])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    calls = []
+    for new in (1, 50):
+        q = queries(3 * new, 8, 128, "bf16", 32 + new)[0].cuda()
+        args = (q, cache, table, lens, i32(cumulative([new] * 3)), new)
+        calls += [(args, dict(prefix=prefix)), (args, dict(window=200, sinks=4))]
+    alone = [Q.paged_attention(*args, **kw) for args, kw in calls]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for i in range(len(calls)):
+            for s, k in zip(streams, (i, (i + 1) % len(calls))):
+                args, kw = calls[k]
+                got.append((k, Q.paged_attention(*args, stream=s, **kw)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(alone[k], out) for k, out in got)
+    assert Q.offq_get_device_status() == Q.OFFQ_OK

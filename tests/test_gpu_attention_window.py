@@ -262,3 +262,56 @@ def test_calls_that_need_no_workspace():
                 check(a[0][rows].cpu().double().numpy(), a[1][rows].cpu().double().numpy(), q64[rows], k_mag, k, v, v_mag,
                       128 ** -0.5, seen, "bf16")
     assert Q.offq_get_device_status() == Q.OFFQ_OK
+
+
+@pytest.mark.parametrize("new", [1, 3, 60])
+def test_outputs_inside_wider_rows(new):
+    """out= as the middle heads of wider rows: what stands around them stays."""
+    pages = Pages([np.ones(200, bool), np.ones(150, bool)], 2, 128, 16, 41)
+    T = 2 * new
+    qb, _ = queries(T, 8, 128, "bf16", 42)
+    args = (qb.cuda(), pages.cache(), i32(pages.table), i32([200, 150]), i32([0, new, T]), new)
+    prefix = Q.SharedPrefix(i32(pages.table[:1]), i32([77]), i32([0, 2]))
+    x, _ = queries(300, 12, 128, "bf16", 43)
+    x = x.cuda()
+    prompt = (x[:, :8], x[:, 8:10], x[:, 10:], i32([0, 130, 300]))
+    for call, n in ((lambda **kw: Q.paged_attention(*args, window=40, sinks=4, **kw), T),
+                    (lambda **kw: Q.paged_attention(*args, prefix=prefix, **kw), T),
+                    (lambda **kw: Q.prompt_attention(*prompt, window=40, sinks=4, **kw), 300)):
+        wide = torch.full((n, 11, 128), 5.0, dtype=torch.bfloat16, device="cuda")
+        out = call(out=wide[:, 2:10])
+        assert out.data_ptr() == wide[:, 2:].data_ptr()
+        assert torch.equal(out, call()) and torch.all(wide[:, :2] == 5.0) and torch.all(wide[:, 10:] == 5.0)
+
+
+@pytest.mark.parametrize("new", [1, 9])
+def test_a_graph_of_a_large_batch(new):
+    """More units than SMs, so parts that cross CTAs; captured, and replayed as lengths grow, as calls compute it."""
+    B_, H = 40, 8
+    lens = [60 + 37 * b for b in range(B_)]
+    pages = Pages([np.ones(L + 20, bool) for L in lens], H, 64, 32, 51)
+    cache, table, n = pages.cache(), i32(pages.table), i32(lens)
+    cu = i32(cumulative([new] * B_))
+    prefix = Q.SharedPrefix(table[3:5].contiguous(), i32([90, 100]), i32([0, 25, B_]))
+    x = torch.zeros((B_ * new, 2 * H, 64), dtype=torch.float16, device="cuda")
+
+    def calls():
+        return (Q.paged_attention(x, cache, table, n, cu, new, window=700, sinks=3),
+                Q.paged_attention(x, cache, table, n, cu, new, prefix=prefix))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        calls()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            a, b = calls()
+    torch.cuda.current_stream().wait_stream(s)
+    for step in (0, 11, 20):
+        x.normal_(generator=torch.Generator(device="cuda").manual_seed(step))
+        n.copy_(i32([L + step for L in lens]))
+        graph.replay()
+        torch.cuda.synchronize()
+        c, d = calls()
+        assert torch.equal(a, c) and torch.equal(b, d)
+    assert Q.offq_get_device_status() == Q.OFFQ_OK
