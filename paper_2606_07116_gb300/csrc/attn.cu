@@ -27,12 +27,15 @@ int check_attention(int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_d
   return OFFQ_OK;
 }
 
+// Most rows of a sequence that the few-row form takes.
+int few_rows_of(AttnMode mode) { return mode == kCausal ? kFewRows : kFewGroupedRows; }
+
 // Calls whose sequences may all have few rows need the small form's parts alone; others may take both forms, one
 // after the other on the same bytes.
-int64_t workspace_bytes_for(int head_dim, int64_t most_rows, int few_rows) {
+int64_t workspace_bytes_for(int head_dim, int64_t most_rows, AttnMode mode) {
   const int64_t few = paged_few_workspace(head_dim), chunk = paged_chunk_workspace(head_dim);
   if (few < 0 || chunk < 0) return -1;
-  return most_rows > few_rows ? std::max(few, chunk) : few;
+  return most_rows > few_rows_of(mode) ? std::max(few, chunk) : few;
 }
 
 // Behind shared prefixes: the most rows that a prefix may have, and the bytes of all rows' two sums and statistics.
@@ -53,7 +56,7 @@ extern "C" int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_
       max_q < 0)
     return -1;
   if (Tq == 0 || B == 0 || max_q == 0) return 0;
-  return workspace_bytes_for(head_dim, static_cast<int64_t>(max_q) * (Hq / H), kFewRows);
+  return workspace_bytes_for(head_dim, static_cast<int64_t>(max_q) * (Hq / H), kCausal);
 }
 
 extern "C" int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim, int32_t B,
@@ -61,7 +64,7 @@ extern "C" int64_t offq_paged_attention_prefix_workspace(int64_t Tq, int32_t Hq,
   if (P < 0 || P > 65535) return -1;
   const int64_t parts = offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q);
   if (parts <= 0 || P == 0) return parts;
-  const int64_t most = workspace_bytes_for(head_dim, shared_rows(Tq, B, max_q, Hq / H), kFewSharedRows);
+  const int64_t most = workspace_bytes_for(head_dim, shared_rows(Tq, B, max_q, Hq / H), kShared);
   return most < 0 ? -1 : most + sums_bytes(Tq, Hq, head_dim);
 }
 
@@ -69,8 +72,7 @@ extern "C" int64_t offq_paged_attention_window_workspace(int64_t Tq, int32_t Hq,
                                                          int32_t max_q, int32_t page_size, int64_t ld_table,
                                                          int32_t window, int32_t sinks) {
   if (!is_pow2(page_size) || page_size < 16 || page_size > 256 || ld_table < 0 || window < 1 || sinks < 0) return -1;
-  const int64_t parts = offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q);
-  if (parts <= 0) return parts;
+  if (const int64_t none = offq_paged_attention_workspace(Tq, Hq, H, head_dim, B, max_q); none <= 0) return none;
   AttnArgs a = {};
   a.Tq = Tq;
   a.H = H;
@@ -81,8 +83,9 @@ extern "C" int64_t offq_paged_attention_window_workspace(int64_t Tq, int32_t Hq,
   a.ld_table = ld_table;
   a.window = std::min(window, kMostTokens);
   a.sinks = std::min(sinks, kMostTokens);
-  a.few_rows = kFewRows;
-  return static_cast<int64_t>(max_q) * a.G <= kFewRows && paged_few_whole(a, kWindowed) ? 0 : parts;
+  a.few_rows = few_rows_of(kWindowed);
+  const int64_t rows = static_cast<int64_t>(max_q) * a.G;
+  return rows <= a.few_rows && paged_few_whole(a, kWindowed) ? 0 : workspace_bytes_for(head_dim, rows, kWindowed);
 }
 
 namespace {
@@ -117,8 +120,8 @@ int paged_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, int32_t 
   a.status = device_status_ptr();
   const int64_t own_rows = static_cast<int64_t>(a.max_q) * a.G;
   const int64_t most_rows = mode == kShared ? shared_rows(a.Tq, a.B, a.max_q, a.G) : own_rows;
-  a.few_rows = mode == kShared ? kFewSharedRows : kFewRows;
-  const int64_t parts = workspace_bytes_for(head_dim, most_rows, a.few_rows);
+  a.few_rows = few_rows_of(mode);
+  const int64_t parts = workspace_bytes_for(head_dim, most_rows, mode);
   if (a.status == nullptr || parts < 0) return OFFQ_ERR_CUDA;
   a.whole = paged_few_whole(a, mode);
   int64_t need = mode == kShared ? parts + sums_bytes(a.Tq, a.Hq, head_dim) : parts;

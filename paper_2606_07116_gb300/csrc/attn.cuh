@@ -250,8 +250,8 @@ __device__ __forceinline__ void write_stats(const AttnArgs& a, int b, int first,
 // The few-row form of offq_paged_attention (csrc/attn_few.cu): rows n * G of a sequence that it takes, its
 // workspace, and its launch with arguments already checked.
 constexpr int kFewRows = 16;
-// Behind shared prefixes it takes groups of 8 or 16 rows, up to this many in all.
-constexpr int kFewSharedRows = 32;
+// Under a window and behind shared prefixes it takes groups of 8 or 16 rows, up to this many in all.
+constexpr int kFewGroupedRows = 32;
 // Under a window or behind shared prefixes: whether every CTA gets a whole unit, so that no parts are joined behind it and a call
 // under a window needs no workspace. So where there are no more units than CTAs and none is longer than this many stages of 32
 // tokens. One token of a stream with a window of 1024: 19.8 us a call against 25.1 split, where the host bounds it; 13.5 against

@@ -144,17 +144,19 @@ __device__ __forceinline__ int stages_of(const AttnArgs& a, const PagedSeq& s) {
   return max(1, (s.len + kTile - 1) / kTile);
 }
 
-// Behind shared prefixes a sequence's rows may be several groups of what the kernel holds. A unit of its work is a group and a
+// Behind shared prefixes, and under a window in the kernel of 16 rows, a sequence's rows may be several groups of what it holds. A unit of its work is a group and a
 // head, number group * H + head, and the groups read the same pages one after the other, from the L2 but for the first.
 constexpr int kMostGroups = 4;
 template <AttnMode M, int ROWS>
+constexpr bool kGrouped = M == kShared || (M == kWindowed && ROWS == 16);
+template <AttnMode M, int ROWS>
 __device__ __forceinline__ int groups_of(const AttnArgs& a, const PagedSeq& s) {
-  return M == kShared ? (s.n * a.G + ROWS - 1) / ROWS : 1;
+  return kGrouped<M, ROWS> ? (s.n * a.G + ROWS - 1) / ROWS : 1;
 }
 // The units of all sequences as one list: unit u of sequence b (fits an int: two lists of 65535 sequences, 4096 heads).
-template <AttnMode M>
+template <AttnMode M, int ROWS>
 __device__ __forceinline__ int unit_id(const AttnArgs& a, int b, int u) {
-  return b * (M == kShared ? kMostGroups : 1) * a.H + u;
+  return b * (kGrouped<M, ROWS> ? kMostGroups : 1) * a.H + u;
 }
 struct Unit {
   int b, h, row0;
@@ -162,7 +164,7 @@ struct Unit {
 template <AttnMode M, int ROWS>
 __device__ __forceinline__ Unit unit_at(const AttnArgs& a, int id) {
   const int b = id / a.H;
-  if constexpr (M == kShared) return {b / kMostGroups, id - b * a.H, b % kMostGroups * ROWS};
+  if constexpr (kGrouped<M, ROWS>) return {b / kMostGroups, id - b * a.H, b % kMostGroups * ROWS};
   return {b, id - b * a.H, 0};
 }
 
@@ -355,7 +357,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
     PagedSeq s = s0;
     int stages = stages_of(a, s);
     int row0 = 0, pgroup = 0, pgroups = 1;  // this unit's first row; where the copies are
-    if constexpr (M == kShared) {
+    if constexpr (kGrouped<M, L::kRows>) {
       pgroup = h / a.H;
       pgroups = groups_of<M, L::kRows>(a, s);
       h %= a.H;
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         if (++ph == a.H) {
           ph = 0;
           next = true;
-          if constexpr (M == kShared) {
+          if constexpr (kGrouped<M, L::kRows>) {
             next = ++pgroup == pgroups;
             if (next) pgroup = 0;
           }
@@ -439,7 +441,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
             pstages = stages_of(a, n);
           } while (pstages == 0);
           plen = n.len;
-          if constexpr (M == kShared) pgroups = groups_of<M, L::kRows>(a, n);
+          if constexpr (kGrouped<M, L::kRows>) pgroups = groups_of<M, L::kRows>(a, n);
           if constexpr (M == kWindowed) {
             pfrom = window_from(a, position<M>(n) + 1);
             pshift = window_gap(a, position<M>(paged_seq<M>(a, pb)), kTile).shift;
@@ -467,7 +469,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         begin = false;
         t_first = t;
         rows = s.n * a.G;
-        if constexpr (M == kShared) rows = min(rows - row0, L::kRows);
+        if constexpr (kGrouped<M, L::kRows>) rows = min(rows - row0, L::kRows);
         sees_least = M == kShared ? min(s.len, max(0, s.at + 1)) : max(0, s.len - s.n + 1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -695,7 +697,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
       }
       if (!complete && lane == 0) {
         ctrl->rows[2 * warp + (first_part ? 0 : 1)] = make_int2(s.first, rows);
-        ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, M == kShared ? row0 / L::kRows * a.H + h : h, t_first, t == stages ? -1 : t);
+        ctrl->part[2 * warp + (first_part ? 0 : 1)] = make_int4(b, kGrouped<M, L::kRows> ? row0 / L::kRows * a.H + h : h, t_first, t == stages ? -1 : t);
       }
       first_part = false;
       begin = true;
@@ -705,7 +707,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
         if (++h == a.H) {
           h = 0;
           next = true;
-          if constexpr (M == kShared) {
+          if constexpr (kGrouped<M, L::kRows>) {
             row0 += L::kRows;
             next = row0 >= s.n * a.G;
             if (next) row0 = 0;
@@ -728,7 +730,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kWarps * 32, 1) paged_few_ke
   constexpr int kParts = 2 * L::kWarps;
   static_assert(kParts <= 32, "a lane for each part");
   const int4 mypart = lane < kParts ? ctrl->part[lane] : make_int4(-1, 0, 0, 0);
-  const int my_id = mypart.x < 0 ? -1 : unit_id<M>(a, mypart.x, mypart.y);
+  const int my_id = mypart.x < 0 ? -1 : unit_id<M, L::kRows>(a, mypart.x, mypart.y);
   const uint32_t same_id = __match_any_sync(kAllLanes, my_id);
   uint32_t left = __ballot_sync(kAllLanes, my_id >= 0 && __ffs(same_id) - 1 == lane);  // the first part of each unit
   const int slices = max(1, min(L::kRows * (D / 8) / 32, L::kWarps / max(1, __popc(left))));
@@ -894,7 +896,7 @@ namespace offq {
 bool paged_few_whole(const AttnArgs& a, AttnMode mode) {
   if (mode == kCausal) return false;
   const int64_t own = static_cast<int64_t>(a.max_q) * a.G, held = std::min<int64_t>(own, kFewRows) > 8 ? 16 : 8;
-  auto groups = [&](int64_t rows) { return mode == kShared ? (std::min<int64_t>(rows, a.few_rows) + held - 1) / held : 1; };
+  auto groups = [&](int64_t rows) { return (std::min<int64_t>(rows, a.few_rows) + held - 1) / held; };
   int64_t units = groups(own) * a.B, tokens = a.ld_table << a.page_shift;
   if (mode == kWindowed) tokens = std::min(tokens, static_cast<int64_t>(a.window) + a.sinks + a.max_q + 2 * kTile);
   if (mode == kShared) {

@@ -38,5 +38,5 @@ def test_positions_behind_the_longest_prefix_fit_an_int():
 def test_unit_numbers_of_the_largest_lists_fit_an_int():
     text = source("attn_few.cu")
     groups = int(re.search(r"constexpr int kMostGroups = (\d+);", text).group(1))
-    shared = int(re.search(r"constexpr int kFewSharedRows = (\d+);", source("attn.cuh")).group(1))
+    shared = int(re.search(r"constexpr int kFewGroupedRows = (\d+);", source("attn.cuh")).group(1))
     assert shared <= 8 * groups and 2 * 65535 * groups * 4096 < 2 ** 31
