@@ -38,6 +38,14 @@ int64_t workspace_bytes_for(int head_dim, int64_t most_rows, AttnMode mode) {
   return most_rows > few_rows_of(mode) ? std::max(few, chunk) : few;
 }
 
+// Whether all sequences of a call that may have many rows take that form, and the other's two kernels (6 us on the device, as much
+// to launch) stay away: where sequences of max_q queries have many, and Tq leaves room for no more than about 16 tiles of shorter
+// ones. (A sequence with few rows in this form costs a tile a head, 10 us and 2.8 for each block of 128 tokens.)
+bool many_rows_alone(const AttnArgs& a) {
+  const int64_t most = std::min<int64_t>(a.max_q, a.Tq), full = (a.Tq + most - 1) / most;
+  return most * a.G > kFewGroupedRows && (a.B - std::min<int64_t>(full, a.B)) * a.H <= 16;
+}
+
 // Behind shared prefixes: the most rows that a prefix may have, and the bytes of all rows' two sums and statistics.
 int64_t shared_rows(int64_t Tq, int32_t B, int32_t max_q, int32_t G) {
   return std::min(Tq, static_cast<int64_t>(B) * max_q) * G;
@@ -120,20 +128,22 @@ int paged_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, int32_t 
   a.status = device_status_ptr();
   const int64_t own_rows = static_cast<int64_t>(a.max_q) * a.G;
   const int64_t most_rows = mode == kShared ? shared_rows(a.Tq, a.B, a.max_q, a.G) : own_rows;
-  a.few_rows = few_rows_of(mode);
+  const bool many = most_rows > few_rows_of(mode), one_form = many && mode != kCausal && many_rows_alone(a);
   const int64_t parts = workspace_bytes_for(head_dim, most_rows, mode);
   if (a.status == nullptr || parts < 0) return OFFQ_ERR_CUDA;
+  a.few_rows = one_form ? 0 : few_rows_of(mode);
   a.whole = paged_few_whole(a, mode);
   int64_t need = mode == kShared ? parts + sums_bytes(a.Tq, a.Hq, head_dim) : parts;
-  if (mode == kWindowed && a.whole && most_rows <= a.few_rows) need = 0;
+  if (mode == kWindowed && a.whole && !many) need = 0;
   if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return OFFQ_ERR_INVALID_ARG;
   if (mode == kShared) {
     a.sums = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + parts);
     a.stats = reinterpret_cast<float2*>(a.sums + 2 * a.Tq * a.Hq * head_dim);
   }
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (const int rc = paged_few(a, mode, dtype, head_dim, s); rc != OFFQ_OK) return rc;
-  if (most_rows > a.few_rows)
+  if (!one_form)
+    if (const int rc = paged_few(a, mode, dtype, head_dim, s); rc != OFFQ_OK) return rc;
+  if (many)
     if (const int rc = paged_chunk(a, mode, dtype, head_dim, s); rc != OFFQ_OK) return rc;
   return mode == kShared ? join_shared(a, dtype, head_dim, s) : OFFQ_OK;
 }

@@ -32,11 +32,11 @@
 // Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 601 us, 800 TFLOP/s, under a window
 // of 4096 with 16 sinks 220 us, 580 TFLOP/s; 256 single tokens behind 32768 shared ones 170 us of 240, 750 TFLOP/s; 16 sequences of
 // 8 tokens over 500 to 6000 122 us. A step (256 rows, 128 keys) takes 2.76 us: a tile's softmax (1.9) and its two products (0.87)
-// follow each other, the other tile's in between. A CTA's first step ends 26 us after the launch. What bounds it: with softmax, widening and reads left out the products take 341 us, since S has
-// both operands in shared memory, which delivers them at 77 % of the tensor rate; reads add about 80, widening 50, the
-// softmax 130. 16 softmax warps of 16 rows were slower (671 against 640), as were maxima taken before the weights (901), products
-// with the first 64 weights while the others are made (window: 239 against 225), scores of 64 keys at a time (328) and queries staged
-// ahead by idle warps (232).
+// follow each other, the other tile's in between. A CTA's first step ends 26 us after the launch. What bounds it: with softmax,
+// widening and reads left out the products of two chunks take 341 us, since S has both operands in shared memory, which delivers
+// them at 77 % of the tensor rate; reads add about 80, widening 50, the softmax 130. 16 softmax warps of 16 rows were slower (671
+// against 640), as were maxima taken before the weights (901), products with the first 64 weights while the others are made
+// (window: 239 against 225), scores of 64 keys at a time (328) and queries staged ahead by idle warps (232).
 #include <algorithm>
 #include <cstddef>
 

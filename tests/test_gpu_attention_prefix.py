@@ -37,11 +37,12 @@ def _check_all(out, lse, pages, P, q64, lens, cu, prefix_lens, cu_prefix, scale,
         check(out[rows], lse[rows], q64[rows], k_mag, k, v, v_mag, scale, seen, dt, joined=True)
 
 
-def _shared(prefix_lens, cu_prefix, lens, news, Hq, H, D, page, dt, seed=0, q_pad=0, table_pad=1, k_off=6.0, scale=None):
+def _shared(prefix_lens, cu_prefix, lens, news, Hq, H, D, page, dt, seed=0, q_pad=0, table_pad=1, k_off=6.0, scale=None,
+            max_q=None):
     P, cu, scale = len(prefix_lens), cumulative(news), scale or D ** -0.5
     pages = Pages([np.ones(L, bool) for L in list(prefix_lens) + list(lens)], H, D, page, seed, k_off, table_pad)
     qb, q64 = queries(sum(news), Hq, D, dt, seed + 1, q_pad)
-    out, lse = _call(pages, P, qb.cuda()[:, :Hq], lens, cu, max(news), prefix_lens, cu_prefix, scale=scale, lse=True)
+    out, lse = _call(pages, P, qb.cuda()[:, :Hq], lens, cu, max_q or max(news), prefix_lens, cu_prefix, scale=scale, lse=True)
     assert Q.offq_get_device_status() == Q.OFFQ_OK
     _check_all(out, lse, pages, P, q64, lens, cu, prefix_lens, cu_prefix, scale, dt)
 
@@ -230,3 +231,13 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     assert all(torch.equal(alone[k], out) for k, out in got)
     assert Q.offq_get_device_status() == Q.OFFQ_OK
+
+
+@pytest.mark.parametrize("Hq,H,D,page,dt", [(8, 2, 128, 64, "bf16"), (5, 1, 64, 16, "f16"), (16, 16, 128, 32, "bf16")])
+def test_few_rows_among_many(Hq, H, D, page, dt):
+    """Sequences, and prefixes, with one query, few and none beside long ones: few enough to take the many-row form with them,
+    or too many. And a bound on the queries that no sequence reaches."""
+    for news in ([1], [3, 0, 1, 70], [90, 1, 2, 1], [1] * 15 + [70, 0, 2, 66, 40], [65] * 3 + [1] * 30):
+        lens, B = [n + 11 * b % 300 for b, n in enumerate(news)], len(news)
+        for max_q in (max(news), max(news) + 100):
+            _shared([140, 0, 33], [0, B // 2, B // 2, max(B // 2, B - 1)], lens, news, Hq, H, D, page, dt, seed=B, max_q=max_q)

@@ -19,13 +19,13 @@ def _lib():
     Q.load_library()
 
 
-def _paged(lens, news, Hq, H, D, page, dt, window, sinks, seed=0, q_pad=0, table_pad=1, k_off=6.0, scale=None):
+def _paged(lens, news, Hq, H, D, page, dt, window, sinks, seed=0, q_pad=0, table_pad=1, k_off=6.0, scale=None, max_q=None):
     seen = [A.in_window(L - n, n, L, window, sinks) for L, n in zip(lens, news)]
     pages = Pages([s.any(0) for s in seen], H, D, page, seed, k_off, table_pad)
     qb, q64 = queries(sum(news), Hq, D, dt, seed + 1, q_pad)
     cu, scale = cumulative(news), scale or D ** -0.5
-    out, lse = Q.paged_attention(qb.cuda()[:, :Hq], pages.cache(), i32(pages.table), i32(lens), i32(cu), max(news + [0]),
-                                 scale=scale, lse=True, window=window, sinks=sinks)
+    out, lse = Q.paged_attention(qb.cuda()[:, :Hq], pages.cache(), i32(pages.table), i32(lens), i32(cu),
+                                 max_q or max(news + [0]), scale=scale, lse=True, window=window, sinks=sinks)
     assert Q.offq_get_device_status() == Q.OFFQ_OK
     out, lse = out.cpu().double().numpy(), lse.cpu().double().numpy()
     for b, L in enumerate(lens):
@@ -315,3 +315,13 @@ def test_a_graph_of_a_large_batch(new):
         c, d = calls()
         assert torch.equal(a, c) and torch.equal(b, d)
     assert Q.offq_get_device_status() == Q.OFFQ_OK
+
+
+@pytest.mark.parametrize("Hq,H,D,page,dt", [(8, 2, 128, 64, "bf16"), (5, 1, 64, 16, "f16"), (16, 16, 128, 32, "bf16")])
+def test_few_rows_among_many(Hq, H, D, page, dt):
+    """Sequences with one query, few and none beside long ones: few enough to take the many-row form with them, or too many.
+    And a bound on the queries that no sequence reaches."""
+    for news in ([1], [3, 0, 1, 70], [90, 1, 2, 1], [1] * 15 + [70, 0, 2, 66, 40], [65] * 3 + [1] * 30):
+        lens = [n + 11 * b % 300 for b, n in enumerate(news)]
+        for max_q in (max(news), max(news) + 100):
+            _paged(lens, news, Hq, H, D, page, dt, 50, 4, seed=len(news), max_q=max_q)
