@@ -1,6 +1,6 @@
 // Attention of many query rows over the paged 4-bit cache (offq_paged_attention where a sequence brings more
-// than 16 rows n * Hq / H per key head: chunks of a prompt, whole prompts, long drafts; under a window; all queries behind a
-// shared prefix where they are more than 32 rows) on the tensor cores.
+// than 16 rows n * Hq / H per key head: chunks of a prompt, whole prompts, long drafts; more than 32 rows under a window, and of
+// all queries behind a shared prefix; fewer as well in batches of long chunks, see attn.cu) on the tensor cores.
 //
 // A row is one query of one head; the rows of a sequence and key head are taken 256 at a time (two tiles of
 // 128) against blocks of 128 cached tokens, as in the prompt kernel: scores, weights and outputs stay in
@@ -30,7 +30,7 @@
 // CTA's work before that.
 //
 // Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 601 us, 800 TFLOP/s, under a window
-// of 4096 with 16 sinks 220 us, 580 TFLOP/s; 256 single tokens behind 32768 shared ones 170 us of 240, 750 TFLOP/s; 16 sequences of
+// of 4096 with 16 sinks 215 us, 595 TFLOP/s; 256 single tokens behind 32768 shared ones 170 us of 240, 750 TFLOP/s; 16 sequences of
 // 8 tokens over 500 to 6000 122 us. A step (256 rows, 128 keys) takes 2.76 us: a tile's softmax (1.9) and its two products (0.87)
 // follow each other, the other tile's in between. A CTA's first step ends 26 us after the launch. What bounds it: with softmax,
 // widening and reads left out the products of two chunks take 341 us, since S has both operands in shared memory, which delivers

@@ -1,5 +1,5 @@
 // Attention of few query rows over the paged 4-bit cache (offq_paged_attention with up to 16 rows
-// n * Hq / H per sequence and key head: single tokens, drafted tokens; under a window; behind shared prefixes up to 32).
+// n * Hq / H per sequence and key head: single tokens, drafted tokens; under a window and behind shared prefixes up to 32).
 //
 // Every cached byte is read once for all rows of its key head, so the cache bounds it: D + 16 bytes per
 // token and head (144 at D = 128) against 4 D multiply-adds per row.
