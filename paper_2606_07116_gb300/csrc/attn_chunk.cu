@@ -682,7 +682,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                       const int key = 32 * q + 8 * k + e;
                       bool hidden = out || key >= sees[x];
                       if constexpr (M == kWindowed) hidden |= key < from[x] && key >= a.sinks - past;
-                      if (hidden) s[x >> 1][4 * k + 2 * (x & 1) + e] = 0x7FFFFFFFu;  // NaN
+                      uint32_t& score = s[x >> 1][4 * k + 2 * (x & 1) + e];
+                      score = hidden ? 0x7FFFFFFFu : score;  // NaN
                     }
                 }
               }
@@ -704,8 +705,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
                     float y0, y1;
                     unpack2(fma2v(pack2(__uint_as_float(e[0]), __uint_as_float(e[1])), a2, fma2v(b2, pack2(qs[x], qs[x]), m2[x])), y0, y1);
                     if constexpr (hide.value) {
-                      if (e[0] == 0x7FFFFFFFu) y0 = -INFINITY;
-                      if (e[1] == 0x7FFFFFFFu) y1 = -INFINITY;
+                      y0 = e[0] == 0x7FFFFFFFu ? -INFINITY : y0;
+                      y1 = e[1] == 0x7FFFFFFFu ? -INFINITY : y1;
                     }
                     const uint64_t p2 = pack2(ex2(y0), ex2(y1));
                     lb[x] = add2_rn(lb[x], p2);
@@ -852,6 +853,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const AttnArgs a) {
               }
             }
           }
+          __syncwarp();  // statistics were written by some lanes; outputs are read by whole warps
 #pragma unroll 1
           for (int q = 0; q < D / 32; ++q) {
             uint32_t o[2][16];

@@ -494,14 +494,14 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
               if (!__any_sync(kAllLanes, hidden != 0u)) continue;
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (hidden >> e & 1u) s[32 * q + e] = 0xFF800000u;  // -inf
+                s[32 * q + e] = hidden >> e & 1u ? 0xFF800000u : s[32 * q + e];  // -inf
             }
           }
         } else if ((j + 1) * kKt > (a.causal ? min(my_row0 + 1, n) : n)) {
           const int valid = (a.causal ? min(row + 1, n) : n) - j * kKt;
 #pragma unroll
           for (int e = 0; e < kKt; ++e)
-            if (e >= valid) s[e] = 0xFF800000u;  // -inf
+            s[e] = e >= valid ? 0xFF800000u : s[e];  // -inf
         }
         float tops[2] = {-INFINITY, -INFINITY};
 #pragma unroll
@@ -546,7 +546,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_ready[i][q >> 1]));
+            mbar_arrive_if(smem_u32(&ctrl->p_ready[i][q >> 1]), lane == 0);
           }
         }
         float x, y;
@@ -555,6 +555,7 @@ prompt_kernel(const AttnArgs a, const __grid_constant__ PromptMaps maps) {
       }
       if (ok) ok = wait(&ctrl->o_full[i], no++);
       if (ok) {
+        __syncwarp();
         tc_fence_after();
         // Outputs as fragments, four words of a row from four lanes: a lane then writes 16 bytes next to its neighbours' (64 bytes of
         // a row). With a row a lane each store touched 32 lines, and an item's took 4 us.

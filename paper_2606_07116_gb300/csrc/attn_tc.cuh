@@ -49,6 +49,18 @@ __device__ __forceinline__ void mma_16_ts(uint32_t d_tmem, uint32_t a_tmem, uint
 
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// The lanes for which `yes` holds arrive, and the warp stays together: the instruction is predicated, not branched around.
+__device__ __forceinline__ void mbar_arrive_if(uint32_t bar, bool yes) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.u32 p, %1, 0;\n"
+      "@p mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];\n"
+      "}\n" ::"r"(bar),
+      "r"(static_cast<uint32_t>(yes))
+      : "memory");
+}
+
 // Each thread of the warp reads 128 consecutive 32-bit columns of its TMEM lane; they are there when it returns.
 __device__ __forceinline__ void tmem_ld_128cols(uint32_t taddr, uint32_t (&r)[128]) {
   asm volatile(
