@@ -39,11 +39,26 @@ int64_t workspace_bytes_for(int head_dim, int64_t most_rows, AttnMode mode) {
 }
 
 // Whether all sequences of a call that may have many rows take that form, and the other's two kernels (6 us on the device, as much
-// to launch) stay away: where sequences of max_q queries have many, and Tq leaves room for no more than about 16 tiles of shorter
-// ones. (A sequence with few rows in this form costs a tile a head, 10 us and 2.8 for each block of 128 tokens.)
-bool many_rows_alone(const AttnArgs& a) {
-  const int64_t most = std::min<int64_t>(a.max_q, a.Tq), full = (a.Tq + most - 1) / most;
-  return most * a.G > kFewGroupedRows && (a.B - std::min<int64_t>(full, a.B)) * a.H <= 16;
+// to launch) stay away. A sequence with few rows costs a tile a head there, and a tile its blocks of 128 tokens and kTileBlocks
+// more, 2.8 us each on one SM. How many there can be: of B sequences of up to `most` queries that share Tq, at most
+// (B most - Tq) / (most - few) have no more than `few`; prefixes with few rows have one of them behind each. Their tokens are what
+// tables and windows have room for, as lengths stand on the device. (Rows of q outside the sequences are counted as theirs: with
+// many of them a batch of short sequences may be taken for long ones.)
+// Measured, one chunk of 1000 tokens beside 1, 4 and 8 short sequences, 2 to 32 key heads, under a window and behind 4000 tokens: up
+// to 600 blocks this form alone is 3 to 15 us faster (137 us against 147 for 600), at 1000 between 9 faster and 4 slower, at 1600 up
+// to 12 slower, at 3200 6 to 31. Tables with more room than their sequences have tokens count for the two forms.
+bool many_rows_alone(const AttnArgs& a, AttnMode mode) {
+  constexpr int64_t kMostShortBlocks = 1000, kTileBlocks = 4;
+  const int64_t most = std::min<int64_t>(a.max_q, a.Tq), few = kFewGroupedRows / a.G;
+  if (most <= few) return false;
+  const int64_t spare = static_cast<int64_t>(a.B) * most - a.Tq;
+  const int64_t short_ones = std::min<int64_t>(a.B, std::max<int64_t>(0, spare) / (most - few));
+  auto blocks = [&](int64_t tokens) { return (tokens + 127) / 128 + kTileBlocks; };
+  int64_t tokens = a.ld_table << a.page_shift;
+  if (mode == kWindowed) tokens = std::min(tokens, static_cast<int64_t>(a.window) + a.sinks + few + 16);
+  int64_t cost = short_ones * blocks(tokens);
+  if (mode == kShared) cost += std::min<int64_t>(a.P, short_ones) * blocks(a.ld_prefix << a.page_shift);
+  return cost * a.H <= kMostShortBlocks;
 }
 
 // Behind shared prefixes: the most rows that a prefix may have, and the bytes of all rows' two sums and statistics.
@@ -128,7 +143,7 @@ int paged_call(AttnArgs& a, AttnMode mode, int dtype, int32_t head_dim, int32_t 
   a.status = device_status_ptr();
   const int64_t own_rows = static_cast<int64_t>(a.max_q) * a.G;
   const int64_t most_rows = mode == kShared ? shared_rows(a.Tq, a.B, a.max_q, a.G) : own_rows;
-  const bool many = most_rows > few_rows_of(mode), one_form = many && mode != kCausal && many_rows_alone(a);
+  const bool many = most_rows > few_rows_of(mode), one_form = many && mode != kCausal && many_rows_alone(a, mode);
   const int64_t parts = workspace_bytes_for(head_dim, most_rows, mode);
   if (a.status == nullptr || parts < 0) return OFFQ_ERR_CUDA;
   a.few_rows = one_form ? 0 : few_rows_of(mode);
