@@ -744,9 +744,10 @@ int64_t offq_paged_attention_window_workspace(int64_t Tq, int32_t Hq, int32_t H,
  * pages prefix_table[g], the sequences cu_prefix[g] .. cu_prefix[g + 1] - 1 share it,
  * and their block_table and lens list the tokens after it. Query i of a sequence sees
  * all of its prefix and tokens 0 .. len - n + i of its own (none where that is
- * negative). Each prefix is read once for all queries of its sequences, whose rows in
- * q follow each other. Every part of a row is summed as in offq_paged_attention, and
- * both are joined in fp32.
+ * negative). Each prefix is read for the queries of all its sequences together, whose
+ * rows in q follow each other: once for 8 or 16 of at most 32 rows (queries times
+ * Hq / H), once for 256 of more, as a rule from the L2 after the first time. Every part
+ * of a row is summed as in offq_paged_attention, and both are joined in fp32.
  *   prefix_table  device, [P][ld_prefix] int32, as block_table (the pages may be
  *             in other rows too).   prefix_lens  device, [P] int32.
  *   cu_prefix device, [P + 1] int32, non-decreasing, cu_prefix[P] <= B. Sequences
@@ -757,7 +758,10 @@ int64_t offq_paged_attention_window_workspace(int64_t Tq, int32_t Hq, int32_t H,
  *             device status word.
  *   P         prefixes, up to 65535 (0: offq_paged_attention).
  *   workspace offq_paged_attention_prefix_workspace(...) bytes: 8 head_dim + 16
- *             for each query and head on top of offq_paged_attention's.
+ *             for each query and head on top of partial sums, whose size goes by
+ *             the rows that a prefix may have and can be more or less than
+ *             offq_paged_attention's (single tokens: 2.5 MB there, 40 MB where
+ *             more than 32 rows may share a prefix).
  */
 int offq_paged_attention_prefix(const void* q, int dtype, int64_t Tq, int32_t Hq, int32_t H, int32_t head_dim,
                                 int64_t ld_q, const uint8_t* k_codes, const float* k_params, const uint8_t* v_codes,

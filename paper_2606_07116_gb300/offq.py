@@ -1000,7 +1000,7 @@ def paged_attention(q: torch.Tensor, cache: KV4Cache, block_table: torch.Tensor,
 
     With window, a query sees the window newest tokens up to itself and the first `sinks` of its sequence; pages that no
     query sees may be given back (entries of any value). With prefix, it sees all of its sequence's prefix before those
-    tokens: each prefix is read once for all its sequences. One of the two at a time."""
+    tokens: each prefix is held once and read for all its sequences together. One of the two at a time."""
     Tq, Hq, hd, ld_q = _heads(q)
     pages, H, page_size, _ = _cache_shape(cache, None, hd)
     B = lens.shape[0]

@@ -1,5 +1,6 @@
 """Which kernels a paged call under a window or behind prefixes launches: the few-row form and its joining, the many-row form
-and its, and the joining of both parts of a row behind prefixes. Calls are captured and their launches counted, none runs."""
+and its, and the joining of both parts of a row behind prefixes. Calls are captured and their launches counted, none runs. And
+the workspaces that go with the forms."""
 
 import ctypes
 
@@ -82,3 +83,42 @@ def test_prefixes_that_may_have_few_rows_are_counted():
     """A single token behind 200000 tokens of its own prefix, beside a chunk behind another."""
     assert launches([1000, 1], 1024, 8, 4, prefix=(200000, [1, 1])) == FEW + MANY + BOTH_PARTS
     assert launches([1000, 1], 1024, 8, 4, prefix=(1000, [1, 1])) == MANY + BOTH_PARTS
+
+
+def test_workspaces_behind_prefixes_go_by_the_rows_that_a_prefix_may_have():
+    """Two fp32 sums and statistics for each query and head, and the parts of the form that a prefix's rows take, whatever the
+    sequences' own rows are."""
+    sums = lambda T, Hq, D: T * Hq * (8 * D + 16)  # noqa: E731
+    for D in (64, 128):
+        few, many = Q.paged_attention_workspace(1, 8, 8, D, 1, 1), Q.paged_attention_workspace(100, 8, 8, D, 1, 100)
+        assert 0 < few < many
+        for Hq, H, n, new, parts in ((8, 8, 32, 1, few), (8, 8, 33, 1, many), (32, 8, 8, 1, few), (32, 8, 9, 1, many),
+                                     (32, 8, 64, 1, many), (8, 8, 1, 20, few), (8, 8, 1, 32, few), (8, 8, 1, 33, many)):
+            got = Q.paged_attention_workspace(n * new, Hq, H, D, n, new, prefixes=1)
+            assert got == sums(n * new, Hq, D) + parts, (Hq, H, n, new)
+    assert Q.paged_attention_workspace(64, 32, 8, 128, 64, 1) < Q.paged_attention_workspace(64, 32, 8, 128, 64, 1, 1) - sums(64, 32, 128)
+    assert Q.paged_attention_workspace(20, 8, 8, 128, 1, 20) > Q.paged_attention_workspace(20, 8, 8, 128, 1, 20, 1) - sums(20, 8, 128)
+
+
+@pytest.mark.parametrize("n", [8, 9])
+def test_a_workspace_of_just_the_bytes_asked_for_is_enough(n):
+    """Single tokens of 32 rows behind a prefix, and of 36."""
+    Hq, H, D, page = 32, 8, 128, 16
+    gen = torch.Generator("cuda").manual_seed(n)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cache = Q.kv4_cache(16, H, D, page)
+    for c in (cache.k_codes, cache.v_codes):
+        c.random_(0, 256, generator=gen)
+    for p in (cache.k_params, cache.v_params):
+        p.uniform_(0.1, 0.3, generator=gen)
+    q = torch.randn((n, Hq, D), generator=gen, device="cuda").to(torch.bfloat16)
+    prefix = Q.SharedPrefix(torch.arange(8, **i32)[None], torch.tensor([120], **i32), torch.tensor([0, n], **i32))
+    table = (8 + torch.arange(n, **i32) % 8)[:, None].contiguous()
+    args = (q, cache, table, torch.full((n,), 9, **i32), torch.arange(n + 1, **i32), 1)
+    need = Q.paged_attention_workspace(n, Hq, H, D, n, 1, 1)
+    room = torch.full((need + 256,), 77, dtype=torch.uint8, device="cuda")
+    out = Q.paged_attention(*args, prefix=prefix, workspace=room[:need])
+    assert torch.equal(out, Q.paged_attention(*args, prefix=prefix)) and torch.all(room[need:] == 77)
+    assert Q.offq_get_device_status() == Q.OFFQ_OK
+    with pytest.raises(Q.OffqError):
+        Q.paged_attention(*args, prefix=prefix, workspace=room[:need - 1])
