@@ -94,6 +94,8 @@ class AttentionLayer:
 
     def prompt(self, x: torch.Tensor, lengths) -> torch.Tensor:
         """Whole prompts, packed: x [sum(lengths), hidden]. Fills empty sequences 0 .. len(lengths) - 1."""
+        if self.before:
+            raise ValueError("behind shared tokens a sequence's own are chunks")
         q, k, v = self.heads(x)
         self.pages.reserve(lengths)
         n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
@@ -109,6 +111,10 @@ class AttentionLayer:
     def share(self, x: torch.Tensor) -> torch.Tensor:
         """Tokens x [n, hidden] that every sequence begins with, taken in once. Sequences must be empty, and the layer
         without a window; their own tokens are chunks (extend) then."""
+        if self.seen:
+            raise ValueError("tokens are shared once, and not under a window: attention takes one of the two at a time")
+        if self.pages.lens.any():
+            raise ValueError("shared tokens stand before those of all sequences, which must be empty")
         n, page_size = x.shape[0], self.pages.page_size
         q, k, v = self.heads(x)
         need = -(-n // page_size)

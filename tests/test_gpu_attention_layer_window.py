@@ -112,3 +112,27 @@ def test_a_full_cache_refuses_to_share():
     layer = E.AttentionLayer(HIDDEN, 8, 2, 64, max_len=256, g=512, pages=4, B=2, page_size=16)
     with pytest.raises(RuntimeError):
         layer.share(_rows(65, 1))
+
+
+def test_what_cannot_share_tokens_refuses_to():
+    """A layer with a window, one that shares some already, and one whose sequences hold tokens: each goes on as it was."""
+    def layer(**kw):
+        return E.AttentionLayer(HIDDEN, 8, 2, 64, max_len=256, g=512, pages=30, B=2, page_size=16, **kw)
+
+    def refuses(one):
+        seen, before, free = one.seen, one.before, list(one.pages.free)
+        with pytest.raises(ValueError):
+            one.share(_rows(20, 5))
+        assert one.seen is seen and one.before == before and one.pages.free == free
+    windowed, behind, held = layer(window=24, sinks=4), layer(), layer()
+    refuses(windowed)
+    behind.share(_rows(20, 1))
+    refuses(behind)
+    held.prompt(_rows(9, 2), [4, 5])
+    refuses(held)
+    for one, n, lengths in ((windowed, 3, [3, 3]), (behind, 3, [3, 3]), (held, 2, [6, 7])):
+        one.pages.reserve(lengths)
+        assert torch.isfinite(one.extend(_rows(2 * n, 6), n, _checked(one, []))).all()
+    with pytest.raises(ValueError):
+        behind.prompt(_rows(9, 2), [4, 5])
+    assert Q.offq_get_device_status() == Q.OFFQ_OK
