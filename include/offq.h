@@ -687,7 +687,9 @@ int offq_kv4_paged_read(const uint8_t* k_codes, const float* k_params, const uin
  * more than 16 queries and heads per key head may round it again, up to four
  * times), in a range that follows the largest of the keys that the row sees:
  * less than 2^-25 of that one adds its offset alone. Scales below 2^-64 count
- * as 2^-64 there.
+ * as 2^-64 there. An infinite or NaN pair of a key that a query does not see
+ * does not reach it; one of a value may, where a query of the same call sees it
+ * (0 times infinity): values are to be finite.
  *
  *   q         device, element (t, h, d) at q[t*ld_q + h*head_dim + d], dtype
  *             OFFQ_BF16 or OFFQ_F16 (OFFQ_F32: OFFQ_ERR_UNSUPPORTED), 16-byte
@@ -784,7 +786,10 @@ int64_t offq_paged_attention_workspace(int64_t Tq, int32_t Hq, int32_t H, int32_
  * offq_paged_attention; k and v [T][H][head_dim] with ld_k, ld_v (multiples of 8)
  * of the same type. cu: device, [B + 1] int32, non-decreasing, cu[B] <= T; rows
  * outside cu[0] .. cu[B] are left as they are. What one sequence holds (infinities
- * or NaN too) does not reach another's outputs. Scores, statistics and sums are
+ * or NaN too) does not reach another's outputs, nor do infinities or NaN of a key
+ * those of queries that do not see it. Of a value they may, where it stands in a
+ * block of 128 keys with ones that the query sees (0 times infinity): v is to be
+ * finite. Scores, statistics and sums are
  * fp32; the weights are rounded to the inputs' type for their product with v.
  * Limits as in offq_paged_attention.
  */
