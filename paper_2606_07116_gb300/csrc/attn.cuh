@@ -254,8 +254,10 @@ constexpr int kFewRows = 16;
 constexpr int kFewGroupedRows = 32;
 // Under a window or behind shared prefixes: whether every CTA gets a whole unit, so that no parts are joined behind it and a call
 // under a window needs no workspace. So where there are no more units than CTAs and none is longer than this many stages of 32
-// tokens. One token of a stream with a window of 1024: 19.8 us a call against 25.1 split, where the host bounds it; 13.5 against
-// 12.5 in a graph; two streams behind 500 shared tokens 14.1 against 15.2 there.
+// tokens. A launch less is what it saves: 19 us a call from the host against 25, at any of these lengths (1 to 4 streams of 1 or 4
+// tokens, 2 to 32 key heads). In a graph it crosses at 700 tokens under a window: 10 us against 12 at 400, 12.0 against 12.2 at
+// 700, 13.5 against 12.2 at 1200 and with 16 rows a key head 15.5 against 13; behind 500 shared tokens 14.2 against 15.4, behind
+// 1000 16.2 against 15.6. The limit is the one of calls from the host.
 constexpr int64_t kMostWhole = 40;
 bool paged_few_whole(const AttnArgs& a, AttnMode mode);
 int64_t paged_few_workspace(int head_dim);

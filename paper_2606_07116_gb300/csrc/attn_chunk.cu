@@ -29,8 +29,8 @@
 // Roles: warps 0-3 and 4-7 the softmax of tile 0 and 1, warp 8 issues the MMAs, warps 12-15 widen; all find the
 // CTA's work before that.
 //
-// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 601 us, 800 TFLOP/s, under a window
-// of 4096 with 16 sinks 215 us, 595 TFLOP/s; 256 single tokens behind 32768 shared ones 170 us of 240, 750 TFLOP/s; 16 sequences of
+// Measured (bf16, 32 heads on 8 of 128): two chunks of 900 to 1024 tokens after 15000 to 16000 600 us, 810 TFLOP/s, under a window
+// of 4096 with 16 sinks 215 us, 595 TFLOP/s; 256 single tokens behind 32768 shared ones 174 us of 240, 790 TFLOP/s; 16 sequences of
 // 8 tokens over 500 to 6000 122 us. A step (256 rows, 128 keys) takes 2.76 us: a tile's softmax (1.9) and its two products (0.87)
 // follow each other, the other tile's in between. A CTA's first step ends 26 us after the launch. What bounds it: with softmax,
 // widening and reads left out the products of two chunks take 341 us, since S has both operands in shared memory, which delivers

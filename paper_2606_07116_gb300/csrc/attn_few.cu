@@ -15,8 +15,9 @@
 // page may be gone), and a row's hidden keys are taken out in the stages at the gap alone, as the last stage's are.
 // Shared prefixes: the list begins with the prefixes, each a sequence with all queries that stand behind it, in groups of 8 or 16
 // rows, and goes on with the sequences' own tokens. Sums and statistics of both go to memory (csrc/attn_prefix.cu). A group more
-// reads its pages from the L2 and costs less than the many-row form up to 32 rows (30 sequences of 1 to 3 tokens behind five
-// prefixes, 12 rows each: 99 us, 119 with groups up to 16, 133 in the many-row form).
+// reads its pages from the L2 and costs less than the many-row form up to 32 rows, which is as far as it was built: 8 single tokens
+// of 32 heads on 8 behind 32768 tokens 44 us (four groups of 8) against 74, behind 131072 124 against 190; 32 sequences of 32 rows
+// under a window of 4096 98 (two groups of 16) against 204.
 //
 // A warp stages its tokens itself, by asynchronous copies of 16 bytes a lane (a head's tokens of a page are contiguous)
 // into a ring of its own, and all lanes read fragments for warp-level MMAs of 16 tokens:
